@@ -1,0 +1,216 @@
+"""Performance cases of the 8-bit integer projections.
+
+  quantize  rows in 8 bits with a scale for each (pp_quantize_rows): attention outputs, SwiGLU
+            products, and weights once by output channel
+  norm      x += add, RMSNorm, and the result in 8 bits with a scale for each row (pp_rmsnorm_quant)
+  gemm      product of 8-bit rows with 8-bit weights, a scale for each row and channel, and the
+            epilogues of a decoder layer (pp_gemm_quant)
+
+Buffers, weights and their 8-bit form are resident, as a serving program keeps them.  With ``own``
+false the same results come from elementary torch operations in float32.  8-bit outputs are
+returned as the values they stand for, in bf16.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def listed():
+    return [
+        # attention output of one prompt being generated, 7B width: the smallest call
+        dict(name="quantize-7b-1-prompt", op="quantize", rows=1, d=4096, dtype="bf16"),
+        # loading: one projection's float32 weights by output channel, small model
+        dict(name="quantize-1.3b-weights", op="quantize", rows=11008, d=2048, dtype="f32"),
+        # attention output of the throughput batch: 64 prompts, 27.7k tokens
+        dict(name="quantize-7b-64-prompts", op="quantize", rows=27721, d=4096, dtype="bf16"),
+        # decode step of ten prompts: residual of a bf16 projection added, then the norm
+        dict(name="norm-7b-10-prompts", op="norm", rows=10, d=4096, dtype="bf16", add=True),
+        # a layer's first norm where the residual projection has added to x itself, 16 chat prompts, 13B width
+        dict(name="norm-13b-16-prompts", op="norm", rows=3951, d=5120, dtype="bf16", add=False),
+        # the throughput batch, residual added on the way
+        dict(name="norm-7b-64-prompts", op="norm", rows=27721, d=4096, dtype="bf16", add=True),
+        # QKV projection of a single prompt's decode step: the weights' bytes alone
+        dict(name="gemm-7b-qkv-1-prompt", op="gemm", epi="store", m=1, n=12288, k=4096, dtype="bf16"),
+        # down projection of ten prompts' decode step
+        dict(name="gemm-7b-down-10-prompts", op="gemm", epi="residual", m=10, n=4096, k=11008, dtype="f32"),
+        # gate and up projections of 48 chats in flight, grouped-query 7B
+        dict(name="gemm-7b-gqa-gateup-48-prompts", op="gemm", epi="swiglu", m=48, n=28672, k=4096, dtype="bf16"),
+        # down projection of 16 short prompts of a small model
+        dict(name="gemm-1.3b-down-16-prompts", op="gemm", epi="residual", m=1309, n=2048, k=5504, dtype="f32"),
+        # QKV projection of the evaluation batch of 16 dataset prompts
+        dict(name="gemm-7b-gqa-qkv-16-prompts", op="gemm", epi="store", m=2926, n=6144, k=4096, dtype="bf16"),
+        # gate and up projections of the throughput batch
+        dict(name="gemm-7b-gateup-64-prompts", op="gemm", epi="swiglu", m=27721, n=22016, k=4096, dtype="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _cost(case):
+    w = work(case)
+    return w["bytes"] / 4e12 + w["flops"] / 2e15
+
+
+def draw(rng):
+    """One more case: any operator, type, epilogue and number of rows, widths of toy models to 13B ones."""
+    most = max(_cost(c) for c in listed())
+    while True:
+        op = rng.choice(["quantize", "norm", "gemm", "gemm"])
+        case = dict(op=op, dtype=rng.choice(["bf16", "bf16", "f32"]))
+        rows = _log(rng, 1, 28000)
+        if op == "gemm":
+            case["epi"] = rng.choice(["store", "residual", "swiglu"])
+            if case["epi"] == "residual":
+                case["dtype"] = "f32"
+            case["m"] = rows
+            case["n"] = 32 * _log(rng, 8, 900)
+            case["k"] = 16 * _log(rng, 16, 900)
+        else:
+            case["rows"] = rows
+            case["d"] = 16 * _log(rng, 16, 900)
+            if op == "norm":
+                case["add"] = rng.random() < 0.7
+        if _cost(case) <= most:
+            return case
+
+
+def work(case):
+    e = 2 if case["dtype"] == "bf16" else 4
+    if case["op"] == "gemm":
+        m, n, k = case["m"], case["n"], case["k"]
+        out = {"store": m * n * e, "residual": m * n * 8, "swiglu": m * n // 2 * e}[case["epi"]]
+        return {"bytes": (m + n) * (k + 4) + out, "flops": 2 * m * n * k}
+    r, d = case["rows"], case["d"]
+    if case["op"] == "quantize":
+        return {"bytes": r * d * (e + 1) + 4 * r, "flops": 3 * r * d}
+    return {"bytes": r * d * (5 + (4 + e if case["add"] else 0)) + 4 * (r + d), "flops": 7 * r * d}
+
+
+# ----------------------------------------------------------------------------- inputs
+def _codes(x):
+    """8-bit form of float rows: int8 [r, d] and float32 [r]."""
+    s = x.abs().amax(dim=1) / 127
+    return (x / s[:, None]).round_().to(torch.int8), s
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(1000003 * seed + 29)
+    t = TYPES[case["dtype"]]
+
+    def normal(r, c):
+        return torch.randn((r, c), generator=g, device=DEV)
+
+    def activations(r, d):
+        """Rows of different size with a few channels well above the others."""
+        x = normal(r, d) * torch.exp(0.5 * normal(r, 1))
+        loud = torch.randint(0, d, (max(1, d // 512),), generator=g, device=DEV)
+        x[:, loud] *= 8
+        return x
+
+    s = dict(case)
+    if case["op"] == "gemm":
+        m, n, k = case["m"], case["n"], case["k"]
+        s["a"], s["a_scale"] = _codes(activations(m, k))
+        s["b"], s["b_scale"] = _codes(normal(n, k) * (0.6 / math.sqrt(k)))
+        cols = n // 2 if case["epi"] == "swiglu" else n
+        s["c"] = normal(m, cols) if case["epi"] == "residual" else torch.empty((m, cols), dtype=t, device=DEV)
+        return s
+    r, d = case["rows"], case["d"]
+    s["q"] = torch.empty((r, d), dtype=torch.int8, device=DEV)
+    s["scale"] = torch.empty(r, dtype=torch.float32, device=DEV)
+    s["values"] = torch.empty((r, d), dtype=torch.bfloat16, device=DEV)
+    if case["op"] == "quantize":
+        s["x"] = activations(r, d).to(t)
+    else:
+        s["x"] = activations(r, d)
+        s["gain"] = 1 + 0.2 * normal(1, d)[0]
+        s["add"] = (0.3 * normal(r, d)).to(t) if case["add"] else None
+    return s
+
+
+# ----------------------------------------------------------------------------- one pass
+EPS = 1e-5
+
+
+def run(s):
+    if own:
+        return _run_own(s)
+    if s["op"] == "quantize":
+        return {"values": _plain_values(s["x"].float())}
+    if s["op"] == "norm":
+        x = s["x"]
+        if s["add"] is not None:
+            x.add_(s["add"].float())
+        y = x * torch.rsqrt(x.square().mean(dim=1, keepdim=True) + EPS) * s["gain"]
+        return {"x": x, "values": _plain_values(y)}
+    v = s["a"].float() @ s["b"].float().T * s["a_scale"][:, None] * s["b_scale"]
+    if s["epi"] == "residual":
+        return {"c": s["c"].add_(v)}
+    if s["epi"] == "swiglu":
+        v = v.view(s["m"], -1, 2, 16)
+        gate, up = v[:, :, 0], v[:, :, 1]
+        v = (gate * torch.sigmoid(gate) * up).reshape(s["m"], -1)
+    return {"c": v.to(s["c"].dtype)}
+
+
+def _plain_values(y):
+    scale = y.abs().amax(dim=1, keepdim=True) / 127
+    return (torch.round(y / scale).clamp_(-127, 127) * scale).to(torch.bfloat16)
+
+
+def _run_own(s):
+    from paper_2404_09529_amd import prepack as pp
+
+    dt = pp.PP_BF16 if s["dtype"] == "bf16" else pp.PP_F32
+    if s["op"] == "gemm":
+        m, n, k = s["m"], s["n"], s["k"]
+        if "ws" not in s:
+            s["ws"] = torch.empty(max(pp.pp_gemm_quant_workspace_size(m, n, k), 1), dtype=torch.uint8, device=DEV)
+        epi = {"store": pp.PP_EPI_STORE, "residual": pp.PP_EPI_RESIDUAL, "swiglu": pp.PP_EPI_SWIGLU}[s["epi"]]
+        c = s["c"]
+        pp.pp_gemm_quant(dt, epi, s["a"], k, s["a_scale"], s["b"], k, s["b_scale"], c, c.shape[1], m, n, k, s["ws"])
+        return {"c": c}
+    r, d = s["rows"], s["d"]
+    if s["op"] == "quantize":
+        pp.pp_quantize_rows(dt, s["x"], d, r, d, s["q"], d, s["scale"])
+        return {"values": _values(s)}
+    pp.pp_rmsnorm_quant(dt, s["x"], s["add"], s["gain"], r, d, EPS, s["q"], s["scale"])
+    return {"x": s["x"], "values": _values(s)}
+
+
+def _values(s):
+    return torch.mul(s["q"], s["scale"][:, None], out=s["values"])
+
+
+# ----------------------------------------------------------------------------- in 64 bits
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "gemm":
+        v = torch.mm(s["a"].double(), s["b"].double().t())
+        v *= s["a_scale"].double().unsqueeze(1)
+        v *= s["b_scale"].double().unsqueeze(0)
+        if case["epi"] == "residual":
+            return {"c": s["c"].double() + v}
+        if case["epi"] == "swiglu":
+            blocks = v.unflatten(1, (-1, 32))
+            gate, up = blocks[..., :16], blocks[..., 16:]
+            v = (up * gate / (1 + torch.exp(-gate))).flatten(1)
+        return {"c": v}
+    x = s["x"].double()
+    if case["op"] == "norm":
+        if s["add"] is not None:
+            x = x + s["add"].double()
+            x = x.float().double()          # the stored sum is float32
+        y = x / torch.sqrt((x * x).sum(1, keepdim=True) / case["d"] + EPS) * s["gain"].double()
+    else:
+        y = x
+    top = torch.max(y.abs(), 1, keepdim=True).values
+    q = torch.round(127 * y / top)
+    return {"x": x, "values": q * top / 127} if case["op"] == "norm" else {"values": q * top / 127}
