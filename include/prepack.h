@@ -297,6 +297,61 @@ pp_status pp_final_norm_unpack(const float* x, const float* gain, int32_t d, flo
                                float* hidden, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * 8-bit integer projections, for callers that assemble their own layer loop: activations in 8
+ * bits with a scale for each row (token), weights in 8 bits with a scale for each row (output
+ * channel).  A value is its code times the scale of its row, codes are -127 .. 127, and a layer's
+ * projections are pp_rmsnorm_quant or pp_quantize_rows followed by pp_gemm_quant; weights take
+ * pp_quantize_rows once, when they are loaded.  Same conventions as the single steps.
+ *
+ * The code of a row y of d values: scale = max|y| / 127 (float32, correctly rounded division),
+ * code = y / scale (the float32 quotient) rounded to the nearest integer, ties to even.  A row of zeros, or one so small that the scale rounds to 0, gets scale 0 and codes 0.  A
+ * row holding a NaN or an infinity gets scale NaN and codes 0, so that what is computed from it is
+ * NaN.
+ * ---------------------------------------------------------------------------------------- */
+
+/* q[r] and scale[r] of x[r] for every row: x [rows, d] in dtype (row stride ldx elements), q [rows, d]
+ * 8-bit codes (row stride ldq bytes; bytes between d and ldq are left alone), scale [rows] float32.
+ * d % 16 == 0; ldx and ldq multiples of 16, x and q 16-byte aligned.
+ * Errors: PP_ERR_INVALID_ARG (NULL, negative count, a stride below d), PP_ERR_UNSUPPORTED (d, ldx, ldq or
+ *         an address that is no multiple of 16), PP_ERR_HIP. */
+pp_status pp_quantize_rows(int32_t dtype, const void* x, int64_t ldx, int32_t rows, int32_t d, int8_t* q,
+                           int64_t ldq, float* scale, void* stream);
+
+/* Residual addition, RMSNorm and the 8-bit form of its result in one pass: x += add (skipped when add
+ * is NULL), y[r] = x[r] / sqrt(mean(x[r]^2) + eps) * gain, and q[r], scale[r] the codes of y[r], which is
+ * not itself stored.  x [rows, d] float32, updated in place; add [rows, d] in dtype (the output of a
+ * projection; not overlapping x); gain [d] float32; q [rows, d]; scale [rows] float32.  d % 16 == 0; x, add,
+ * gain and q 16-byte aligned.  The sum of squares is float32, as pp_rmsnorm's.
+ * Errors: PP_ERR_INVALID_ARG (NULL, negative count, eps < 0), PP_ERR_UNSUPPORTED (d or an address that is
+ *         no multiple of 16), PP_ERR_HIP. */
+pp_status pp_rmsnorm_quant(int32_t dtype, float* x, const void* add, const float* gain, int32_t rows, int32_t d,
+                           float eps, int8_t* q, float* scale, void* stream);
+
+/* Bytes of device workspace pp_gemm_quant needs for these sizes (0: none, and the workspace may be
+ * NULL).  Errors: PP_ERR_INVALID_ARG (negative M, N or K not positive, NULL bytes). */
+pp_status pp_gemm_quant_workspace_size(int32_t M, int32_t N, int32_t K, size_t* bytes);
+
+/* Projection GEMM of 8-bit codes: v[m][n] = (sum_k A[m][k] B[n][k]) * a_scale[m] * b_scale[n], the sum exact
+ * in int32, the products with the scales float32; then the epilogue as pp_gemm's:
+ *   PP_EPI_STORE     C [M, N] = v in dtype
+ *   PP_EPI_RESIDUAL  C [M, N] float32 += v (dtype is not read)
+ *   PP_EPI_SWIGLU    C [M, N/2] = SiLU(gate) * up in dtype, B in w_gateup layout (its rows, and b_scale,
+ *                    interleaved in blocks of 16)
+ * A [M, K] int8 (row stride lda bytes), a_scale [M] float32, B [N, K] int8 (row stride ldb bytes), b_scale
+ * [N] float32.  K % 16 == 0 and K <= 131056 (the sum of codes down to -128 fits 32 bits), N % 16 == 0
+ * (SwiGLU: % 32), lda and ldb multiples of 16 up to 8,388,592, ldc % 4 == 0; A, B and C 16-byte aligned.
+ * plan may be NULL; when given (M must be n_rows * capacity), only the plan's row tiles are computed, as
+ * in pp_gemm.  workspace: >= pp_gemm_quant_workspace_size bytes, 256-byte aligned, not used by two
+ * calls at a time.  C overlaps no operand.  Results do not depend on M, the plan or the workspace's contents.
+ * Errors: PP_ERR_INVALID_ARG (NULL pointer, negative size, a stride below its row, unknown epilogue,
+ *         inconsistent plan, misaligned workspace), PP_ERR_BUFFER_TOO_SMALL (workspace),
+ *         PP_ERR_UNSUPPORTED (a size, stride or address outside the above), PP_ERR_HIP. */
+pp_status pp_gemm_quant(int32_t dtype, int32_t epilogue, const int8_t* A, int64_t lda, const float* a_scale,
+                        const int8_t* B, int64_t ldb, const float* b_scale, void* C, int64_t ldc, int32_t M,
+                        int32_t N, int32_t K, const pp_dplan* plan, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * First token (section 2.3: the time to first token is the time to prefill the KV cache and
  * generate the first token; section 4.3 adds the unpacking, which pp_prefill already did).
  * ---------------------------------------------------------------------------------------- */

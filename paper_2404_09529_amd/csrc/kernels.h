@@ -114,6 +114,34 @@ void next_token(int dtype, int k, const void* lm_head, int V, int d, void* works
 // pp_first_token_noalloc (its address looked up once per device).
 hipError_t first_token_scratch(void** ptr);
 
+// ---------------------------------------------------------------------- 8-bit projections
+// Codes and scales of rows (pp_quantize_rows): x [rows, ldx] in dtype, q [rows, ldq], d % 16 == 0.
+void quantize_rows(int dtype, const void* x, int64_t ldx, int rows, int d, int8_t* q, int64_t ldq, float* scale,
+                   hipStream_t s);
+
+// x += add (null: nothing), then the codes and scales of RMSNorm(x) * g (pp_rmsnorm_quant); d % 16 == 0.
+void rmsnorm_quant(int dtype, float* x, const void* add, const float* g, int rows, int d, float eps, int8_t* q,
+                   float* scale, hipStream_t s);
+
+// C = (A B^T) scaled by row and column, with the epilogues kStore, kResidual and kSwiGLU (pp_gemm_quant).
+// out_f32: type of C (kResidual: always float32).
+struct QuantGemm {
+    const int8_t* A;
+    int64_t lda;
+    const float* a_scale;
+    const int8_t* B;
+    int64_t ldb;
+    const float* b_scale;
+    void* C;
+    int64_t ldc;
+    int M, N, K;
+    const int32_t* mtile_m0;   // a plan's row-tile list, or null for every row
+    int n_mtiles;
+    int32_t* part;             // quant_gemm_workspace(M, N, K) bytes
+};
+size_t quant_gemm_workspace(int M, int N, int K);
+void quant_gemm(int epi, bool out_f32, const QuantGemm& g, hipStream_t s);
+
 // ---------------------------------------------------------------------- generation (decode)
 constexpr int kDecodeChunk = 128;   // keys per workgroup of the decode attention
 

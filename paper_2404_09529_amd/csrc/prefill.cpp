@@ -37,25 +37,6 @@ pp_status validate_attention_span(const pp_config* c, const pp_dplan* p) {
     return PP_OK;
 }
 
-pp_status validate_plan(const pp_dplan* p) {
-    if (!p) return pp::fail(PP_ERR_INVALID_ARG, "plan is NULL");
-    if (p->k < 0 || p->capacity < 0 || p->n_rows < 0 || p->max_len < 0 || p->total_len < 0 || p->n_qtiles < 0 ||
-        p->n_mtiles < 0)
-        return pp::fail(PP_ERR_INVALID_ARG, "plan scalars must be non-negative");
-    if (int64_t(p->n_rows) * p->capacity > INT32_MAX)
-        return pp::fail(PP_ERR_INVALID_ARG, "n_rows * capacity overflows int32");
-    const int64_t T = int64_t(p->n_rows) * p->capacity;
-    if (p->total_len > T || p->max_len > p->capacity || int64_t(p->n_mtiles) * PP_MTILE >= T + PP_MTILE ||
-        (p->total_len > 0 && (p->n_qtiles == 0 || p->n_mtiles == 0 || p->max_len == 0)))
-        return pp::fail(PP_ERR_INVALID_ARG, "inconsistent plan (total_len %d, rows %d x %d, max_len %d)",
-                        p->total_len, p->n_rows, p->capacity, p->max_len);
-    if (p->total_len > 0 && (!p->seg_prompt || !p->seg_start || !p->seg_len || !p->prompt_kv_off ||
-                             !p->slot_seg || !p->slot_pos || !p->slot_kv || !p->qtile_seg || !p->qtile_q0 ||
-                             !p->mtile_m0))
-        return pp::fail(PP_ERR_INVALID_ARG, "a device plan array is NULL");
-    return PP_OK;
-}
-
 Layout layout_of(const pp_config* c, const pp_dplan* p) {
     const size_t T = size_t(p->n_rows) * p->capacity;
     const size_t e = elem_size(c->dtype);
@@ -82,6 +63,25 @@ Layout layout_of(const pp_config* c, const pp_dplan* p) {
 }  // namespace
 
 namespace pp {
+
+pp_status validate_plan(const pp_dplan* p) {
+    if (!p) return pp::fail(PP_ERR_INVALID_ARG, "plan is NULL");
+    if (p->k < 0 || p->capacity < 0 || p->n_rows < 0 || p->max_len < 0 || p->total_len < 0 || p->n_qtiles < 0 ||
+        p->n_mtiles < 0)
+        return pp::fail(PP_ERR_INVALID_ARG, "plan scalars must be non-negative");
+    if (int64_t(p->n_rows) * p->capacity > INT32_MAX)
+        return pp::fail(PP_ERR_INVALID_ARG, "n_rows * capacity overflows int32");
+    const int64_t T = int64_t(p->n_rows) * p->capacity;
+    if (p->total_len > T || p->max_len > p->capacity || int64_t(p->n_mtiles) * PP_MTILE >= T + PP_MTILE ||
+        (p->total_len > 0 && (p->n_qtiles == 0 || p->n_mtiles == 0 || p->max_len == 0)))
+        return pp::fail(PP_ERR_INVALID_ARG, "inconsistent plan (total_len %d, rows %d x %d, max_len %d)",
+                        p->total_len, p->n_rows, p->capacity, p->max_len);
+    if (p->total_len > 0 && (!p->seg_prompt || !p->seg_start || !p->seg_len || !p->prompt_kv_off ||
+                             !p->slot_seg || !p->slot_pos || !p->slot_kv || !p->qtile_seg || !p->qtile_q0 ||
+                             !p->mtile_m0))
+        return pp::fail(PP_ERR_INVALID_ARG, "a device plan array is NULL");
+    return PP_OK;
+}
 
 pp_status validate_config(const pp_config* c) {
     if (!c) return pp::fail(PP_ERR_INVALID_ARG, "config is NULL");
@@ -126,6 +126,7 @@ pp_status validate_weights(const pp_config* c, const pp_weights* w) {
 }  // namespace pp
 
 using pp::validate_config;
+using pp::validate_plan;
 using pp::validate_weights;
 
 extern "C" pp_status pp_prefill_workspace_size(const pp_config* cfg, const pp_dplan* plan, size_t* bytes) {

@@ -117,6 +117,11 @@ def lib() -> ctypes.CDLL:
         L.pp_attention.argtypes = [cfgp, dpp, vp, i64, vp, vp, vp, vp]
         L.pp_qkv_projection.argtypes = [cfgp, dpp, vp, vp, vp, vp, vp, vp, vp]
         L.pp_final_norm_unpack.argtypes = [vp, vp, i32, f32, dpp, vp, vp]
+        L.pp_quantize_rows.argtypes = [i32, vp, i64, i32, i32, vp, i64, vp, vp]
+        L.pp_rmsnorm_quant.argtypes = [i32, vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        L.pp_gemm_quant_workspace_size.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.pp_gemm_quant.argtypes = [i32, i32, vp, i64, vp, vp, i64, vp, vp, i64, i32, i32, i32, dpp, vp,
+                                    ctypes.c_size_t, vp]
         L.pp_first_token_workspace_size.argtypes = [cfgp, dpp, ctypes.POINTER(ctypes.c_size_t)]
         L.pp_first_token.argtypes = [cfgp, dpp, vp, vp, vp, ctypes.c_size_t, vp, vp, vp]
         L.pp_first_token_noalloc.argtypes = [cfgp, dpp, vp, vp, vp, vp, vp]
@@ -127,7 +132,9 @@ def lib() -> ctypes.CDLL:
         L.pp_generate.argtypes = [cfgp, wp, gdp, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp]
         for name in ("pp_plan_bounds", "pp_pack", "pp_pack_padded", "pp_prefill_workspace_size", "pp_prefill",
                      "pp_embed", "pp_rmsnorm", "pp_gemm", "pp_rope", "pp_kv_scatter", "pp_attention",
-                     "pp_final_norm_unpack", "pp_first_token_workspace_size", "pp_first_token",
+                     "pp_final_norm_unpack", "pp_quantize_rows", "pp_rmsnorm_quant",
+                     "pp_gemm_quant_workspace_size", "pp_gemm_quant",
+                     "pp_first_token_workspace_size", "pp_first_token",
                      "pp_first_token_noalloc",
                      "pp_gen_layout_make", "pp_decode_workspace_size", "pp_decode_step", "pp_generate"):
             getattr(L, name).restype = ctypes.c_int
@@ -419,6 +426,35 @@ def pp_final_norm_unpack(x, gain, d: int, eps: float, dplan: DevicePlan, hidden,
                                       _stream(stream)), "pp_final_norm_unpack")
 
 
+# ----------------------------------------------------------------------------- 8-bit projections
+def pp_quantize_rows(dtype: int, x, ldx: int, rows: int, d: int, q, ldq: int, scale, stream=None) -> None:
+    """8-bit codes q [rows, d] int8 and scale [rows] float32 of the rows of x."""
+    _check(lib().pp_quantize_rows(dtype, _p(x), ldx, rows, d, _p(q), ldq, _p(scale), _stream(stream)),
+           "pp_quantize_rows")
+
+
+def pp_rmsnorm_quant(dtype: int, x, add, gain, rows: int, d: int, eps: float, q, scale, stream=None) -> None:
+    """x += add (None: nothing), then the codes and scales of RMSNorm(x) * gain."""
+    _check(lib().pp_rmsnorm_quant(dtype, _p(x), _p(add), _p(gain), rows, d, eps, _p(q), _p(scale), _stream(stream)),
+           "pp_rmsnorm_quant")
+
+
+def pp_gemm_quant_workspace_size(M: int, N: int, K: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().pp_gemm_quant_workspace_size(M, N, K, ctypes.byref(n)), "pp_gemm_quant_workspace_size")
+    return n.value
+
+
+def pp_gemm_quant(dtype: int, epilogue: int, A, lda: int, a_scale, B, ldb: int, b_scale, C, ldc: int, M: int, N: int,
+                  K: int, workspace=None, dplan: Optional[DevicePlan] = None, stream=None) -> None:
+    """Product of 8-bit rows A [M, K] and B [N, K] with their scales, and an epilogue of pp_gemm."""
+    _check(lib().pp_gemm_quant(dtype, epilogue, _p(A), lda, _p(a_scale), _p(B), ldb, _p(b_scale), _p(C), ldc, M, N, K,
+                               None if dplan is None else ctypes.byref(dplan.struct), _p(workspace),
+                               0 if workspace is None else workspace.numel() * workspace.element_size(),
+                               _stream(stream)), "pp_gemm_quant")
+
+
+# ----------------------------------------------------------------------------- first token
 def pp_first_token_workspace_size(cfg: PPConfig, dplan: DevicePlan) -> int:
     n = ctypes.c_size_t(0)
     _check(lib().pp_first_token_workspace_size(ctypes.byref(cfg), ctypes.byref(dplan.struct), ctypes.byref(n)),
