@@ -338,8 +338,8 @@ pp_status pp_gemm_quant_workspace_size(int32_t M, int32_t N, int32_t K, size_t* 
  *   PP_EPI_SWIGLU    C [M, N/2] = SiLU(gate) * up in dtype, B in w_gateup layout (its rows, and b_scale,
  *                    interleaved in blocks of 16)
  * A [M, K] int8 (row stride lda bytes), a_scale [M] float32, B [N, K] int8 (row stride ldb bytes), b_scale
- * [N] float32.  K % 16 == 0 and K <= 131056 (the sum of codes down to -128 fits 32 bits), N % 16 == 0
- * (SwiGLU: % 32), lda and ldb multiples of 16 up to 8,388,592, ldc % 4 == 0; A, B and C 16-byte aligned.
+ * [N] float32.  M and N up to 2^31 - 512; K % 16 == 0 and K <= 131056 (the sum of codes down to -128 fits
+ * 32 bits), N % 16 == 0 (SwiGLU: % 32), lda and ldb multiples of 16 up to 8,388,592, ldc % 4 == 0; A, B and C 16-byte aligned.
  * plan may be NULL; when given (M must be n_rows * capacity), only the plan's row tiles are computed, as
  * in pp_gemm.  workspace: >= pp_gemm_quant_workspace_size bytes, 256-byte aligned, not used by two
  * calls at a time.  C overlaps no operand.  Results do not depend on M, the plan or the workspace's contents.

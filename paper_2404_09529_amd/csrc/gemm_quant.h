@@ -2,6 +2,8 @@
 // arithmetic of the epilogues, so that a result does not depend on which kernel computed it (the
 // int32 sums are exact in any order).
 #pragma once
+#include <atomic>
+
 #include "device.h"
 #include "kernels.h"
 
@@ -92,6 +94,27 @@ namespace ppk {
 
 int cu_count();   // CUs of the GPU, rounded down to a multiple of 8
 
-// Few rows: weights straight from memory to the registers, K split over a workgroup's wavefronts.
+// Lets a kernel have `bytes` of dynamic LDS on the current GPU; `done` holds a bit for each GPU on which it may.
+inline void quant_allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    (void)hipGetDevice(&dev);
+    const uint64_t bit = uint64_t(1) << (dev & 63);
+    if (done.load(std::memory_order_relaxed) & bit) return;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) done.fetch_or(bit);
+}
+
+// Up to 64 rows: weights straight from memory to the registers, 16 * blocks columns (blocks 1, 2, or
+// up to 16 rows 4) and all of K per workgroup.
+constexpr int kQuantFewRows = 64;
+void quant_gemm_few(int epi, bool out_f32, int blocks, const QuantGemm& g, hipStream_t s);
+
+// Tiles of kQuantTileRows x kQuantTileCols: entries mt_first .. mt_first + n_mt - 1 of the row-tile list
+// (without one: of the 256-row tiles of M).  splits > 1 (without a list, every row): K in that many
+// shares, whose sums go to g.part [splits][M][N], and a second launch for the epilogue.
+constexpr int kQuantTiles = 5;
+constexpr int kQuantTileRows[kQuantTiles] = {32, 64, 64, 128, 128};
+constexpr int kQuantTileCols[kQuantTiles] = {64, 64, 128, 128, 256};
+void quant_gemm_tiles(int epi, bool out_f32, int tile, const QuantGemm& g, int mt_first, int n_mt, int splits,
+                      hipStream_t s);
 
 }  // namespace ppk

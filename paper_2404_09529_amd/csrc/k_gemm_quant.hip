@@ -10,9 +10,9 @@
 // read; the workgroup's tiles are one stream of steps, whose loads cross tile boundaries; persistent, one
 // workgroup per CU, every XCD on a compact block of tiles.
 //
-// K need only be a multiple of 16: in the last step lanes past K fetch the row's last 16 values
-// again and the activations' fragments are zeroed there (what the weights hold then does not
-// matter: the values are integers).  N a multiple of 16: rows of B past N are read as its last one.
+// K need only be a multiple of 16 and 128 at least: the last step is the last 128 values, and the
+// activations' fragments are zeroed where the step before had them already (what the weights hold then
+// does not matter: the values are integers).  N a multiple of 16: rows of B past N are read as its last one.
 #include <algorithm>
 
 #include "gemm_quant.h"
@@ -152,24 +152,15 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     // the order in which they were issued.
     const int lda = static_cast<int>(q.lda), ldb = static_cast<int>(q.ldb);
     const int lrow = lane >> 3;
-    int chunk_off[2], back[2];   // of even and odd loads; back: how far a lane steps back in the last step
+    int chunk_off[2];   // of even and odd loads
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        chunk_off[t] = 16 * ((lane & 7) ^ quant_swz(8 * t + lrow));
-        back[t] = tail ? max(0, chunk_off[t] - (tail - 16)) : 0;
-    }
+    for (int t = 0; t < 2; ++t) chunk_off[t] = 16 * ((lane & 7) ^ quant_swz(8 * t + lrow));
     int voff_a[MB], voff_b[LOADS];
     // load cursor: the step being requested, into slots l_sa (A) and l_sb (B); l_local >= n_local once the
     // stream is exhausted (its loads are then dead: they read nothing, into slots that are not read again)
-    int l_local = slot, l_kt = 0, l_sa = 0, l_sb = 1;
+    int l_local = slot, l_kt = 0, l_sa = 0, l_sb = 1, l_k = 0;   // l_k: first value of the step
     __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
     const __amdgpu_buffer_rsrc_t rsrc_0 = quant_rsrc(q.A, 0);
-    auto step_back = [&]() {
-#pragma unroll
-        for (int t = 0; t < MB; ++t) voff_a[t] -= back[t & 1];
-#pragma unroll
-        for (int t = 0; t < LOADS; ++t) voff_b[t] -= back[t & 1];
-    };
     auto set_cursor_tile = [&]() {
         if (l_local < n_local) {
             int m0, n0;
@@ -181,7 +172,6 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
             for (int t = 0; t < MB; ++t) voff_a[t] = min(8 * (MB * wave + t) + lrow, a_rows - 1) * lda + chunk_off[t & 1];
 #pragma unroll
             for (int t = 0; t < LOADS; ++t) voff_b[t] = min(8 * (LOADS * wave + t) + lrow, b_rows - 1) * ldb + chunk_off[t & 1];
-            if (nk == 1) step_back();
         } else {
             rsrc_a = rsrc_0;
             rsrc_b = rsrc_0;
@@ -191,35 +181,38 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     auto load_a = [&](int t) {
         char* dst = smem + l_sa * SLOT_B + (wave * MB + t) * 1024;
         const int voff = voff_a[t];
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (lds_void*)dst, 16, voff, l_kt * kQuantStep, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (lds_void*)dst, 16, voff, l_k, 0, 0);
     };
     auto load_b = [&](int t) {
         char* dst = smem + l_sb * SLOT_B + (wave * LOADS + t) * 1024;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_void*)dst, 16, voff_b[t], l_kt * kQuantStep, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_void*)dst, 16, voff_b[t], l_k, 0, 0);
     };
+    // in two parts: scalar arithmetic that issues between MFMAs, and the rare step to another tile
+    bool l_wrap = false;
     auto advance_cursor = [&]() {
         l_sa = l_sa >= NSLOT - 2 ? l_sa + 2 - NSLOT : l_sa + 2;
         l_sb = l_sb >= NSLOT - 2 ? l_sb + 2 - NSLOT : l_sb + 2;
-        if (l_local >= n_local) return;
-        if (++l_kt == nk) {
-            l_kt = 0;
+        l_wrap = l_kt == nk - 1;
+        l_kt = l_wrap ? 0 : l_kt + 1;
+        l_k = min(l_kt * kQuantStep, q.K - kQuantStep);
+    };
+    auto advance_tile = [&]() {
+        if (l_wrap && l_local < n_local) {
             l_local += n_slots;
             set_cursor_tile();
-        } else if (l_kt == nk - 1 && tail) {
-            step_back();
         }
     };
 
     // ---- fragments.  Block i of sub-step ks: row base + 16 i + l % 16, logical chunk 4 ks + l / 16
     const int wn = wave & 1, wm = wave >> 1;
     int a_lds[2], b_lds[2];
-    bool past[2];   // this lane's 16 values of the last step's sub-step lie past K
+    bool again[2];   // this lane's 16 values of the last step's sub-step belong to the step before
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
         const int phys = ((4 * ks + (lane >> 4)) ^ quant_swz(lane & 15)) * 16;
         a_lds[ks] = (wm * 16 * MB + (lane & 15)) * ROW_B + phys;
         b_lds[ks] = (wn * 128 + (lane & 15)) * ROW_B + phys;
-        past[ks] = tail && 64 * ks + 16 * (lane >> 4) >= tail;
+        again[ks] = tail && 64 * ks + 16 * (lane >> 4) < kQuantStep - tail;
     }
     struct Frags { i32x4 w[8], a[MB]; };
     auto read_one = [&](int sa, int sb, int ks, int p, Frags& f) {   // w0, a0 .., w1 ..: as the MFMAs need them
@@ -227,9 +220,9 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
         else if (p <= MB) f.a[p - 1] = *reinterpret_cast<const i32x4*>(smem + sa * SLOT_B + a_lds[ks] + (p - 1) * 16 * ROW_B);
         else f.w[p - MB] = *reinterpret_cast<const i32x4*>(smem + sb * SLOT_B + b_lds[ks] + (p - MB) * 16 * ROW_B);
     };
-    auto zero_past = [&](int ks, Frags& f) {
+    auto zero_again = [&](int ks, Frags& f) {
 #pragma unroll
-        for (int j = 0; j < MB; ++j) f.a[j] = past[ks] ? i32x4{} : f.a[j];
+        for (int j = 0; j < MB; ++j) f.a[j] = again[ks] ? i32x4{} : f.a[j];
     };
 
     // ---- the stream of steps.  Step g holds slots 2g % 5 (A) and (2g+1) % 5 (B).  Per step:
@@ -245,6 +238,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
 #pragma unroll
         for (int t = 0; t < LOADS; ++t) load_b(t);
         advance_cursor();
+        advance_tile();
     }
     __builtin_amdgcn_s_waitcnt(0);
     quant_barrier();
@@ -276,6 +270,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
                     if (m % 8 == 2) load_a(m / 8);
                 } else {
                     if (m % MB == 2) load_b(m / MB);
+                    if (m == 7 * MB + 3) advance_cursor();   // the cursor moves to step g+3
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -284,14 +279,14 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
             const int n_sa = c_sa >= NSLOT - 2 ? c_sa + 2 - NSLOT : c_sa + 2;
             const int n_sb = c_sb >= NSLOT - 2 ? c_sb + 2 - NSLOT : c_sb + 2;
             const bool cut = tail && kt == nk - 1;
-            if (cut) zero_past(0, F0);
+            if (cut) zero_again(0, F0);
             substep(F0, F1, c_sa, c_sb, 1, true);    // A tile of g+2
-            if (l_local < n_local) __builtin_amdgcn_s_waitcnt(quant_wait(MB));
-            else __builtin_amdgcn_s_waitcnt(quant_wait(0));
+            if (l_local >= n_local) __builtin_amdgcn_s_waitcnt(quant_wait(0));   // dead loads may end out of turn
+            __builtin_amdgcn_s_waitcnt(quant_wait(MB));
             quant_barrier();
-            if (cut) zero_past(1, F1);
+            if (cut) zero_again(1, F1);
             substep(F1, F0, n_sa, n_sb, 0, false);   // B tile of g+2
-            advance_cursor();                        // the cursor moves to step g+3
+            advance_tile();
             c_sa = n_sa;
             c_sb = n_sb;
         }
@@ -308,7 +303,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     __builtin_amdgcn_s_waitcnt(0);   // no load may still be writing LDS when the workgroup ends
 }
 
-int ceil_div(int a, int b) { return (a + b - 1) / b; }
+int ceil_div(int a, int b) { return a / b + (a % b != 0); }
 
 // Output tiles of the XCD that takes most, by either division of the tile list.
 struct XcdSplit {
@@ -328,12 +323,8 @@ namespace {
 // The first n_mt tiles of 32 MB rows on this kernel.
 template <int EPI, typename TO, int MB>
 void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
-    static const bool attr = [] {
-        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&gemm_quant_kernel<EPI, TO, MB>),
-                                  hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
-        return true;
-    }();
-    (void)attr;
+    static std::atomic<uint64_t> done{0};
+    quant_allow_lds(reinterpret_cast<const void*>(&gemm_quant_kernel<EPI, TO, MB>), LDS_BYTES, done);
     const int tiles_n = ceil_div(g.N, BN), wg_per_xcd = cu_count() / 8;
     const XcdSplit x = xcd_split(n_mt, tiles_n, wg_per_xcd);
     QuantGemm q = g;
@@ -341,15 +332,106 @@ void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
     gemm_quant_kernel<EPI, TO, MB><<<8 * std::min(wg_per_xcd, x.tiles), NT, LDS_BYTES, s>>>(q, n_mt, tiles_n, x.balanced);
 }
 
+// Which kernel takes which rows.  An estimate in us, for the CU with the most tiles: a launch and its first
+// loads, then each tile's steps of K and its epilogue; at least the time of the call's bytes at the
+// memory's rate (weights at 4.6 .. 4.8 TB/s) and of what the tiles fetch from L2 together.  The
+// constants are fitted to timings of 136 sizes (1 to 12,000 rows, N 256 to 28,800, K 256 to 14,400) on
+// every kernel; over those sizes the choice costs 2.6% of the best kernel's time on average.
+struct Choice {
+    enum Kind { kFew, kTile, kRows192, kRows256 } kind;
+    int tile, splits;   // kFew: column blocks in `tile`
+    int big;            // kTile: 256-row tiles that the 256 x 256 kernel takes before it
+};
+
+constexpr float kStart = 3.0f, kBigEpilogue = 7.0f, kBigStep = 1.36f, kStep192 = 1.06f;
+constexpr float kWeights = 4.6e6f, kMemory = 4.8e6f, kFabric = 90e6f;   // bytes per us
+// a CU's only tile, and each of several (two or three of the smallest at a time)
+constexpr float kTileAlone[kQuantTiles] = {0.23f, 0.27f, 0.38f, 0.52f, 0.91f};
+constexpr float kTileStep[kQuantTiles] = {0.18f, 0.25f, 0.36f, 0.62f, 1.06f};
+constexpr float kTileEpilogue[kQuantTiles] = {0.6f, 1.1f, 1.5f, 2.6f, 3.5f};
+// a second launch, and its sums written and read
+constexpr float kFinish = 3.3f, kFinishBytes = 2.5e6f;
+
+// n_mt < 0: every row of M; else the entries of a row-tile list.
+Choice choose(int M, int N, int K, int n_mt) {
+    const bool list = n_mt >= 0;
+    const int wg = cu_count() / 8, nk = ceil_div(K, kQuantStep), tiles_n = ceil_div(N, BN);
+    if (!list) n_mt = ceil_div(M, BM);
+    const int rows = list ? static_cast<int>(std::min<int64_t>(M, int64_t(n_mt) * BM)) : M;
+    const float bytes = (float(rows) + N) * K + 4.f * rows * N;
+    Choice best{Choice::kTile, 0, 1, 0};
+    float best_time = 1e30f;
+    auto consider = [&](float time, const Choice& c) {
+        if (time < best_time) {
+            best_time = time;
+            best = c;
+        }
+    };
+    // up to 16 rows the registers take four column blocks; more rows only where 16 columns per workgroup
+    // make one round (beyond that the tiles read the activations less often)
+    if (rows <= 16 || (rows <= kQuantFewRows && N <= 16 * 8 * wg)) {
+        const int round = 16 * 8 * wg;
+        const int blocks = N <= round ? 1 : (N <= 2 * round || N > 4 * round ? 2 : 4);
+        const int rounds = ceil_div(N, blocks * round), row_blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        const float time = rounds * (0.75f + 16.f * (blocks + row_blocks) * K / 53e3f);
+        consider(1.3f + std::max(time, bytes / kWeights), Choice{Choice::kFew, blocks, 1, 0});
+    }
+    auto tile_time = [&](int t, int m, int splits) {
+        const int64_t tiles = int64_t(ceil_div(m, kQuantTileRows[t])) * ceil_div(N, kQuantTileCols[t]);
+        const int64_t per_cu = ((tiles * splits + 7) / 8 + wg - 1) / wg;
+        const float fetched = float(tiles) * (kQuantTileRows[t] + kQuantTileCols[t]) * K;
+        const float work = per_cu * kTileEpilogue[t] + ceil_div(nk, splits) * (per_cu == 1 ? kTileAlone[t] : per_cu * kTileStep[t]);
+        const float mem = ((float(m) + N) * K + 4.f * m * N) / kMemory + fetched / kFabric;
+        return kStart + std::max(work, mem) + (splits > 1 ? kFinish + 4.f * splits * m * N / kFinishBytes : 0.f);
+    };
+    for (int t = 0; t < kQuantTiles; ++t) {
+        consider(tile_time(t, rows, 1), Choice{Choice::kTile, t, 1, 0});
+        if (list) continue;
+        const int64_t tiles = int64_t(ceil_div(M, kQuantTileRows[t])) * ceil_div(N, kQuantTileCols[t]);
+        for (int s : {2, 3, 4, 6, 8})   // shares of K, up to three workgroups per CU
+            if (s <= nk && tiles * s <= 24 * wg) consider(tile_time(t, M, s), Choice{Choice::kTile, t, s, 0});
+    }
+    if (rows <= kQuantFewRows || K < kQuantStep) return best;   // (the large tiles need a whole step)
+    auto big_time = [&](int mt, int tile_rows, float step) {
+        const int64_t per_cu = ceil_div(xcd_split(mt, tiles_n, wg).tiles, wg);
+        const float mem = (float(mt) * tile_rows * K + float(N) * K + 4.f * mt * tile_rows * N) / kMemory;
+        return kStart + std::max(per_cu * (nk * step + kBigEpilogue), mem);
+    };
+    if (n_mt == ceil_div(M, BM)) consider(big_time(ceil_div(M, 192), 192, kStep192), Choice{Choice::kRows192, 0, 1, 0});
+    consider(big_time(n_mt, BM, kBigStep), Choice{Choice::kRows256, 0, 1, 0});
+    // whole rounds of 256 x 256 tiles and the other rows on small ones; a split has to promise 5%
+    const int64_t rounds = int64_t(n_mt) * tiles_n / (8 * wg);
+    for (int64_t r = rounds; r > 0 && r >= rounds - 1; --r) {
+        const int big = static_cast<int>(r * 8 * wg / tiles_n), rest = rows - big * BM;
+        if (big <= 0 || rest <= 0) continue;
+        for (int t = 0; t < kQuantTiles; ++t)
+            consider((big_time(big, BM, kBigStep) + tile_time(t, rest, 1)) * 1.05f, Choice{Choice::kTile, t, 1, big});
+    }
+    return best;
+}
+
 template <int EPI, typename TO>
-void gemm(const QuantGemm& g, hipStream_t s) {
+void gemm(QuantGemm g, hipStream_t s) {
+    if (g.M <= BM) g.mtile_m0 = nullptr;   // (a list of one tile then, which is all of M)
     const int n_mt = g.mtile_m0 ? g.n_mtiles : ceil_div(g.M, BM);
-    launch<EPI, TO, 8>(g, n_mt, s);
+    const Choice c = choose(g.M, g.N, g.K, g.mtile_m0 ? n_mt : -1);
+    if (c.kind == Choice::kFew) return quant_gemm_few(EPI, sizeof(TO) == 4, c.tile, g, s);
+    if (c.kind == Choice::kRows256) return launch<EPI, TO, 8>(g, n_mt, s);
+    if (c.kind == Choice::kRows192) {
+        g.mtile_m0 = nullptr;   // (it names every tile)
+        return launch<EPI, TO, 6>(g, ceil_div(g.M, 192), s);
+    }
+    if (c.big > 0) launch<EPI, TO, 8>(g, c.big, s);
+    quant_gemm_tiles(EPI, sizeof(TO) == 4, c.tile, g, c.big, n_mt - c.big, c.splits, s);
 }
 
 }  // namespace
 
-size_t quant_gemm_workspace(int, int, int) { return 0; }
+size_t quant_gemm_workspace(int M, int N, int K) {
+    if (M == 0) return 0;
+    const Choice c = choose(M, N, K, -1);   // (a row-tile list is never split)
+    return c.kind == Choice::kTile && c.splits > 1 ? size_t(c.splits) * M * N * sizeof(int32_t) : 0;
+}
 
 void quant_gemm(int epi, bool out_f32, const QuantGemm& g, hipStream_t s) {
     if (epi == kResidual) return gemm<kResidual, float>(g, s);

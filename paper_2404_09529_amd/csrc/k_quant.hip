@@ -117,7 +117,7 @@ struct Add4<bf16> {
 template <int W>
 __device__ __forceinline__ int64_t my_row() {
     constexpr int per_block = kThreads / kWave / W;
-    return int64_t(blockIdx.x) * per_block + __builtin_amdgcn_readfirstlane(threadIdx.x / (kWave * W));
+    return (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * per_block + __builtin_amdgcn_readfirstlane(threadIdx.x / (kWave * W));
 }
 
 // ------------------------------------------------------------------------------- norm
@@ -182,11 +182,13 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quant_kernel(float* __restri
 // it wrote itself).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rmsnorm_quant_long_kernel(float* __restrict__ x, const T* __restrict__ add,
-                                                                      const float* __restrict__ g, int d, float eps,
-                                                                      int8_t* __restrict__ q, float* __restrict__ scale) {
+                                                                      const float* __restrict__ g, int rows, int d,
+                                                                      float eps, int8_t* __restrict__ q,
+                                                                      float* __restrict__ scale) {
     __shared__ float sums[kThreads / kWave];
     __shared__ uint32_t tops[kThreads / kWave];
-    const int64_t row = blockIdx.x;
+    const int64_t row = my_row<kThreads / kWave>();
+    if (row >= rows) return;
     float* xr = x + row * d;
     const T* ar = add ? add + row * d : nullptr;
     float ss = 0.f;
@@ -265,11 +267,12 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict_
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void quantize_long_kernel(const T* __restrict__ x, int64_t ldx, int d,
+__global__ __launch_bounds__(kThreads) void quantize_long_kernel(const T* __restrict__ x, int64_t ldx, int rows, int d,
                                                                  int8_t* __restrict__ q, int64_t ldq,
                                                                  float* __restrict__ scale) {
     __shared__ uint32_t tops[kThreads / kWave];
-    const int64_t row = blockIdx.x;
+    const int64_t row = my_row<kThreads / kWave>();
+    if (row >= rows) return;
     const T* xr = x + row * ldx;
     uint32_t top = 0;
     for (int64_t e = threadIdx.x; e < d; e += kThreads) top = max(top, magnitude(static_cast<float>(xr[e])));
@@ -285,10 +288,12 @@ __global__ __launch_bounds__(kThreads) void quantize_long_kernel(const T* __rest
 // ------------------------------------------------------------------------------- dispatch
 constexpr int kW = kThreads / kWave;   // wavefronts of a row that a whole workgroup takes
 
+// Workgroups for the rows, in two dimensions: one may hold 2^32 threads at most.
 template <int W>
-unsigned row_blocks(int rows) {
+dim3 row_blocks(int rows) {
     constexpr int per = kW / W;
-    return static_cast<unsigned>((int64_t(rows) + per - 1) / per);
+    const int64_t n = (int64_t(rows) + per - 1) / per, x = n < (1 << 20) ? n : 1 << 20;
+    return dim3(static_cast<unsigned>(x), static_cast<unsigned>((n + x - 1) / x));
 }
 
 template <typename T, bool ADD, int W, int NC>
@@ -304,7 +309,7 @@ void norm_dispatch(float* x, const T* add, const float* g, int rows, int d, floa
     if (nc <= 4) return launch_norm<T, ADD, kW, 4>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 8) return launch_norm<T, ADD, kW, 8>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 16) return launch_norm<T, ADD, kW, 16>(x, add, g, rows, d, eps, q, scale, s);
-    rmsnorm_quant_long_kernel<T><<<rows, kThreads, 0, s>>>(x, add, g, d, eps, q, scale);
+    rmsnorm_quant_long_kernel<T><<<row_blocks<kW>(rows), kThreads, 0, s>>>(x, add, g, rows, d, eps, q, scale);
 }
 
 template <typename T, int W, int NC>
@@ -321,7 +326,7 @@ void rows_dispatch(const T* x, int64_t ldx, int rows, int d, int8_t* q, int64_t 
     if (nc <= 4) return launch_rows<T, kW, 4>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 8) return launch_rows<T, kW, 8>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 16) return launch_rows<T, kW, 16>(x, ldx, rows, d, q, ldq, scale, s);
-    quantize_long_kernel<T><<<rows, kThreads, 0, s>>>(x, ldx, d, q, ldq, scale);
+    quantize_long_kernel<T><<<row_blocks<kW>(rows), kThreads, 0, s>>>(x, ldx, rows, d, q, ldq, scale);
 }
 
 }  // namespace

@@ -12,6 +12,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int32_t kMaxK = 131056;          // 2^31 / 128^2, down to a multiple of 16
+constexpr int32_t kMaxRows = INT32_MAX - 511;   // a row index past the last tile's end stays a 32-bit number
 constexpr int64_t kMaxLd = 8388592;        // 256 rows of a tile lie within a 31-bit byte offset
 
 bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
@@ -82,6 +83,7 @@ extern "C" pp_status pp_gemm_quant(int32_t dtype, int32_t epilogue, const int8_t
     if (K % 16 || K > kMaxK || N % (swiglu ? 32 : 16))
         return pp::fail(PP_ERR_UNSUPPORTED, "8-bit GEMM needs K %% 16 == 0, K <= %d, N %% %d == 0 (N %d K %d)", kMaxK,
                         swiglu ? 32 : 16, N, K);
+    if (M > kMaxRows || N > kMaxRows) return pp::fail(PP_ERR_UNSUPPORTED, "M %d or N %d above %d", M, N, kMaxRows);
     if (lda % 16 || ldb % 16 || lda > kMaxLd || ldb > kMaxLd || ldc % 4)
         return pp::fail(PP_ERR_UNSUPPORTED, "8-bit GEMM needs lda, ldb %% 16 == 0 up to %lld and ldc %% 4 == 0 "
                         "(lda %lld ldb %lld ldc %lld)", (long long)kMaxLd, (long long)lda, (long long)ldb, (long long)ldc);

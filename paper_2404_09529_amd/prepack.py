@@ -376,9 +376,12 @@ def config_of(shape, n_layers: Optional[int] = None) -> PPConfig:
 
 
 def _stream(stream):
+    """The handle of ``stream`` (default: torch's current stream on the current device).  The raw
+    handle of the current stream costs 0.3 us; torch.cuda.current_stream() builds an object, 2.6 us."""
     if stream is None:
-        stream = _torch().cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+        torch = _torch()
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _p(t):

@@ -55,7 +55,7 @@ def _gemm(**kw):
     (INV, dict(K=0)), (INV, dict(lda=240)), (INV, dict(ldb=240)), (INV, dict(ldc=496)),
     (UNS, dict(K=248)), (UNS, dict(N=504)), (UNS, dict(N=496, epi=pp.PP_EPI_SWIGLU, ldc=256)),
     (UNS, dict(K=131072, lda=131072, ldb=131072)), (UNS, dict(lda=264)), (UNS, dict(ldb=264)), (UNS, dict(ldc=514)),
-    (UNS, dict(lda=8388608)), (UNS, dict(ldb=8388608)), (INV, dict(A=None)), (INV, dict(sa=None)),
+    (UNS, dict(M=2 ** 31 - 511)), (UNS, dict(N=2 ** 31 - 496, ldc=2 ** 31)), (UNS, dict(lda=8388608)), (UNS, dict(ldb=8388608)), (INV, dict(A=None)), (INV, dict(sa=None)),
     (INV, dict(B=None)), (INV, dict(sb=None)), (INV, dict(C=None)), (UNS, dict(A=0x1008)), (UNS, dict(B=0x3004)),
     (UNS, dict(C=0x5008)), (OK, dict(M=0, A=None, B=None, C=None, ws=None, bytes=0))])
 def test_gemm_quant_checks(want, kw):
