@@ -317,6 +317,11 @@ pp_status pp_final_norm_unpack(const float* x, const float* gain, int32_t d, flo
 pp_status pp_quantize_rows(int32_t dtype, const void* x, int64_t ldx, int32_t rows, int32_t d, int8_t* q,
                            int64_t ldq, float* scale, void* stream);
 
+/* The values that codes stand for: x[r] = q[r] * scale[r] in dtype, the float32 product rounded once (a
+ * layer run in bf16 from weights kept in 8 bits; inspection).  Buffers, sizes and errors as pp_quantize_rows. */
+pp_status pp_dequantize_rows(int32_t dtype, const int8_t* q, int64_t ldq, const float* scale, int32_t rows,
+                             int32_t d, void* x, int64_t ldx, void* stream);
+
 /* Residual addition, RMSNorm and the 8-bit form of its result in one pass: x += add (skipped when add
  * is NULL), y[r] = x[r] / sqrt(mean(x[r]^2) + eps) * gain, and q[r], scale[r] the codes of y[r], which is
  * not itself stored.  x [rows, d] float32, updated in place; add [rows, d] in dtype (the output of a

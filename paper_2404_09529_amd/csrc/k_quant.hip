@@ -3,7 +3,9 @@
 //
 // scale = max|y| / 127, code = round(y / scale).  Both need the whole row before the first code
 // is written, so a row stays in registers between its one read and its one write: memory bounds
-// both kernels.
+// both kernels (27,721 x 4096: quantize_rows of bf16 59 us, 5.8 TB/s; rmsnorm_quant with a bf16 residual 219 us,
+// 5.7 TB/s).  A row of up to four 16-byte chunks per lane is one wavefront's, a longer one a workgroup's: 20,000 rows
+// of 688 bf16 values 9.3 us and 19.4, of 4096 46.2 and 43.5.
 #include "device.h"
 #include "kernels.h"
 #include "prepack.h"
@@ -145,6 +147,9 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quant_kernel(float* __restri
 #pragma unroll
         for (int c = 0; c < NC; ++c) ar[c].load(ra, at(c));
     }
+    u32x4 gr[NC];   // requested with the rest, so that they are there when the sum is
+#pragma unroll
+    for (int c = 0; c < NC; ++c) gr[c] = __builtin_amdgcn_raw_buffer_load_b128(rg, at(c) * 4, 0, 0);
     float v[NC][4], ss = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -164,10 +169,9 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quant_kernel(float* __restri
     uint32_t top = 0;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const u32x4 gg = __builtin_amdgcn_raw_buffer_load_b128(rg, at(c) * 4, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[c][i] = v[c][i] * r * __uint_as_float(gg[i]);
+            v[c][i] = v[c][i] * r * __uint_as_float(gr[c][i]);
             top = max(top, magnitude(v[c][i]));
         }
     }
@@ -285,6 +289,33 @@ __global__ __launch_bounds__(kThreads) void quantize_long_kernel(const T* __rest
     if (threadIdx.x == 0) scale[row] = rc.scale;
 }
 
+// ------------------------------------------------------------------------------- back to values
+// 16 codes per thread.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void dequantize_kernel(const int8_t* __restrict__ q, int64_t ldq,
+                                                              const float* __restrict__ scale, int64_t n, uint32_t per_row,
+                                                              T* __restrict__ x, int64_t ldx) {
+    const int64_t t = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * kThreads + threadIdx.x;
+    if (t >= n) return;
+    int64_t row;
+    uint32_t c;
+    if (n <= UINT32_MAX) {   // (a 32-bit division where it will do)
+        row = static_cast<uint32_t>(t) / per_row;
+        c = static_cast<uint32_t>(t) % per_row;
+    } else {
+        row = t / per_row;
+        c = static_cast<uint32_t>(t % per_row);
+    }
+    const u32x4 codes = *reinterpret_cast<const u32x4*>(q + row * ldq + int64_t(c) * 16);
+    const float s = scale[row];
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = static_cast<float>(static_cast<int8_t>(codes[i / 4] >> (8 * (i % 4)))) * s;
+    T* o = x + row * ldx + int64_t(c) * 16;
+    store8(o, v);
+    store8(o + 8, v + 8);
+}
+
 // ------------------------------------------------------------------------------- dispatch
 constexpr int kW = kThreads / kWave;   // wavefronts of a row that a whole workgroup takes
 
@@ -303,8 +334,11 @@ void launch_norm(float* x, const T* add, const float* g, int rows, int d, float 
 
 template <typename T, bool ADD>
 void norm_dispatch(float* x, const T* add, const float* g, int rows, int d, float eps, int8_t* q, float* scale, hipStream_t s) {
-    const int nc = (d + kThreads * 4 - 1) / (kThreads * 4);   // chunks of a lane of a whole workgroup
-    if (nc <= 1) return launch_norm<T, ADD, kW, 1>(x, add, g, rows, d, eps, q, scale, s);
+    const int of_wave = (d + kWave * 4 - 1) / (kWave * 4);    // chunks of a lane of one wavefront
+    if (of_wave <= 1) return launch_norm<T, ADD, 1, 1>(x, add, g, rows, d, eps, q, scale, s);
+    if (of_wave <= 2) return launch_norm<T, ADD, 1, 2>(x, add, g, rows, d, eps, q, scale, s);
+    if (of_wave <= 4) return launch_norm<T, ADD, 1, 4>(x, add, g, rows, d, eps, q, scale, s);
+    const int nc = (d + kThreads * 4 - 1) / (kThreads * 4);   // and of a whole workgroup
     if (nc <= 2) return launch_norm<T, ADD, kW, 2>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 4) return launch_norm<T, ADD, kW, 4>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 8) return launch_norm<T, ADD, kW, 8>(x, add, g, rows, d, eps, q, scale, s);
@@ -320,8 +354,11 @@ void launch_rows(const T* x, int64_t ldx, int rows, int d, int8_t* q, int64_t ld
 template <typename T>
 void rows_dispatch(const T* x, int64_t ldx, int rows, int d, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
     constexpr int E = 16 / sizeof(T);
+    const int of_wave = (d + kWave * E - 1) / (kWave * E);
+    if (of_wave <= 1) return launch_rows<T, 1, 1>(x, ldx, rows, d, q, ldq, scale, s);
+    if (of_wave <= 2) return launch_rows<T, 1, 2>(x, ldx, rows, d, q, ldq, scale, s);
+    if (of_wave <= 4) return launch_rows<T, 1, 4>(x, ldx, rows, d, q, ldq, scale, s);
     const int nc = (d + kThreads * E - 1) / (kThreads * E);
-    if (nc <= 1) return launch_rows<T, kW, 1>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 2) return launch_rows<T, kW, 2>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 4) return launch_rows<T, kW, 4>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 8) return launch_rows<T, kW, 8>(x, ldx, rows, d, q, ldq, scale, s);
@@ -329,9 +366,25 @@ void rows_dispatch(const T* x, int64_t ldx, int rows, int d, int8_t* q, int64_t 
     quantize_long_kernel<T><<<row_blocks<kW>(rows), kThreads, 0, s>>>(x, ldx, rows, d, q, ldq, scale);
 }
 
+template <typename T>
+void dequantize(const int8_t* q, int64_t ldq, const float* scale, int rows, int d, T* x, int64_t ldx, hipStream_t s) {
+    const int64_t n = int64_t(rows) * (d / 16), blocks = (n + kThreads - 1) / kThreads;
+    const int64_t bx = blocks < (1 << 20) ? blocks : 1 << 20;
+    dequantize_kernel<T><<<dim3(static_cast<unsigned>(bx), static_cast<unsigned>((blocks + bx - 1) / bx)), kThreads, 0, s>>>(
+        q, ldq, scale, n, static_cast<uint32_t>(d / 16), x, ldx);
+}
+
 }  // namespace
 
 namespace ppk {
+
+void dequantize_rows(int dtype, const int8_t* q, int64_t ldq, const float* scale, int rows, int d, void* x, int64_t ldx,
+                     hipStream_t s) {
+    if (dtype == PP_BF16)
+        dequantize(q, ldq, scale, rows, d, static_cast<bf16*>(x), ldx, s);
+    else
+        dequantize(q, ldq, scale, rows, d, static_cast<float*>(x), ldx, s);
+}
 
 void quantize_rows(int dtype, const void* x, int64_t ldx, int rows, int d, int8_t* q, int64_t ldq, float* scale,
                    hipStream_t s) {

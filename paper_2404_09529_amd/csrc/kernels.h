@@ -119,6 +119,10 @@ hipError_t first_token_scratch(void** ptr);
 void quantize_rows(int dtype, const void* x, int64_t ldx, int rows, int d, int8_t* q, int64_t ldq, float* scale,
                    hipStream_t s);
 
+// And back: x [rows, ldx] = q * scale in dtype (pp_dequantize_rows).
+void dequantize_rows(int dtype, const int8_t* q, int64_t ldq, const float* scale, int rows, int d, void* x, int64_t ldx,
+                     hipStream_t s);
+
 // x += add (null: nothing), then the codes and scales of RMSNorm(x) * g (pp_rmsnorm_quant); d % 16 == 0.
 void rmsnorm_quant(int dtype, float* x, const void* add, const float* g, int rows, int d, float eps, int8_t* q,
                    float* scale, hipStream_t s);

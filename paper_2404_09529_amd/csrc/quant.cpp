@@ -25,9 +25,12 @@ pp_status finish(const char* what) {
 
 }  // namespace
 
-extern "C" pp_status pp_quantize_rows(int32_t dtype, const void* x, int64_t ldx, int32_t rows, int32_t d, int8_t* q,
-                                      int64_t ldq, float* scale, void* stream) {
-    pp::clear_error();
+namespace {
+
+// The checks pp_quantize_rows and pp_dequantize_rows share; *done: there is nothing to do.
+pp_status check_rows(int32_t dtype, const void* x, int64_t ldx, int32_t rows, int32_t d, const void* q, int64_t ldq,
+                     const void* scale, bool* done) {
+    *done = false;
     if (dtype != PP_F32 && dtype != PP_BF16) return pp::fail(PP_ERR_INVALID_ARG, "unknown dtype %d", dtype);
     if (rows < 0 || d <= 0) return pp::fail(PP_ERR_INVALID_ARG, "rows %d, d %d", rows, d);
     if (ldx < d || ldq < d)
@@ -35,12 +38,35 @@ extern "C" pp_status pp_quantize_rows(int32_t dtype, const void* x, int64_t ldx,
     if (d % 16 || ldx % 16 || ldq % 16)
         return pp::fail(PP_ERR_UNSUPPORTED, "d %d, ldx %lld and ldq %lld must be multiples of 16", d, (long long)ldx,
                         (long long)ldq);
-    if (rows == 0) return PP_OK;
+    *done = rows == 0;
+    if (*done) return PP_OK;
     if (!x || !q || !scale) return pp::fail(PP_ERR_INVALID_ARG, "NULL buffer");
     if (misaligned(x) || misaligned(q)) return pp::fail(PP_ERR_UNSUPPORTED, "x and q must be 16-byte aligned");
+    return PP_OK;
+}
+
+}  // namespace
+
+extern "C" pp_status pp_quantize_rows(int32_t dtype, const void* x, int64_t ldx, int32_t rows, int32_t d, int8_t* q,
+                                      int64_t ldq, float* scale, void* stream) {
+    pp::clear_error();
+    bool done;
+    if (pp_status st = check_rows(dtype, x, ldx, rows, d, q, ldq, scale, &done)) return st;
+    if (done) return PP_OK;
     (void)hipGetLastError();
     ppk::quantize_rows(dtype, x, ldx, rows, d, q, ldq, scale, static_cast<hipStream_t>(stream));
     return finish("quantize_rows");
+}
+
+extern "C" pp_status pp_dequantize_rows(int32_t dtype, const int8_t* q, int64_t ldq, const float* scale, int32_t rows,
+                                        int32_t d, void* x, int64_t ldx, void* stream) {
+    pp::clear_error();
+    bool done;
+    if (pp_status st = check_rows(dtype, x, ldx, rows, d, q, ldq, scale, &done)) return st;
+    if (done) return PP_OK;
+    (void)hipGetLastError();
+    ppk::dequantize_rows(dtype, q, ldq, scale, rows, d, x, ldx, static_cast<hipStream_t>(stream));
+    return finish("dequantize_rows");
 }
 
 extern "C" pp_status pp_rmsnorm_quant(int32_t dtype, float* x, const void* add, const float* gain, int32_t rows,

@@ -118,6 +118,7 @@ def lib() -> ctypes.CDLL:
         L.pp_qkv_projection.argtypes = [cfgp, dpp, vp, vp, vp, vp, vp, vp, vp]
         L.pp_final_norm_unpack.argtypes = [vp, vp, i32, f32, dpp, vp, vp]
         L.pp_quantize_rows.argtypes = [i32, vp, i64, i32, i32, vp, i64, vp, vp]
+        L.pp_dequantize_rows.argtypes = [i32, vp, i64, vp, i32, i32, vp, i64, vp]
         L.pp_rmsnorm_quant.argtypes = [i32, vp, vp, vp, i32, i32, f32, vp, vp, vp]
         L.pp_gemm_quant_workspace_size.argtypes = [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
         L.pp_gemm_quant.argtypes = [i32, i32, vp, i64, vp, vp, i64, vp, vp, i64, i32, i32, i32, dpp, vp,
@@ -132,7 +133,7 @@ def lib() -> ctypes.CDLL:
         L.pp_generate.argtypes = [cfgp, wp, gdp, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp]
         for name in ("pp_plan_bounds", "pp_pack", "pp_pack_padded", "pp_prefill_workspace_size", "pp_prefill",
                      "pp_embed", "pp_rmsnorm", "pp_gemm", "pp_rope", "pp_kv_scatter", "pp_attention",
-                     "pp_final_norm_unpack", "pp_quantize_rows", "pp_rmsnorm_quant",
+                     "pp_final_norm_unpack", "pp_quantize_rows", "pp_dequantize_rows", "pp_rmsnorm_quant",
                      "pp_gemm_quant_workspace_size", "pp_gemm_quant",
                      "pp_first_token_workspace_size", "pp_first_token",
                      "pp_first_token_noalloc",
@@ -434,6 +435,12 @@ def pp_quantize_rows(dtype: int, x, ldx: int, rows: int, d: int, q, ldq: int, sc
     """8-bit codes q [rows, d] int8 and scale [rows] float32 of the rows of x."""
     _check(lib().pp_quantize_rows(dtype, _p(x), ldx, rows, d, _p(q), ldq, _p(scale), _stream(stream)),
            "pp_quantize_rows")
+
+
+def pp_dequantize_rows(dtype: int, q, ldq: int, scale, rows: int, d: int, x, ldx: int, stream=None) -> None:
+    """The values that codes q [rows, d] with scale [rows] stand for, into x [rows, d]."""
+    _check(lib().pp_dequantize_rows(dtype, _p(q), ldq, _p(scale), rows, d, _p(x), ldx, _stream(stream)),
+           "pp_dequantize_rows")
 
 
 def pp_rmsnorm_quant(dtype: int, x, add, gain, rows: int, d: int, eps: float, q, scale, stream=None) -> None:

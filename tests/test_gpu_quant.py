@@ -42,7 +42,7 @@ def check_codes(y, q, scale, rel):
 
 
 ROWS = [(1, 16), (1, 4096), (3, 48), (5, 688), (65, 1024), (7, 1040), (130, 2064), (33, 5120), (9, 8192), (4, 14336),
-        (3, 20000), (2, 33040)]
+        (3, 20000), (2, 33040), (4100, 256), (2500, 688)]
 
 
 @pytest.mark.parametrize("rows,d", ROWS)
@@ -98,6 +98,26 @@ def test_quantize_rows_special(dtype, d):
         else:
             assert np.all(np.abs(k[i] - np.clip(y[i] / s[i], -127, 127)) <= 0.5 + 127.1 * 2 * U)
     assert k[5, :4].tolist() == [127, 0, 2, -2]
+
+
+@pytest.mark.parametrize("rows,d", ROWS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_dequantize_rows(rows, d, dtype):
+    """One float32 product, rounded once more to bf16: equal to the same in numpy and torch."""
+    code, t = DT[dtype]
+    g = torch.Generator().manual_seed(rows * 100000 + d + 2)
+    q = torch.randint(-128, 128, (rows, d + 48), generator=g, dtype=torch.int8)
+    scale = torch.exp(20 * torch.randn(rows, generator=g))
+    scale[-1] = float("nan")
+    if rows > 2:
+        scale[0], scale[1] = 0.0, 1e-45
+    x0 = torch.full((rows + 1, d + 16), 9.0).to(t)
+    x = x0.cuda()
+    pp.pp_dequantize_rows(code, q.cuda(), d + 48, scale.cuda(), rows, d, x, d + 16)
+    got = x.cpu()
+    want = (q[:, :d].float() * scale[:, None]).to(t)
+    assert torch.equal(got[:rows - 1, :d], want[:-1]) and bool(got[rows - 1, :d].isnan().all())
+    assert torch.equal(got[rows], x0[rows]) and torch.equal(got[:, d:], x0[:, d:])
 
 
 def rel_norm(d):

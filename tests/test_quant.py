@@ -24,6 +24,9 @@ def _rows(**kw):
 def test_quantize_rows_checks(want, kw):
     assert _rows(**kw) == want
     assert (want == OK) == (pp.pp_last_error() == "")
+    a = {**dict(dtype=BF, x=0x1000, ldx=256, rows=4, d=256, q=0x2000, ldq=256, scale=0x3004), **kw}
+    assert pp.lib().pp_dequantize_rows(a["dtype"], a["q"], a["ldq"], a["scale"], a["rows"], a["d"], a["x"], a["ldx"],
+                                       None) == want
 
 
 def _norm(**kw):
