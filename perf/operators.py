@@ -180,13 +180,15 @@ def _run_own(s):
     r, d = s["rows"], s["d"]
     if s["op"] == "quantize":
         pp.pp_quantize_rows(dt, s["x"], d, r, d, s["q"], d, s["scale"])
-        return {"values": _values(s)}
+        return {"values": _values(pp, s)}
     pp.pp_rmsnorm_quant(dt, s["x"], s["add"], s["gain"], r, d, EPS, s["q"], s["scale"])
-    return {"x": s["x"], "values": _values(s)}
+    return {"x": s["x"], "values": _values(pp, s)}
 
 
-def _values(s):
-    return torch.mul(s["q"], s["scale"][:, None], out=s["values"])
+def _values(pp, s):
+    r, d = s["rows"], s["d"]
+    pp.pp_dequantize_rows(pp.PP_BF16, s["q"], d, s["scale"], r, d, s["values"], d)
+    return s["values"]
 
 
 # ----------------------------------------------------------------------------- in 64 bits
