@@ -303,7 +303,7 @@ pp_status pp_final_norm_unpack(const float* x, const float* gain, int32_t d, flo
  * projections are pp_rmsnorm_quant or pp_quantize_rows followed by pp_gemm_quant; weights take
  * pp_quantize_rows once, when they are loaded.  Same conventions as the single steps.
  *
- * The code of a row y of d values: scale = max|y| / 127 (float32, correctly rounded division),
+ * The code of a row y of d values: scale = max|y| * (1/127) (the float32 product with the float32 1/127),
  * code = y / scale (the float32 quotient) rounded to the nearest integer, ties to even.  A row of zeros, or one so small that the scale rounds to 0, gets scale 0 and codes 0.  A
  * row holding a NaN or an infinity gets scale NaN and codes 0, so that what is computed from it is
  * NaN.

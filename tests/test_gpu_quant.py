@@ -29,11 +29,11 @@ def h64(t):
 # ----------------------------------------------------------------------------- rows in 8 bits
 def check_codes(y, q, scale, rel):
     """q, scale against the float64 rows y, which the kernel saw with relative error rel.
-    scale = max / 127 with one rounding.  What is rounded to an integer is y / scale, of at most 127
+    scale = max * (1 / 127) with a rounding in each.  What is rounded to an integer is y / scale, of at most 127
     and off by 2 rel (once in y, once in the scale) and two more roundings; a code by half a step
-    more."""
+    more.  (scale is the one the kernel wrote.)"""
     top = np.abs(y).max(axis=1)
-    assert np.all(np.abs(scale - top / 127) <= (rel + 1.01 * U) * top / 127 + 2.0 ** -149)
+    assert np.all(np.abs(scale - top / 127) <= (rel + 2.01 * U) * top / 127 + 2.0 ** -149)
     assert np.abs(q).max(initial=0) <= 127
     live = scale > 0
     assert np.all(q[~live] == 0)
@@ -56,7 +56,7 @@ def test_quantize_rows(rows, d, dtype):
     pp.pp_quantize_rows(code, x, d + 32, rows, d, q, d + 16, scale)
     y, s = h64(x[:, :d]), h64(scale)
     check_codes(y, h64(q)[:rows, :d], s[:rows], 0.0)
-    assert np.array_equal(s[:rows], (np.abs(y).max(1).astype(np.float32) / np.float32(127)).astype(np.float64))
+    assert np.array_equal(s[:rows], (np.abs(y).max(1).astype(np.float32) * (np.float32(1) / np.float32(127))).astype(np.float64))
     with np.errstate(invalid="ignore"):                        # the float32 quotient, ties to even
         want = np.rint(y.astype(np.float32) / s[:rows, None].astype(np.float32))
     assert np.array_equal(h64(q)[:rows, :d], want)
@@ -90,7 +90,7 @@ def test_quantize_rows_special(dtype, d):
     bad = [6, 7, 8]
     assert np.isnan(s[bad]).all() and (k[bad] == 0).all()
     good = [i for i in range(12) if i not in bad]
-    want = (np.abs(y[good]).max(1).astype(np.float32) / np.float32(127)).astype(np.float64)
+    want = (np.abs(y[good]).max(1).astype(np.float32) * (np.float32(1) / np.float32(127))).astype(np.float64)
     assert np.array_equal(s[good], want)
     for i in good:
         if s[i] == 0:
