@@ -350,7 +350,7 @@ constexpr float kTileAlone[kQuantTiles] = {0.23f, 0.27f, 0.38f, 0.52f, 0.91f};
 constexpr float kTileStep[kQuantTiles] = {0.18f, 0.25f, 0.36f, 0.62f, 1.06f};
 constexpr float kTileEpilogue[kQuantTiles] = {0.6f, 1.1f, 1.5f, 2.6f, 3.5f};
 // a second launch, and its sums written and read
-constexpr float kFinish = 3.3f, kFinishBytes = 2.5e6f;
+constexpr float kFinish = 5.0f, kFinishBytes = 2.5e6f;
 
 // n_mt < 0: every row of M; else the entries of a row-tile list.
 Choice choose(int M, int N, int K, int n_mt) {

@@ -295,6 +295,75 @@ def test_gemm_quant_plan_row_tiles(epi, N, K):
     check_gemm(h64(got[covered]), product(a[covered], sa[covered], b, sb), epi, h64(c0[covered]), t == torch.bfloat16)
 
 
+@pytest.mark.parametrize("M,N,K", [(66000, 33024, 128), (66000, 256, 33024), (256, 66016, 33024), (20, 66016, 33024)])
+def test_gemm_quant_offsets_past_32_bits(M, N, K):
+    """Operands and outputs of more than 2^31 elements: rows and columns at both ends."""
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    a = torch.randint(-127, 128, (M, K), generator=g, dtype=torch.int8, device="cuda")
+    b = torch.randint(-127, 128, (N, K), generator=g, dtype=torch.int8, device="cuda")
+    sa, sb = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda") / K
+    c = torch.zeros((M, N), dtype=torch.bfloat16, device="cuda")
+    gpu_gemm(pp.PP_EPI_STORE, pp.PP_BF16, a, sa, b, sb, c, M, N, K)
+    m = torch.tensor([0, 1, M // 2, M - 2, M - 1], device="cuda")
+    n = torch.cat([torch.arange(0, 40), torch.arange(N // 2, N // 2 + 24), torch.arange(N - 40, N)]).cuda()
+    check_gemm(h64(c[m][:, n]), product(a[m].cpu(), sa[m].cpu(), b[n].cpu(), sb[n].cpu()), pp.PP_EPI_STORE, None, True)
+
+
+def test_rows_offsets_past_32_bits():
+    rows, d = 140000, 16384
+    x = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda")
+    x.zero_()
+    ends = torch.tensor([0, 1, rows // 2, rows - 2, rows - 1], device="cuda")
+    x[ends] = torch.randn((5, d), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda").bfloat16()
+    q, scale = torch.empty((rows, d), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    pp.pp_quantize_rows(pp.PP_BF16, x, d, rows, d, q, d, scale)
+    check_codes(h64(x[ends]), h64(q[ends]), h64(scale[ends]), 0.0)
+    x2 = torch.empty_like(x)
+    pp.pp_dequantize_rows(pp.PP_BF16, q, d, scale, rows, d, x2, d)
+    assert torch.equal(x2[ends], (q[ends].float() * scale[ends][:, None]).bfloat16())
+    assert int((scale != 0).sum()) == 5
+
+
+def test_rows_more_than_a_launch_dimension_holds():
+    """17 million rows of 16 values: more than 2^32 threads in one dimension, were each row a workgroup."""
+    rows, d = 17_000_003, 16
+    x = (torch.arange(rows, device="cuda") % 1000).float()[:, None].repeat(1, d)
+    q, scale = torch.empty((rows, d), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    pp.pp_quantize_rows(pp.PP_F32, x, d, rows, d, q, d, scale)
+    assert torch.equal(scale, x[:, 0] * (torch.ones((), device="cuda") / 127))
+    assert torch.equal(q, ((x > 0) * 127).to(torch.int8))
+    pp.pp_rmsnorm_quant(pp.PP_F32, x, None, torch.ones(d, device="cuda"), rows, d, 0.5, q, scale)
+    assert torch.equal(q, ((x > 0) * 127).to(torch.int8))
+
+
+@pytest.mark.parametrize("M,N,K", [(7, 512, 272), (100, 512, 272), (1309, 2048, 688)])
+def test_gemm_quant_scales_at_any_float(M, N, K):
+    g, a, sa, b, sb = gemm_case(M, N, K, 5)
+    sa1, sb1 = torch.cat([torch.zeros(1), sa]).cuda()[1:], torch.cat([torch.zeros(3), sb]).cuda()[3:]
+    c = torch.empty(M, N, device="cuda")
+    gpu_gemm(pp.PP_EPI_STORE, pp.PP_F32, a.cuda(), sa1, b.cuda(), sb1, c, M, N, K)
+    check_gemm(h64(c), product(a, sa, b, sb), pp.PP_EPI_STORE, None, False)
+
+
+def test_gemm_quant_on_two_streams_at_once():
+    """Calls that split K (a workspace each) and calls that do not, on two streams, each on its own buffers."""
+    M, N, K = 64, 4096, 14336
+    assert pp.pp_gemm_quant_workspace_size(M, N, K) > 0
+    g, a, sa, b, sb = gemm_case(M, N, K, 6)
+    a, sa, b, sb = a.cuda(), sa.cuda(), b.cuda(), sb.cuda()
+    want = torch.empty(M, N, device="cuda")
+    gpu_gemm(pp.PP_EPI_STORE, pp.PP_F32, a, sa, b, sb, want, M, N, K)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [torch.empty(pp.pp_gemm_quant_workspace_size(M, N, K), dtype=torch.uint8, device="cuda") for _ in streams]
+    out = [[torch.empty(M, N, device="cuda") for _ in range(10)] for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(10):
+        for s, w, o in zip(streams, ws, out):
+            pp.pp_gemm_quant(pp.PP_F32, pp.PP_EPI_STORE, a, K, sa, b, K, sb, o[i], N, M, N, K, w, None, s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, want) for o in out for t in o)
+
+
 # ----------------------------------------------------------------------------- together
 class Layer:
     """One decoder layer in 8 bits over a packed batch, as a caller assembles it from the single steps."""
