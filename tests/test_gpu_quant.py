@@ -174,8 +174,9 @@ def codes(g, *shape):
 
 
 def product(a, sa, b, sb):
-    """(A B^T) scaled, in float64 (the integer sums stay below 2^53)."""
-    return (a.double() @ b.double().T * sa.double()[:, None] * sb.double()).numpy()
+    """(A B^T) scaled, in float64 (the integer sums stay below 2^53, so they are exact in any order)."""
+    a, sa, b, sb = (t.cuda().double() for t in (a, sa, b, sb))
+    return torch.mm(a, b.t()).mul_(sa[:, None]).mul_(sb).cpu().numpy()
 
 
 def swiglu(v):
@@ -204,7 +205,11 @@ def check_gemm(got, v, epi, c0, bf):
 SIZES = [(1, 32, 16), (1, 512, 64), (2, 96, 144), (3, 32, 4096), (7, 4096, 688), (16, 256, 4112), (17, 544, 1024),
          (31, 2048, 5504), (32, 6144, 512), (33, 160, 1040), (48, 1024, 4096), (64, 4096, 2048), (65, 512, 272),
          (100, 2080, 11008), (128, 128, 128), (129, 2048, 1360), (255, 608, 4096), (256, 4096, 64), (344, 2048, 5504),
-         (513, 1056, 2000), (700, 11008, 512), (1309, 2048, 1376), (2926, 6144, 144), (4097, 800, 256)]
+         (513, 1056, 2000), (700, 11008, 512), (1309, 2048, 1376), (2926, 6144, 144), (4097, 800, 256),
+         # the other ways a call may go: two and four column blocks of the few-row kernel and more than a round
+         # of them, 192- and 256-row tiles, whole rounds of 256-row tiles with smaller ones after them
+         (12, 8192, 1040), (14, 12288, 528), (9, 20000, 144), (3000, 4096, 1040), (3500, 4064, 1040), (5000, 4064, 1040),
+         (8500, 4096, 1040), (33000, 544, 144)]
 
 
 def gemm_case(M, N, K, seed=0):
@@ -275,10 +280,12 @@ def test_gemm_quant_extremes(M):
 
 
 @pytest.mark.parametrize("epi", [pp.PP_EPI_STORE, pp.PP_EPI_RESIDUAL, pp.PP_EPI_SWIGLU])
-@pytest.mark.parametrize("N,K", [(4096, 2048), (544, 208)])
-def test_gemm_quant_plan_row_tiles(epi, N, K):
+@pytest.mark.parametrize("lengths,N,K", [([700, 700, 700, 600, 600, 600, 300], 4096, 2048),
+                                         ([700, 700, 700, 600, 600, 600, 300], 544, 208),
+                                         ([700] * 18, 1024, 2064), ([700] * 18, 1280, 2064)])
+def test_gemm_quant_plan_row_tiles(epi, lengths, N, K):
     """With a plan exactly its row tiles are computed; tiles of padding alone keep what they held."""
-    plan = pp.pp_pack([700, 700, 700, 600, 600, 600, 300], 1024)
+    plan = pp.pp_pack(lengths, 1024)
     T = plan.n_slots
     assert plan.n_mtiles < T // 256
     g, a, sa, b, sb = gemm_case(T, N, K)
