@@ -335,8 +335,8 @@ void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
 // Which kernel takes which rows.  An estimate in us, for the CU with the most tiles: a launch and its first
 // loads, then each tile's steps of K and its epilogue; at least the time of the call's bytes at the
 // memory's rate (weights at 4.6 .. 4.8 TB/s) and of what the tiles fetch from L2 together.  The
-// constants are fitted to timings of 136 sizes (1 to 12,000 rows, N 256 to 28,800, K 256 to 14,400) on
-// every kernel; over those sizes the choice costs 2.6% of the best kernel's time on average.
+// constants are fitted to timings of 236 sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400) on
+// every kernel; over those sizes the choice costs 2% of the best kernel's time on average.
 struct Choice {
     enum Kind { kFew, kTile, kRows192, kRows256 } kind;
     int tile, splits;   // kFew: column blocks in `tile`
@@ -350,7 +350,7 @@ constexpr float kTileAlone[kQuantTiles] = {0.23f, 0.27f, 0.38f, 0.52f, 0.91f};
 constexpr float kTileStep[kQuantTiles] = {0.18f, 0.25f, 0.36f, 0.62f, 1.06f};
 constexpr float kTileEpilogue[kQuantTiles] = {0.6f, 1.1f, 1.5f, 2.6f, 3.5f};
 // a second launch, and its sums written and read
-constexpr float kFinish = 5.0f, kFinishBytes = 2.5e6f;
+constexpr float kFinish = 4.0f, kFinishShare = 0.4f, kFinishBytes = 2.5e6f;
 
 // n_mt < 0: every row of M; else the entries of a row-tile list.
 Choice choose(int M, int N, int K, int n_mt) {
@@ -382,7 +382,7 @@ Choice choose(int M, int N, int K, int n_mt) {
         const float fetched = float(tiles) * (kQuantTileRows[t] + kQuantTileCols[t]) * K;
         const float work = per_cu * kTileEpilogue[t] + ceil_div(nk, splits) * (per_cu == 1 ? kTileAlone[t] : per_cu * kTileStep[t]);
         const float mem = ((float(m) + N) * K + 4.f * m * N) / kMemory + fetched / kFabric;
-        return kStart + std::max(work, mem) + (splits > 1 ? kFinish + 4.f * splits * m * N / kFinishBytes : 0.f);
+        return kStart + std::max(work, mem) + (splits > 1 ? kFinish + splits * (kFinishShare + 4.f * m * N / kFinishBytes) : 0.f);
     };
     for (int t = 0; t < kQuantTiles; ++t) {
         consider(tile_time(t, rows, 1), Choice{Choice::kTile, t, 1, 0});
