@@ -11,11 +11,13 @@
 // What bounds it is what a CU receives.  A direct-to-LDS load of 1 KB holds its wavefront's next one back
 // for 140 cycles (17 GB/s a wavefront), so a CU wants 8 wavefronts at work: one workgroup of 8 where
 // the ring takes the LDS, or several of 4 (64 rows, N 4096, K 8192 on 128 x 128 tiles: 43 us with 4
-// wavefronts, 37 with 8).  Lines that another CU of the XCD wants too come at up to 98 GB/s, the
+// wavefronts, 37 with 8).  In the 32 x 64, 64 x 64 and 128 x 128 tiles two wavefronts share a
+// sub-tile, each with half of every step's K, so that they read a third less from LDS (35 us; 64 x 64
+// tiles 19.8 to 17.8); on 64 x 128 and 128 x 256 tiles that gave nothing or lost.  Lines that another CU of the XCD wants too come at up to 98 GB/s, the
 // others at 70.  Deeper rings and other orders of K are no faster.
-// Measured (us; 256 x 256 tiles, the tile chosen): 344 rows, N 2048, K 5504: 70, 15.2 (64 x 64); 1309 rows:
-// 72, 30.0 (128 x 128); 200 rows, N 4096, K 4096: 51, 12.8 (64 x 64); 64 rows, N 4096, K 14336: 158, 19.8
-// (32 x 64 in shares of K); 48 rows, N 28672, K 4096: 53, 29.0, 4.1 TB/s (64 x 64).
+// Measured (us; 256 x 256 tiles, the tile chosen): 344 rows, N 2048, K 5504: 70, 14.2 (64 x 64); 1309 rows:
+// 72, 29.0 (128 x 128); 100 rows, N 4096, K 4096: 51, 10.9 (32 x 64); 64 rows, N 4096, K 14336: 158, 19.8
+// (32 x 64 in shares of K); 48 rows, N 28672, K 4096: 53, 29.5, 4.0 TB/s (64 x 128).
 #include <algorithm>
 
 #include "gemm_quant.h"
@@ -24,16 +26,20 @@ namespace {
 
 constexpr int ROW_B = kQuantStep;
 
-// WM x WN wavefronts; wavefront (wm, wn) of a tile holds MB x NB blocks of 16 x 16.
-template <int BM_, int BN_, int WM_, int WN_, int NS_>
+// WM x WN x WK wavefronts: wavefront (wm, wn, wk) holds MB x NB blocks of 16 x 16 and, where WK is 2,
+// takes the half wk of every step's K (XB: blocks that each hands over at a time when the halves are
+// added at the end of a tile).
+template <int BM_, int BN_, int WM_, int WN_, int WK_, int NS_, int XB_>
 struct Geom {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_, NW = WM * WN, NT = 64 * NW;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WK = WK_, NS = NS_, XB = XB_;
+    static constexpr int NW = WM * WN * WK, NT = 64 * NW, KS = 2 / WK;   // KS: MFMAs deep in a step, per wavefront
     static constexpr int MB = BM / 16 / WM, NB = BN / 16 / WN;
     static constexpr int A_LD = BM * ROW_B / 1024 / NW, B_LD = BN * ROW_B / 1024 / NW;   // 1 KB loads per wavefront
     static constexpr int STEP_LD = A_LD + B_LD;
     static constexpr int SLOT_B = (BM + BN) * ROW_B;
-    static constexpr int LDS = NS * SLOT_B;
-    static_assert(MB >= 1 && NB >= 2 && NB % 2 == 0, "gate and up blocks of a pair in one wavefront");
+    static constexpr int LDS = NS * SLOT_B + (WK == 2 ? NW * XB * 1024 : 0);
+    static_assert(NB >= 2 && NB % 2 == 0, "gate and up blocks of a pair in one wavefront");
+    static_assert(WK == 1 || (MB % 2 == 0 && MB / 2 * NB % XB == 0), "each of the two keeps half of the rows");
     static_assert(A_LD * NW * 1024 == BM * ROW_B && B_LD * NW * 1024 == BN * ROW_B, "whole loads");
     static_assert(NS >= 3 && LDS <= 160 * 1024 && (NS - 1) * STEP_LD <= 63, "ring");
 };
@@ -44,7 +50,7 @@ struct Geom {
 // contiguous ranges, one per XCD (workgroup id mod 8).
 template <int EPI, typename TO, class G, int WGS>
 __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kernel(ppk::QuantGemm q, int mt_first, int n_mt) {
-    constexpr int BM = G::BM, BN = G::BN, NS = G::NS, MB = G::MB, NB = G::NB;
+    constexpr int BM = G::BM, BN = G::BN, NS = G::NS, MB = G::MB, NB = G::NB, KS = G::KS;
     constexpr int SUB = kQuantListRows / BM, GM = 2048 / BM;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x & 63;
@@ -137,25 +143,26 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
         }
     };
 
-    const int wn = wave % G::WN, wm = wave / G::WN;
-    int a_lds[2], b_lds[2];
-    bool past[2];   // this lane's 16 values of the last step's half lie past K
+    const int wn = wave % G::WN, wm = wave / G::WN % G::WM, wk = wave / (G::WN * G::WM);
+    int a_lds[KS], b_lds[KS];
+    bool past[KS];   // this lane's 16 values of the last step's half lie past K
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int h = 0; h < KS; ++h) {
+        const int ks = G::WK == 2 ? wk : h;
         const int phys = ((4 * ks + (lane >> 4)) ^ quant_swz(lane & 15)) * 16;
-        a_lds[ks] = (wm * 16 * MB + (lane & 15)) * ROW_B + phys;
-        b_lds[ks] = (BM + wn * 16 * NB + (lane & 15)) * ROW_B + phys;
-        past[ks] = tail && 64 * ks + 16 * (lane >> 4) >= tail;
+        a_lds[h] = (wm * 16 * MB + (lane & 15)) * ROW_B + phys;
+        b_lds[h] = (BM + wn * 16 * NB + (lane & 15)) * ROW_B + phys;
+        past[h] = tail && 64 * ks + 16 * (lane >> 4) >= tail;
     }
-    struct Frags { i32x4 w[2][NB], a[2][MB]; };   // a whole step's
+    struct Frags { i32x4 w[KS][NB], a[KS][MB]; };   // a whole step's
     auto read_all = [&](int slot, Frags& f) {
         const char* base = smem + slot * G::SLOT_B;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int h = 0; h < KS; ++h) {
 #pragma unroll
-            for (int i = 0; i < NB; ++i) f.w[ks][i] = *reinterpret_cast<const i32x4*>(base + b_lds[ks] + i * 16 * ROW_B);
+            for (int i = 0; i < NB; ++i) f.w[h][i] = *reinterpret_cast<const i32x4*>(base + b_lds[h] + i * 16 * ROW_B);
 #pragma unroll
-            for (int j = 0; j < MB; ++j) f.a[ks][j] = *reinterpret_cast<const i32x4*>(base + a_lds[ks] + j * 16 * ROW_B);
+            for (int j = 0; j < MB; ++j) f.a[h][j] = *reinterpret_cast<const i32x4*>(base + a_lds[h] + j * 16 * ROW_B);
         }
     };
     i32x4 acc[NB][MB];
@@ -174,16 +181,16 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
         advance_cursor();
         if (cut) {
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
+            for (int h = 0; h < KS; ++h)
 #pragma unroll
-                for (int j = 0; j < MB; ++j) cur.a[ks][j] = past[ks] ? i32x4{} : cur.a[ks][j];
+                for (int j = 0; j < MB; ++j) cur.a[h][j] = past[h] ? i32x4{} : cur.a[h][j];
         }
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+        for (int h = 0; h < KS; ++h)
 #pragma unroll
             for (int i = 0; i < NB; ++i)
 #pragma unroll
-                for (int j = 0; j < MB; ++j) acc[i][j] = quant_mfma(cur.w[ks][i], cur.a[ks][j], acc[i][j]);
+                for (int j = 0; j < MB; ++j) acc[i][j] = quant_mfma(cur.w[h][i], cur.a[h][j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
     };
 
@@ -220,18 +227,11 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
         tile_m0n0(c_local, m0, n0);
         // block (i, j): row m0 + .. + l % 16 and columns n .. n + 3 of 16-column block i
         const int n_base = n0 + wn * 16 * NB + 4 * (lane >> 4);
-#pragma unroll
-        for (int j = 0; j < MB; ++j) {
+        auto finish_row = [&](int j, const i32x4 (&a)[NB]) {
             const int m = m0 + wm * 16 * MB + 16 * j + (lane & 15);
             float as = 0.f;
             if constexpr (EPI != ppk::kPartial) as = q.a_scale[min(m, q.M - 1)];
-            i32x4 a[NB];
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-                if constexpr (NB * MB >= 16) asm volatile("" : "+a"(acc[i][j]) : : "memory");
-                a[i] = acc[i][j];
-            }
-            if (m >= q.M) continue;
+            if (m >= q.M) return;
 #pragma unroll
             for (int i = 0; i < NB; i += EPI == ppk::kSwiGLU ? 2 : 1) {
                 if (n_base + 16 * i >= q.N) continue;
@@ -239,6 +239,43 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
                     *reinterpret_cast<i32x4*>(q.part + (int64_t(blockIdx.y) * q.M + m) * q.N + n_base + 16 * i) = a[i];
                 else quant_finish4<EPI, TO>(q, m, n_base + 16 * i, as, a[i], a[EPI == ppk::kSwiGLU ? i + 1 : i]);
             }
+        };
+        if constexpr (G::WK == 1) {
+#pragma unroll
+            for (int j = 0; j < MB; ++j) {
+                i32x4 a[NB];
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    if constexpr (NB * MB >= 16) asm volatile("" : "+a"(acc[i][j]) : : "memory");
+                    a[i] = acc[i][j];
+                }
+                finish_row(j, a);
+            }
+        } else {
+            // the two halves of K: wavefront wk keeps the block rows 2 t + wk and hands over the others,
+            // XB blocks at a time through LDS of their own (the ring is full of the next tile)
+            i32x4* mine = reinterpret_cast<i32x4*>(smem + NS * G::SLOT_B + wave * G::XB * 1024) + lane;
+            const i32x4* other = reinterpret_cast<const i32x4*>(smem + NS * G::SLOT_B + (wave ^ (G::NW / 2)) * G::XB * 1024) + lane;
+            i32x4 sum[MB / 2][NB];
+#pragma unroll
+            for (int r = 0; r < MB / 2 * NB; r += G::XB) {
+                if (r > 0) {
+                    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): what was handed over has been read
+                    quant_barrier();
+                }
+#pragma unroll
+                for (int x = 0; x < G::XB; ++x) {
+                    const int t = (r + x) / NB, i = (r + x) % NB;
+                    mine[x * 64] = wk ? acc[i][2 * t] : acc[i][2 * t + 1];
+                    sum[t][i] = wk ? acc[i][2 * t + 1] : acc[i][2 * t];
+                }
+                __builtin_amdgcn_s_waitcnt(0xc07f);
+                quant_barrier();
+#pragma unroll
+                for (int x = 0; x < G::XB; ++x) sum[(r + x) / NB][(r + x) % NB] += other[x * 64];
+            }
+#pragma unroll
+            for (int t = 0; t < MB / 2; ++t) finish_row(2 * t + wk, sum[t]);
         }
         // waited for once, here: otherwise the compiler waits for the epilogue's loads inside the next K
         // loop, in every step, where that empties the ring
@@ -282,11 +319,11 @@ void launch(const ppk::QuantGemm& g, int mt_first, int n_mt, int splits, hipStre
 template <int EPI, typename TO>
 void launch_tile(int tile, const ppk::QuantGemm& g, int mt_first, int n_mt, int splits, hipStream_t s) {
     switch (tile) {
-        case 0: return launch<EPI, TO, Geom<32, 64, 2, 2, 4>, 3>(g, mt_first, n_mt, splits, s);
-        case 1: return launch<EPI, TO, Geom<64, 64, 4, 2, 5>, 2>(g, mt_first, n_mt, splits, s);
-        case 2: return launch<EPI, TO, Geom<64, 128, 2, 4, 3>, 2>(g, mt_first, n_mt, splits, s);
-        case 3: return launch<EPI, TO, Geom<128, 128, 2, 4, 5>, 1>(g, mt_first, n_mt, splits, s);
-        default: return launch<EPI, TO, Geom<128, 256, 2, 4, 3>, 1>(g, mt_first, n_mt, splits, s);
+        case 0: return launch<EPI, TO, Geom<32, 64, 1, 2, 2, 4, 1>, 3>(g, mt_first, n_mt, splits, s);
+        case 1: return launch<EPI, TO, Geom<64, 64, 2, 2, 2, 4, 2>, 2>(g, mt_first, n_mt, splits, s);
+        case 2: return launch<EPI, TO, Geom<64, 128, 2, 4, 1, 3, 0>, 2>(g, mt_first, n_mt, splits, s);
+        case 3: return launch<EPI, TO, Geom<128, 128, 2, 2, 2, 4, 4>, 1>(g, mt_first, n_mt, splits, s);
+        default: return launch<EPI, TO, Geom<128, 256, 2, 4, 1, 3, 0>, 1>(g, mt_first, n_mt, splits, s);
     }
 }
 
