@@ -335,8 +335,8 @@ void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
 // Which kernel takes which rows.  An estimate in us, for the CU with the most tiles: a launch and its first
 // loads, then each tile's steps of K and its epilogue; at least the time of the call's bytes at the
 // memory's rate (weights at 4.6 .. 4.8 TB/s) and of what the tiles fetch from L2 together.  The
-// constants are fitted to timings of 236 sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400) on
-// every kernel; over those sizes the choice costs 2% of the best kernel's time on average.
+// constants are fitted to timings of some 240 sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400)
+// on every kernel; over those sizes the choice costs 2% of the best kernel's time on average, 46% at worst.
 struct Choice {
     enum Kind { kFew, kTile, kRows192, kRows256 } kind;
     int tile, splits;   // kFew: column blocks in `tile`
@@ -346,8 +346,8 @@ struct Choice {
 constexpr float kStart = 3.0f, kBigEpilogue = 7.0f, kBigStep = 1.36f, kStep192 = 1.06f;
 constexpr float kWeights = 4.6e6f, kMemory = 4.8e6f, kFabric = 90e6f;   // bytes per us
 // a CU's only tile, and each of several (two or three of the smallest at a time)
-constexpr float kTileAlone[kQuantTiles] = {0.23f, 0.27f, 0.38f, 0.52f, 0.91f};
-constexpr float kTileStep[kQuantTiles] = {0.18f, 0.25f, 0.36f, 0.62f, 1.06f};
+constexpr float kTileAlone[kQuantTiles] = {0.22f, 0.24f, 0.38f, 0.49f, 0.91f};
+constexpr float kTileStep[kQuantTiles] = {0.175f, 0.235f, 0.36f, 0.60f, 1.06f};
 constexpr float kTileEpilogue[kQuantTiles] = {0.6f, 1.1f, 1.5f, 2.6f, 3.5f};
 // a second launch, and its sums written and read
 constexpr float kFinish = 4.0f, kFinishShare = 0.4f, kFinishBytes = 2.5e6f;

@@ -377,12 +377,12 @@ def config_of(shape, n_layers: Optional[int] = None) -> PPConfig:
 
 
 def _stream(stream):
-    """The handle of ``stream`` (default: torch's current stream on the current device).  The raw
-    handle of the current stream costs 0.3 us; torch.cuda.current_stream() builds an object, 2.6 us."""
-    if stream is None:
-        torch = _torch()
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-    return stream.cuda_stream
+    """The handle of ``stream`` (default: torch's current stream on the current device).  The current
+    stream's raw handle costs 0.2 us; torch.cuda.current_stream() builds an object, 2.6 us."""
+    if stream is not None:
+        return stream.cuda_stream
+    c = _torch()._C
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 def _p(t):
