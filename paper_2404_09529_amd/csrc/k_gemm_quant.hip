@@ -20,29 +20,29 @@
 
 namespace {
 
-constexpr int BM = 256, BN = 256, NT = 256;
+constexpr int BM = 256, BN = 256, NT = 256;   // of the largest tile
 constexpr int ROW_B = kQuantStep, SLOT_B = BM * ROW_B, NSLOT = 5, LDS_BYTES = NSLOT * SLOT_B;
-constexpr int LOADS = SLOT_B / 1024 / 4;   // 1 KB loads per wavefront per operand tile
 
-// The epilogue of one wavefront's 16 MB rows x 128 columns, 16 rows at a time (float32 rows in halves of
-// 64 columns, which bounds the registers): lanes put their runs of four results into the staging area
+// The epilogue of one wavefront's 16 MB rows x 16 NB columns, 16 rows at a time (float32 rows in halves,
+// which bounds the registers): lanes put their runs of four results into the staging area
 // (LDS, this wavefront's own) and take back 16-byte chunks of whole rows, so that memory is read and
 // written in whole lines.  Block (i, j): row mb + 16 j + l % 16, columns nb0 + 16 i + 4 (l / 16) + 0..3.
-// Staging row r's chunk c sits at c ^ (r % chunks).
-template <int EPI, typename TO, int MB>
-__device__ __forceinline__ void epilogue(i32x4 (&acc)[8][MB], const ppk::QuantGemm& q, int mb, int nb0, int lane, char* stg) {
+// Staging row r's chunk c sits at c ^ (r % chunks); a row of 6 blocks is staged in the room of 8.
+template <int EPI, typename TO, int MB, int NB>
+__device__ __forceinline__ void epilogue(i32x4 (&acc)[NB][MB], const ppk::QuantGemm& q, int mb, int nb0, int lane, char* stg) {
     constexpr bool PAIRS = EPI == ppk::kSwiGLU;
-    constexpr int HALVES = !PAIRS && sizeof(TO) == 4 ? 2 : 1, IB = 8 / HALVES;   // passes over a block row, blocks of each
-    constexpr int COLS = PAIRS ? 64 : 128 / HALVES;
-    constexpr int RB = COLS * static_cast<int>(sizeof(TO)), CH = RB / 16;   // bytes, chunks of a staged row
+    constexpr int HALVES = !PAIRS && sizeof(TO) == 4 ? 2 : 1, IB = NB / HALVES;   // passes over a block row, blocks of each
+    constexpr int COLS = PAIRS ? 8 * NB : 16 * NB / HALVES;                 // columns of a pass
+    constexpr int RB = (PAIRS ? 64 : 128 / HALVES) * static_cast<int>(sizeof(TO)), CH = RB / 16;   // bytes, chunks of a staged row
     constexpr int RPI = 64 / CH, NI = 16 / RPI;                             // rows per instruction, instructions
     constexpr int PER = 16 / static_cast<int>(sizeof(TO));                  // values of a chunk
     const int lr = lane & 15, g = lane >> 4;
     const int n_out = PAIRS ? q.N / 2 : q.N;
     const int col0 = (PAIRS ? nb0 / 2 : nb0) + lane % CH * PER;
-    f32x4 bs[8];
+    const bool in_row = lane % CH * PER < COLS;   // (chunks past a row of 6 blocks hold nothing)
+    f32x4 bs[NB];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bs[i] = *reinterpret_cast<const f32x4*>(q.b_scale + min(nb0 + 16 * i, q.N - 16) + 4 * g);
+    for (int i = 0; i < NB; ++i) bs[i] = *reinterpret_cast<const f32x4*>(q.b_scale + min(nb0 + 16 * i, q.N - 16) + 4 * g);
     float as[MB];
 #pragma unroll
     for (int j = 0; j < MB; ++j) as[j] = q.a_scale[min(mb + 16 * j + lr, q.M - 1)];
@@ -88,7 +88,7 @@ __device__ __forceinline__ void epilogue(i32x4 (&acc)[8][MB], const ppk::QuantGe
 #pragma unroll
         for (int k = 0; k < NI; ++k) {
             const int m = mb + 16 * j + RPI * k + lane / CH, col = col0 + COLS * (t % HALVES);
-            if (m < q.M && col < n_out) {
+            if (m < q.M && col < n_out && in_row) {
                 u32x4* p = reinterpret_cast<u32x4*>(static_cast<TO*>(q.C) + int64_t(m) * q.ldc + col);
                 if constexpr (EPI == ppk::kResidual) {
 #pragma unroll
@@ -107,10 +107,11 @@ __device__ __forceinline__ void epilogue(i32x4 (&acc)[8][MB], const ppk::QuantGe
     __builtin_amdgcn_s_waitcnt(quant_wait(0));
 }
 
-// MB: 16-row blocks of a wavefront, so 32 MB rows of a tile (8: 256; 6: 192, without a row-tile list).
-template <int EPI, typename TO, int MB>
+// MB, NB: 16-row and 16-column blocks of a wavefront, so tiles of 32 MB x 32 NB (6: 192, rows without a
+// row-tile list).
+template <int EPI, typename TO, int MB, int NB>
 __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int tiles_m, int tiles_n, int balanced) {
-    constexpr int TM = 32 * MB, GM = 64 / MB;   // rows of a tile; M-tiles of a group
+    constexpr int TM = 32 * MB, TN = 32 * NB, GM = 64 / MB;   // of a tile; M-tiles of a group
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
         const int first = group * gm, gsz = min(m_cnt - first, gm);
         const int mt = m_begin + first + within % gsz;
         m0 = q.mtile_m0 ? q.mtile_m0[mt] : mt * TM;
-        n0 = within / gsz * BN;
+        n0 = within / gsz * TN;
     };
     const int nk = (q.K + kQuantStep - 1) / kQuantStep;
     const int tail = q.K % kQuantStep;   // values of the last step, 0: a whole one
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     int chunk_off[2];   // of even and odd loads
 #pragma unroll
     for (int t = 0; t < 2; ++t) chunk_off[t] = 16 * ((lane & 7) ^ quant_swz(8 * t + lrow));
-    int voff_a[MB], voff_b[LOADS];
+    int voff_a[MB], voff_b[NB];
     // load cursor: the step being requested, into slots l_sa (A) and l_sb (B); l_local >= n_local once the
     // stream is exhausted (its loads are then dead: they read nothing, into slots that are not read again)
     int l_local = slot, l_kt = 0, l_sa = 0, l_sb = 1, l_k = 0;   // l_k: first value of the step
@@ -165,13 +166,13 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
         if (l_local < n_local) {
             int m0, n0;
             tile_m0n0(l_local, m0, n0);
-            const int a_rows = min(q.M - m0, TM), b_rows = min(q.N - n0, BN);
+            const int a_rows = min(q.M - m0, TM), b_rows = min(q.N - n0, TN);
             rsrc_a = quant_rsrc(q.A + int64_t(m0) * lda, (a_rows - 1) * lda + q.K);
             rsrc_b = quant_rsrc(q.B + int64_t(n0) * ldb, (b_rows - 1) * ldb + q.K);
 #pragma unroll
             for (int t = 0; t < MB; ++t) voff_a[t] = min(8 * (MB * wave + t) + lrow, a_rows - 1) * lda + chunk_off[t & 1];
 #pragma unroll
-            for (int t = 0; t < LOADS; ++t) voff_b[t] = min(8 * (LOADS * wave + t) + lrow, b_rows - 1) * ldb + chunk_off[t & 1];
+            for (int t = 0; t < NB; ++t) voff_b[t] = min(8 * (NB * wave + t) + lrow, b_rows - 1) * ldb + chunk_off[t & 1];
         } else {
             rsrc_a = rsrc_0;
             rsrc_b = rsrc_0;
@@ -184,8 +185,9 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (lds_void*)dst, 16, voff, l_k, 0, 0);
     };
     auto load_b = [&](int t) {
-        char* dst = smem + l_sb * SLOT_B + (wave * LOADS + t) * 1024;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_void*)dst, 16, voff_b[t], l_k, 0, 0);
+        char* dst = smem + l_sb * SLOT_B + (wave * NB + t) * 1024;
+        const int voff = voff_b[t];
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_void*)dst, 16, voff, l_k, 0, 0);
     };
     // in two parts: scalar arithmetic that issues between MFMAs, and the rare step to another tile
     bool l_wrap = false;
@@ -211,10 +213,10 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     for (int ks = 0; ks < 2; ++ks) {
         const int phys = ((4 * ks + (lane >> 4)) ^ quant_swz(lane & 15)) * 16;
         a_lds[ks] = (wm * 16 * MB + (lane & 15)) * ROW_B + phys;
-        b_lds[ks] = (wn * 128 + (lane & 15)) * ROW_B + phys;
+        b_lds[ks] = (wn * 16 * NB + (lane & 15)) * ROW_B + phys;
         again[ks] = tail && 64 * ks + 16 * (lane >> 4) < kQuantStep - tail;
     }
-    struct Frags { i32x4 w[8], a[MB]; };
+    struct Frags { i32x4 w[NB], a[MB]; };
     auto read_one = [&](int sa, int sb, int ks, int p, Frags& f) {   // w0, a0 .., w1 ..: as the MFMAs need them
         if (p == 0) f.w[0] = *reinterpret_cast<const i32x4*>(smem + sb * SLOT_B + b_lds[ks]);
         else if (p <= MB) f.a[p - 1] = *reinterpret_cast<const i32x4*>(smem + sa * SLOT_B + a_lds[ks] + (p - 1) * 16 * ROW_B);
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
 #pragma unroll
         for (int t = 0; t < MB; ++t) load_a(t);
 #pragma unroll
-        for (int t = 0; t < LOADS; ++t) load_b(t);
+        for (int t = 0; t < NB; ++t) load_b(t);
         advance_cursor();
         advance_tile();
     }
@@ -245,32 +247,32 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     Frags F0, F1;
     int c_sa = 0, c_sb = 1;
 #pragma unroll
-    for (int p = 0; p < 8 + MB; ++p) read_one(c_sa, c_sb, 0, p, F0);
+    for (int p = 0; p < NB + MB; ++p) read_one(c_sa, c_sb, 0, p, F0);
     while (true) {
-        i32x4 acc[8][MB];
+        i32x4 acc[NB][MB];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
             for (int j = 0; j < MB; ++j) acc[i][j] = i32x4{};
         // One sub-step: the MFMAs on `cur`, with the fragment reads of the next one (into `nxt`) and a
-        // load after every eighth MFMA, in a fixed order.  The first sub-step ends at the barrier: its
+        // load per row of blocks, in a fixed order.  The first sub-step ends at the barrier: its
         // reads go among the first three quarters of the MFMAs, so they have landed by then.
         auto substep = [&](const Frags& cur, Frags& nxt, int rsa, int rsb, int rks, bool first) {
 #pragma unroll
-            for (int m = 0; m < 8 * MB; ++m) {
+            for (int m = 0; m < NB * MB; ++m) {
                 const int i = m / MB, j = m % MB;
                 acc[i][j] = quant_mfma(cur.w[i], cur.a[j], acc[i][j]);
                 __builtin_amdgcn_sched_barrier(0);
-                const int span = first ? 6 * MB : 8 * MB;
+                const int span = first ? NB * MB * 3 / 4 : NB * MB;
 #pragma unroll
-                for (int p = (m * (8 + MB) + span - 1) / span;
-                     p < ((m + 1) * (8 + MB) + span - 1) / span && p < 8 + MB; ++p)
+                for (int p = (m * (NB + MB) + span - 1) / span;
+                     p < ((m + 1) * (NB + MB) + span - 1) / span && p < NB + MB; ++p)
                     read_one(rsa, rsb, rks, p, nxt);
                 if (first) {
-                    if (m % 8 == 2) load_a(m / 8);
+                    if (m % NB == 2) load_a(m / NB);
                 } else {
                     if (m % MB == 2) load_b(m / MB);
-                    if (m == 7 * MB + 3) advance_cursor();   // the cursor moves to step g+3
+                    if (m == (NB - 1) * MB + 3) advance_cursor();   // the cursor moves to step g+3
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
         int m0, n0;
         tile_m0n0(c_local, m0, n0);
         const int free_slot = c_sb >= 2 ? c_sb - 2 : c_sb + NSLOT - 2;
-        epilogue<EPI, TO, MB>(acc, q, m0 + wm * 16 * MB, n0 + wn * 128, lane, smem + free_slot * SLOT_B + wave * MB * 1024);
+        epilogue<EPI, TO, MB, NB>(acc, q, m0 + wm * 16 * MB, n0 + wn * 16 * NB, lane, smem + free_slot * SLOT_B + wave * MB * 1024);
         c_local += n_slots;
         if (c_local >= n_local) break;
     }
@@ -321,34 +323,36 @@ namespace ppk {
 namespace {
 
 // The first n_mt tiles of 32 MB rows on this kernel.
-template <int EPI, typename TO, int MB>
+template <int EPI, typename TO, int MB, int NB>
 void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
     static std::atomic<uint64_t> done{0};
-    quant_allow_lds(reinterpret_cast<const void*>(&gemm_quant_kernel<EPI, TO, MB>), LDS_BYTES, done);
-    const int tiles_n = ceil_div(g.N, BN), wg_per_xcd = cu_count() / 8;
+    quant_allow_lds(reinterpret_cast<const void*>(&gemm_quant_kernel<EPI, TO, MB, NB>), LDS_BYTES, done);
+    const int tiles_n = ceil_div(g.N, 32 * NB), wg_per_xcd = cu_count() / 8;
     const XcdSplit x = xcd_split(n_mt, tiles_n, wg_per_xcd);
     QuantGemm q = g;
     if (MB == 8 && !g.mtile_m0) q.M = std::min<int64_t>(g.M, int64_t(n_mt) * BM);
-    gemm_quant_kernel<EPI, TO, MB><<<8 * std::min(wg_per_xcd, x.tiles), NT, LDS_BYTES, s>>>(q, n_mt, tiles_n, x.balanced);
+    gemm_quant_kernel<EPI, TO, MB, NB><<<8 * std::min(wg_per_xcd, x.tiles), NT, LDS_BYTES, s>>>(q, n_mt, tiles_n, x.balanced);
 }
 
 // Which kernel takes which rows.  An estimate in us, for the CU with the most tiles: a launch and its first
 // loads, then each tile's steps of K and its epilogue; at least the time of the call's bytes at the
 // memory's rate (weights at 4.6 .. 4.8 TB/s) and of what the tiles fetch from L2 together.  The
-// constants are fitted to timings of some 240 sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400)
+// constants are fitted to timings of some 260 sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400)
 // on every kernel; over those sizes the choice costs 2% of the best kernel's time on average, 46% at worst.
+// The 192-row tiles are for the rounds that 256 x 256 ones leave part empty: 2000 rows, N 4096, K 11008 in
+// 242 of 192 x 192 88 us, in 128 of 256 x 256 113; 2926 rows, N 4096, K 14336 in 256 of 192 x 256 143 and 169 us.
 struct Choice {
-    enum Kind { kFew, kTile, kRows192, kRows256 } kind;
+    enum Kind { kFew, kTile, k192x192, k192x256, k256x256 } kind;
     int tile, splits;   // kFew: column blocks in `tile`
     int big;            // kTile: 256-row tiles that the 256 x 256 kernel takes before it
 };
 
-constexpr float kStart = 3.0f, kBigEpilogue = 7.0f, kBigStep = 1.36f, kStep192 = 1.06f;
+constexpr float kStart = 3.0f, kBigEpilogue = 7.0f, kBigStep = 1.36f, kStep192 = 1.12f, kStepSquare192 = 0.80f;
 constexpr float kWeights = 4.6e6f, kMemory = 4.8e6f, kFabric = 90e6f;   // bytes per us
 // a CU's only tile, and each of several (two or three of the smallest at a time)
-constexpr float kTileAlone[kQuantTiles] = {0.22f, 0.24f, 0.38f, 0.49f, 0.91f};
-constexpr float kTileStep[kQuantTiles] = {0.175f, 0.235f, 0.36f, 0.60f, 1.06f};
-constexpr float kTileEpilogue[kQuantTiles] = {0.6f, 1.1f, 1.5f, 2.6f, 3.5f};
+constexpr float kTileAlone[kQuantTiles] = {0.22f, 0.24f, 0.38f, 0.49f, 1.0f};
+constexpr float kTileStep[kQuantTiles] = {0.175f, 0.235f, 0.38f, 0.65f, 1.06f};
+constexpr float kTileEpilogue[kQuantTiles] = {0.6f, 1.1f, 1.5f, 2.6f, 6.0f};
 // a second launch, and its sums written and read
 constexpr float kFinish = 4.0f, kFinishShare = 0.4f, kFinishBytes = 2.5e6f;
 
@@ -392,13 +396,16 @@ Choice choose(int M, int N, int K, int n_mt) {
             if (s <= nk && tiles * s <= 24 * wg) consider(tile_time(t, M, s), Choice{Choice::kTile, t, s, 0});
     }
     if (rows <= kQuantFewRows || K < kQuantStep) return best;   // (the large tiles need a whole step)
-    auto big_time = [&](int mt, int tile_rows, float step) {
-        const int64_t per_cu = ceil_div(xcd_split(mt, tiles_n, wg).tiles, wg);
+    auto big_time = [&](int mt, int tile_rows, float step, int tile_cols = BN) {
+        const int64_t per_cu = ceil_div(xcd_split(mt, ceil_div(N, tile_cols), wg).tiles, wg);
         const float mem = (float(mt) * tile_rows * K + float(N) * K + 4.f * mt * tile_rows * N) / kMemory;
         return kStart + std::max(per_cu * (nk * step + kBigEpilogue), mem);
     };
-    if (n_mt == ceil_div(M, BM)) consider(big_time(ceil_div(M, 192), 192, kStep192), Choice{Choice::kRows192, 0, 1, 0});
-    consider(big_time(n_mt, BM, kBigStep), Choice{Choice::kRows256, 0, 1, 0});
+    if (n_mt == ceil_div(M, BM)) {   // (a list must name every tile: it counts in 256 rows)
+        consider(big_time(ceil_div(M, 192), 192, kStep192), Choice{Choice::k192x256, 0, 1, 0});
+        consider(big_time(ceil_div(M, 192), 192, kStepSquare192, 192), Choice{Choice::k192x192, 0, 1, 0});
+    }
+    consider(big_time(n_mt, BM, kBigStep), Choice{Choice::k256x256, 0, 1, 0});
     // whole rounds of 256 x 256 tiles and the other rows on small ones; a split has to promise 5%
     const int64_t rounds = int64_t(n_mt) * tiles_n / (8 * wg);
     for (int64_t r = rounds; r > 0 && r >= rounds - 1; --r) {
@@ -416,12 +423,13 @@ void gemm(QuantGemm g, hipStream_t s) {
     const int n_mt = g.mtile_m0 ? g.n_mtiles : ceil_div(g.M, BM);
     const Choice c = choose(g.M, g.N, g.K, g.mtile_m0 ? n_mt : -1);
     if (c.kind == Choice::kFew) return quant_gemm_few(EPI, sizeof(TO) == 4, c.tile, g, s);
-    if (c.kind == Choice::kRows256) return launch<EPI, TO, 8>(g, n_mt, s);
-    if (c.kind == Choice::kRows192) {
+    if (c.kind == Choice::k256x256) return launch<EPI, TO, 8, 8>(g, n_mt, s);
+    if (c.kind == Choice::k192x256 || c.kind == Choice::k192x192) {
         g.mtile_m0 = nullptr;   // (it names every tile)
-        return launch<EPI, TO, 6>(g, ceil_div(g.M, 192), s);
+        return c.kind == Choice::k192x256 ? launch<EPI, TO, 6, 8>(g, ceil_div(g.M, 192), s)
+                                          : launch<EPI, TO, 6, 6>(g, ceil_div(g.M, 192), s);
     }
-    if (c.big > 0) launch<EPI, TO, 8>(g, c.big, s);
+    if (c.big > 0) launch<EPI, TO, 8, 8>(g, c.big, s);
     quant_gemm_tiles(EPI, sizeof(TO) == 4, c.tile, g, c.big, n_mt - c.big, c.splits, s);
 }
 

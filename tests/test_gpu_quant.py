@@ -207,8 +207,9 @@ SIZES = [(1, 32, 16), (1, 512, 64), (2, 96, 144), (3, 32, 4096), (7, 4096, 688),
          (100, 2080, 11008), (128, 128, 128), (129, 2048, 1360), (255, 608, 4096), (256, 4096, 64), (344, 2048, 5504),
          (513, 1056, 2000), (700, 11008, 512), (1309, 2048, 1376), (2926, 6144, 144), (4097, 800, 256),
          # the other ways a call may go: two and four column blocks of the few-row kernel and more than a round
-         # of them, 192- and 256-row tiles, whole rounds of 256-row tiles with smaller ones after them
-         (12, 8192, 1040), (14, 12288, 528), (9, 20000, 144), (3000, 4096, 1040), (3500, 4064, 1040), (5000, 4064, 1040),
+         # of them, tiles of 64 x 128 and 128 x 256, 192 x 192 (700 rows above), 192 x 256 and 256 x 256, whole
+         # rounds of 256-row tiles with smaller ones after them
+         (2800, 1600, 656), (640, 12800, 400), (2500, 2080, 1040), (12, 8192, 1040), (14, 12288, 528), (9, 20000, 144), (3000, 4096, 1040), (3500, 4064, 1040), (5000, 4064, 1040),
          (8500, 4096, 1040), (33000, 544, 144)]
 
 
