@@ -304,13 +304,14 @@ pp_status pp_final_norm_unpack(const float* x, const float* gain, int32_t d, flo
  * pp_quantize_rows once, when they are loaded.  Same conventions as the single steps.
  *
  * The code of a row y of d values: scale = max|y| * (1/127) (the float32 product with the float32 1/127),
- * code = y / scale (the float32 quotient) rounded to the nearest integer, ties to even.  A row of zeros, or one so small that the scale rounds to 0, gets scale 0 and codes 0.  A
- * row holding a NaN or an infinity gets scale NaN and codes 0, so that what is computed from it is
- * NaN.
+ * code = y / scale (the float32 quotient) rounded to the nearest integer, ties to even.  A row of zeros, or
+ * one so small that the scale rounds to 0, gets scale 0 and codes 0.  A row holding a NaN or an infinity
+ * gets scale NaN and codes 0, so that what is computed from it is NaN.
  * ---------------------------------------------------------------------------------------- */
 
 /* q[r] and scale[r] of x[r] for every row: x [rows, d] in dtype (row stride ldx elements), q [rows, d]
- * 8-bit codes (row stride ldq bytes; bytes between d and ldq are left alone), scale [rows] float32.
+ * 8-bit codes (row stride ldq bytes; bytes between d and ldq are left alone; not overlapping x), scale
+ * [rows] float32.
  * d % 16 == 0; ldx and ldq multiples of 16, x and q 16-byte aligned.
  * Errors: PP_ERR_INVALID_ARG (NULL, negative count, a stride below d), PP_ERR_UNSUPPORTED (d, ldx, ldq or
  *         an address that is no multiple of 16), PP_ERR_HIP. */

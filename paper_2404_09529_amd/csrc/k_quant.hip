@@ -3,9 +3,11 @@
 //
 // scale = max|y| * (1 / 127), code = round(y / scale).  Both need the whole row before the first code
 // is written, so a row stays in registers between its one read and its one write: memory bounds
-// both kernels (27,721 x 4096: quantize_rows of bf16 59 us, 5.8 TB/s; rmsnorm_quant with a bf16 residual 219 us,
-// 5.7 TB/s).  A row of up to four 16-byte chunks per lane is one wavefront's, a longer one a workgroup's: 20,000 rows
-// of 688 bf16 values 9.3 us and 19.4, of 4096 46.2 and 43.5.
+// both kernels (27,721 x 4096: quantize_rows of bf16 59 us, 5.8 TB/s; rmsnorm_quant with a bf16 residual 217 us,
+// 5.7 TB/s; and dequantize_rows to bf16 57 to 70 us, 4.9 to 6.0 TB/s).  A row of up to four 16-byte chunks per lane is one
+// wavefront's, a longer one a workgroup's: 20,000 rows of 688 bf16 values 9.3 us and 19.4, of 4096 46.2 and
+// 43.5.  quantize_rows has workgroups of 16 wavefronts too, for the rows of a wide layer's second weight (up to
+// 65,536 float32 or 131,072 bf16 values): 4096 x 28,672 float32 106 us, 5.5 TB/s, instead of 156 with two reads.
 #include "device.h"
 #include "kernels.h"
 #include "prepack.h"
@@ -61,6 +63,10 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
     return v;
 }
 
+// Threads of a workgroup whose rows have W wavefronts each: kThreads, or those of one row.
+template <int W>
+constexpr int kBlock = kWave * W > kThreads ? kWave * W : kThreads;
+
 // Over the W wavefronts of a row (W = 1: each wavefront of the workgroup has a row of its own).
 template <int W>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
@@ -115,10 +121,16 @@ struct Add4<bf16> {
     }
 };
 
+__device__ __forceinline__ f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
+__device__ __forceinline__ f32x4 load4(const bf16* p) {
+    const bf16x4 v = *reinterpret_cast<const bf16x4*>(p);
+    return f32x4{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]), static_cast<float>(v[3])};
+}
+
 // Row of this thread's W wavefronts, uniform in each of them.
 template <int W>
 __device__ __forceinline__ int64_t my_row() {
-    constexpr int per_block = kThreads / kWave / W;
+    constexpr int per_block = kBlock<W> / kWave / W;
     return (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * per_block + __builtin_amdgcn_readfirstlane(threadIdx.x / (kWave * W));
 }
 
@@ -182,8 +194,9 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quant_kernel(float* __restri
     if (t == 0) scale[row] = rc.scale;
 }
 
-// Rows too long for the registers: one workgroup each, read three times (a thread reads again what
-// it wrote itself).
+// Rows too long for the registers: one workgroup each, a thread's four values at a time, read three times
+// (a thread reads again what it wrote itself; 4096 rows of 28,672 values, bf16 residual: 335 us,
+// 3.9 TB/s).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rmsnorm_quant_long_kernel(float* __restrict__ x, const T* __restrict__ add,
                                                                       const float* __restrict__ g, int rows, int d,
@@ -196,33 +209,42 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quant_long_kernel(float* __r
     float* xr = x + row * d;
     const T* ar = add ? add + row * d : nullptr;
     float ss = 0.f;
-    for (int64_t e = threadIdx.x; e < d; e += kThreads) {
-        float v = xr[e];
+#pragma unroll 4
+    for (int64_t e = 4 * threadIdx.x; e < d; e += 4 * kThreads) {
+        f32x4 v = load4(xr + e);
         if (ar) {
-            v += static_cast<float>(ar[e]);
-            xr[e] = v;
+            v += load4(ar + e);
+            *reinterpret_cast<f32x4*>(xr + e) = v;
         }
-        ss += v * v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ss += v[i] * v[i];
     }
     ss = row_sum<kThreads / kWave>(ss, sums);
     const float r = rsqrtf(ss / static_cast<float>(d) + eps);
     uint32_t top = 0;
-    for (int64_t e = threadIdx.x; e < d; e += kThreads) top = max(top, magnitude(xr[e] * r * g[e]));
+#pragma unroll 4
+    for (int64_t e = 4 * threadIdx.x; e < d; e += 4 * kThreads) {
+        const f32x4 v = load4(xr + e) * r * load4(g + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, magnitude(v[i]));
+    }
     top = row_umax<kThreads / kWave>(top, tops);
     const RowCode rc = row_code(top);
-    for (int64_t e = threadIdx.x; e < d; e += kThreads) {
-        const float v[4] = {xr[e] * r * g[e], 0.f, 0.f, 0.f};
-        q[row * d + e] = static_cast<int8_t>(codes4(v, rc) & 0xffu);
+#pragma unroll 4
+    for (int64_t e = 4 * threadIdx.x; e < d; e += 4 * kThreads) {
+        const f32x4 y = load4(xr + e) * r * load4(g + e);
+        const float v[4] = {y[0], y[1], y[2], y[3]};
+        *reinterpret_cast<uint32_t*>(q + row * d + e) = codes4(v, rc);
     }
     if (threadIdx.x == 0) scale[row] = rc.scale;
 }
 
 // ------------------------------------------------------------------------------- rows as they are
 template <typename T, int W, int NC>
-__global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict__ x, int64_t ldx, int rows, int d,
+__global__ __launch_bounds__(kBlock<W>) void quantize_kernel(const T* __restrict__ x, int64_t ldx, int rows, int d,
                                                             int8_t* __restrict__ q, int64_t ldq,
                                                             float* __restrict__ scale) {
-    __shared__ uint32_t tops[kThreads / kWave];
+    __shared__ uint32_t tops[kBlock<W> / kWave];
     const int64_t row = my_row<W>();
     if (row >= rows) return;
     const int t = threadIdx.x % (kWave * W);
@@ -279,12 +301,19 @@ __global__ __launch_bounds__(kThreads) void quantize_long_kernel(const T* __rest
     if (row >= rows) return;
     const T* xr = x + row * ldx;
     uint32_t top = 0;
-    for (int64_t e = threadIdx.x; e < d; e += kThreads) top = max(top, magnitude(static_cast<float>(xr[e])));
+#pragma unroll 4
+    for (int64_t e = 4 * threadIdx.x; e < d; e += 4 * kThreads) {
+        const f32x4 v = load4(xr + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, magnitude(v[i]));
+    }
     top = row_umax<kThreads / kWave>(top, tops);
     const RowCode rc = row_code(top);
-    for (int64_t e = threadIdx.x; e < d; e += kThreads) {
-        const float v[4] = {static_cast<float>(xr[e]), 0.f, 0.f, 0.f};
-        q[row * ldq + e] = static_cast<int8_t>(codes4(v, rc) & 0xffu);
+#pragma unroll 4
+    for (int64_t e = 4 * threadIdx.x; e < d; e += 4 * kThreads) {
+        const f32x4 y = load4(xr + e);
+        const float v[4] = {y[0], y[1], y[2], y[3]};
+        *reinterpret_cast<uint32_t*>(q + row * ldq + e) = codes4(v, rc);
     }
     if (threadIdx.x == 0) scale[row] = rc.scale;
 }
@@ -322,7 +351,7 @@ constexpr int kW = kThreads / kWave;   // wavefronts of a row that a whole workg
 // Workgroups for the rows, in two dimensions: one may hold 2^32 threads at most.
 template <int W>
 dim3 row_blocks(int rows) {
-    constexpr int per = kW / W;
+    constexpr int per = kBlock<W> / kWave / W;
     const int64_t n = (int64_t(rows) + per - 1) / per, x = n < (1 << 20) ? n : 1 << 20;
     return dim3(static_cast<unsigned>(x), static_cast<unsigned>((n + x - 1) / x));
 }
@@ -334,11 +363,11 @@ void launch_norm(float* x, const T* add, const float* g, int rows, int d, float 
 
 template <typename T, bool ADD>
 void norm_dispatch(float* x, const T* add, const float* g, int rows, int d, float eps, int8_t* q, float* scale, hipStream_t s) {
-    const int of_wave = (d + kWave * 4 - 1) / (kWave * 4);    // chunks of a lane of one wavefront
+    const int of_wave = (d - 1) / (kWave * 4) + 1;    // chunks of a lane of one wavefront
     if (of_wave <= 1) return launch_norm<T, ADD, 1, 1>(x, add, g, rows, d, eps, q, scale, s);
     if (of_wave <= 2) return launch_norm<T, ADD, 1, 2>(x, add, g, rows, d, eps, q, scale, s);
     if (of_wave <= 4) return launch_norm<T, ADD, 1, 4>(x, add, g, rows, d, eps, q, scale, s);
-    const int nc = (d + kThreads * 4 - 1) / (kThreads * 4);   // and of a whole workgroup
+    const int nc = (d - 1) / (kThreads * 4) + 1;   // and of a whole workgroup
     if (nc <= 2) return launch_norm<T, ADD, kW, 2>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 4) return launch_norm<T, ADD, kW, 4>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 8) return launch_norm<T, ADD, kW, 8>(x, add, g, rows, d, eps, q, scale, s);
@@ -348,21 +377,24 @@ void norm_dispatch(float* x, const T* add, const float* g, int rows, int d, floa
 
 template <typename T, int W, int NC>
 void launch_rows(const T* x, int64_t ldx, int rows, int d, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
-    quantize_kernel<T, W, NC><<<row_blocks<W>(rows), kThreads, 0, s>>>(x, ldx, rows, d, q, ldq, scale);
+    quantize_kernel<T, W, NC><<<row_blocks<W>(rows), kBlock<W>, 0, s>>>(x, ldx, rows, d, q, ldq, scale);
 }
 
 template <typename T>
 void rows_dispatch(const T* x, int64_t ldx, int rows, int d, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
     constexpr int E = 16 / sizeof(T);
-    const int of_wave = (d + kWave * E - 1) / (kWave * E);
+    const int of_wave = (d - 1) / (kWave * E) + 1;
     if (of_wave <= 1) return launch_rows<T, 1, 1>(x, ldx, rows, d, q, ldq, scale, s);
     if (of_wave <= 2) return launch_rows<T, 1, 2>(x, ldx, rows, d, q, ldq, scale, s);
     if (of_wave <= 4) return launch_rows<T, 1, 4>(x, ldx, rows, d, q, ldq, scale, s);
-    const int nc = (d + kThreads * E - 1) / (kThreads * E);
+    const int nc = (d - 1) / (kThreads * E) + 1;
     if (nc <= 2) return launch_rows<T, kW, 2>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 4) return launch_rows<T, kW, 4>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 8) return launch_rows<T, kW, 8>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 16) return launch_rows<T, kW, 16>(x, ldx, rows, d, q, ldq, scale, s);
+    const int nc16 = (d - 1) / (16 * kWave * E) + 1;          // and of one of 16 wavefronts
+    if (nc16 <= 8) return launch_rows<T, 16, 8>(x, ldx, rows, d, q, ldq, scale, s);
+    if (nc16 <= 16) return launch_rows<T, 16, 16>(x, ldx, rows, d, q, ldq, scale, s);
     quantize_long_kernel<T><<<row_blocks<kW>(rows), kThreads, 0, s>>>(x, ldx, rows, d, q, ldq, scale);
 }
 

@@ -42,7 +42,7 @@ def check_codes(y, q, scale, rel):
 
 
 ROWS = [(1, 16), (1, 4096), (3, 48), (5, 688), (65, 1024), (7, 1040), (130, 2064), (33, 5120), (9, 8192), (4, 14336),
-        (3, 20000), (2, 33040), (4100, 256), (2500, 688)]
+        (3, 20000), (2, 33040), (2, 70000), (3, 140000), (4100, 256), (2500, 688)]
 
 
 @pytest.mark.parametrize("rows,d", ROWS)
@@ -64,7 +64,7 @@ def test_quantize_rows(rows, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("d", [64, 2048, 20000])
+@pytest.mark.parametrize("d", [64, 2048, 20000, 140000])
 def test_quantize_rows_special(dtype, d):
     """Zero rows, magnitudes at both ends of the type, ties, and rows with NaN or infinities."""
     code, t = DT[dtype]
@@ -342,6 +342,26 @@ def test_rows_more_than_a_launch_dimension_holds():
     assert torch.equal(q, ((x > 0) * 127).to(torch.int8))
     pp.pp_rmsnorm_quant(pp.PP_F32, x, None, torch.ones(d, device="cuda"), rows, d, 0.5, q, scale)
     assert torch.equal(q, ((x > 0) * 127).to(torch.int8))
+
+
+def test_rows_of_nearly_2_31_values():
+    """The longest row: three values that are not 0, at its ends and in the middle."""
+    d = 2 ** 31 - 16
+    at = torch.tensor([0, d // 2 + 1, d - 1], device="cuda")
+    val = torch.tensor([-1.0, 2.0, 3.0], device="cuda")
+    want = torch.tensor([-42, 85, 127], dtype=torch.int8, device="cuda")       # 127 / 3, 254 / 3, 127
+    q, scale = torch.empty(d, dtype=torch.int8, device="cuda"), torch.empty(1, device="cuda")
+    for t, code in ((torch.bfloat16, pp.PP_BF16), (torch.float32, pp.PP_F32)):
+        x = torch.zeros(d, dtype=t, device="cuda")
+        x[at] = val.to(t)
+        q.fill_(9)
+        pp.pp_quantize_rows(code, x, d, 1, d, q, d, scale)
+        assert torch.equal(q[at], want) and int(q.count_nonzero()) == 3
+        pp.pp_dequantize_rows(code, q, d, scale, 1, d, x, d)
+        assert torch.equal(x[at], (want.float() * scale).to(t)) and int(x.count_nonzero()) == 3
+    q.fill_(9)
+    pp.pp_rmsnorm_quant(pp.PP_F32, x, None, torch.ones(d, device="cuda"), 1, d, 0.0, q, scale)
+    assert torch.equal(q[at], want) and int(q.count_nonzero()) == 3
 
 
 @pytest.mark.parametrize("M,N,K", [(7, 512, 272), (100, 512, 272), (1309, 2048, 688)])
