@@ -56,6 +56,12 @@ __device__ __forceinline__ float quant_add(float c, float v) {
     return c + v;
 }
 
+// Four scales, which start at any float.
+__device__ __forceinline__ f32x4 quant_scales4(const float* p) {
+    typedef f32x4 unaligned __attribute__((aligned(4)));
+    return *reinterpret_cast<const unaligned*>(p);
+}
+
 // Four consecutive results to memory (8- or 16-byte store; rows start on 8-byte boundaries at least).
 __device__ __forceinline__ void quant_store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
 __device__ __forceinline__ void quant_store4(bf16* p, f32x4 v) {
@@ -69,7 +75,7 @@ __device__ __forceinline__ void quant_store4(bf16* p, f32x4 v) {
 // the gate's sums and up those of the column block 16 further.
 template <int EPI, typename TO>
 __device__ __forceinline__ void quant_finish4(const ppk::QuantGemm& g, int m, int n, float as, i32x4 acc, i32x4 up) {
-    const f32x4 bs = *reinterpret_cast<const f32x4*>(g.b_scale + n);
+    const f32x4 bs = quant_scales4(g.b_scale + n);
     f32x4 v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = quant_scaled(acc[e], as, bs[e]);
@@ -80,7 +86,7 @@ __device__ __forceinline__ void quant_finish4(const ppk::QuantGemm& g, int m, in
         for (int e = 0; e < 4; ++e) v[e] = quant_add(o[e], v[e]);
         quant_store4(c, v);
     } else if constexpr (EPI == ppk::kSwiGLU) {
-        const f32x4 bu = *reinterpret_cast<const f32x4*>(g.b_scale + n + 16);
+        const f32x4 bu = quant_scales4(g.b_scale + n + 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = quant_swiglu<TO>(v[e], quant_scaled(up[e], as, bu[e]));
         // columns 32 j + c (gate) become 16 j + c

@@ -1,14 +1,23 @@
 // Projection GEMM of 8-bit codes: C[M, N] = A[M, K] B[N, K]^T with a scale for each row of A (token)
 // and of B (output channel), exact int32 sums on the matrix cores, and the epilogues of a decoder
-// layer.  This file: the 256 x 256 tiles of large batches, and the choice between the kernels.
+// layer.  This file: the 256 x 256, 192 x 256 and 192 x 192 tiles of large batches, and the choice between
+// the kernels.
 //
 // The arrangement is k_gemm_bf16.hip's, whose 64-value steps of K are 128 bytes as the 128-value
-// steps here are: one 256-thread workgroup (4 wavefronts, one per SIMD) per tile, each wavefront
-// 128 x 128 values as 8 x 8 blocks of the 16x16x64 int8 MFMA (twice the products of the bf16 one in the
-// same time), its accumulators in the accumulation registers; operand tiles go from memory straight into an
-// LDS ring of 5 slots of 32 KB (A and B of a step are one slot each), two in flight while a step is
-// read; the workgroup's tiles are one stream of steps, whose loads cross tile boundaries; persistent, one
-// workgroup per CU, every XCD on a compact block of tiles.
+// steps here are: one 256-thread workgroup (4 wavefronts, one per SIMD) per tile, a quarter of it to
+// each wavefront (of the largest tile 128 x 128 values, 8 x 8 blocks of the 16x16x64 int8 MFMA: twice the
+// products of the bf16 one in the same time), accumulators in the accumulation registers; operand
+// tiles go from memory straight into an LDS ring of 5 slots of 32 KB (A and B of a step are one slot
+// each), two in flight while a step is read; the workgroup's tiles are one stream of steps, whose loads cross
+// tile boundaries; persistent, one workgroup per CU, every XCD on a compact block of tiles.
+//
+// What bounds it: 27,721 rows, N 22016, K 4096 with SwiGLU take 1.86 ms, 2.69 POP/s (a large int8 product of
+// the vendor's library 2.43); the matrix cores are 67% busy at 1.93 GHz.  The MFMAs alone reach 3.9 POP/s on
+// random codes and 4.75 on zeros: power holds the clock.  A step takes 1.54 us, 1.17 without the
+// loads of operands (zeros: 1.21 and 1.12); with every operand in L2 the call would be 4% faster.  One
+// wavefront a SIMD has to issue everything between its MFMAs, so nothing else may stand in the loop: moving
+// the last step's offsets for a ragged K (instead of the step as a whole) cost 10%.  Weights through registers
+// instead of direct loads: 4% slower.
 //
 // K need only be a multiple of 16 and 128 at least: the last step is the last 128 values, and the
 // activations' fragments are zeroed where the step before had them already (what the weights hold then
@@ -42,7 +51,7 @@ __device__ __forceinline__ void epilogue(i32x4 (&acc)[NB][MB], const ppk::QuantG
     const bool in_row = lane % CH * PER < COLS;   // (chunks past a row of 6 blocks hold nothing)
     f32x4 bs[NB];
 #pragma unroll
-    for (int i = 0; i < NB; ++i) bs[i] = *reinterpret_cast<const f32x4*>(q.b_scale + min(nb0 + 16 * i, q.N - 16) + 4 * g);
+    for (int i = 0; i < NB; ++i) bs[i] = quant_scales4(q.b_scale + min(nb0 + 16 * i, q.N - 16) + 4 * g);
     float as[MB];
 #pragma unroll
     for (int j = 0; j < MB; ++j) as[j] = q.a_scale[min(mb + 16 * j + lr, q.M - 1)];
@@ -305,14 +314,16 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     __builtin_amdgcn_s_waitcnt(0);   // no load may still be writing LDS when the workgroup ends
 }
 
-int ceil_div(int a, int b) { return a / b + (a % b != 0); }
+template <typename T>
+T ceil_div(T a, int b) { return a / b + (a % b != 0); }
 
 // Output tiles of the XCD that takes most, by either division of the tile list.
 struct XcdSplit {
-    int balanced, tiles;
+    int balanced;
+    int64_t tiles;
 };
 XcdSplit xcd_split(int tiles_m, int tiles_n, int wg_per_xcd) {
-    const int blocked = ceil_div(tiles_m, 8) * tiles_n, even = ceil_div(tiles_m * tiles_n, 8);
+    const int64_t blocked = int64_t(ceil_div(tiles_m, 8)) * tiles_n, even = ceil_div(int64_t(tiles_m) * tiles_n, 8);
     const int balanced = ceil_div(even, wg_per_xcd) < ceil_div(blocked, wg_per_xcd) ? 1 : 0;
     return XcdSplit{balanced, balanced ? even : blocked};
 }
@@ -331,7 +342,7 @@ void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
     const XcdSplit x = xcd_split(n_mt, tiles_n, wg_per_xcd);
     QuantGemm q = g;
     if (MB == 8 && !g.mtile_m0) q.M = std::min<int64_t>(g.M, int64_t(n_mt) * BM);
-    gemm_quant_kernel<EPI, TO, MB, NB><<<8 * std::min(wg_per_xcd, x.tiles), NT, LDS_BYTES, s>>>(q, n_mt, tiles_n, x.balanced);
+    gemm_quant_kernel<EPI, TO, MB, NB><<<8 * static_cast<int>(std::min<int64_t>(wg_per_xcd, x.tiles)), NT, LDS_BYTES, s>>>(q, n_mt, tiles_n, x.balanced);
 }
 
 // Which kernel takes which rows.  An estimate in us, for the CU with the most tiles: a launch and its first
