@@ -4,9 +4,12 @@
 // scale = max|y| * (1 / 127), code = round(y / scale).  Both need the whole row before the first code
 // is written, so a row stays in registers between its one read and its one write: memory bounds
 // both kernels (27,721 x 4096: quantize_rows of bf16 59 us, 5.8 TB/s; rmsnorm_quant with a bf16 residual 217 us,
-// 5.7 TB/s; and dequantize_rows to bf16 57 to 70 us, 4.9 to 6.0 TB/s).  A row of up to four 16-byte chunks per lane is one
-// wavefront's, a longer one a workgroup's: 20,000 rows of 688 bf16 values 9.3 us and 19.4, of 4096 46.2 and
-// 43.5.  quantize_rows has workgroups of 16 wavefronts too, for the rows of a wide layer's second weight (up to
+// 5.7 TB/s; and dequantize_rows to bf16 57 to 70 us, 4.9 to 6.0 TB/s).
+//
+// A row of up to four 16-byte chunks per lane is one wavefront's, a longer one a workgroup's: 20,000 rows
+// of 688 bf16 values 9.3 us and 19.4, of 4096 46.2 and 43.5.  Six chunks a thread beside eight, for the
+// registers: rmsnorm_quant of 3951 x 5120 20.0 -> 19.0 us, 300 x 5120 5.7 -> 5.1, 27,721 x 5120 1% slower.
+// quantize_rows has workgroups of 16 wavefronts too, for the rows of a wide layer's second weight (up to
 // 65,536 float32 or 131,072 bf16 values): 4096 x 28,672 float32 106 us, 5.5 TB/s, instead of 156 with two reads.
 #include "device.h"
 #include "kernels.h"
@@ -370,6 +373,7 @@ void norm_dispatch(float* x, const T* add, const float* g, int rows, int d, floa
     const int nc = (d - 1) / (kThreads * 4) + 1;   // and of a whole workgroup
     if (nc <= 2) return launch_norm<T, ADD, kW, 2>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 4) return launch_norm<T, ADD, kW, 4>(x, add, g, rows, d, eps, q, scale, s);
+    if (nc <= 6) return launch_norm<T, ADD, kW, 6>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 8) return launch_norm<T, ADD, kW, 8>(x, add, g, rows, d, eps, q, scale, s);
     if (nc <= 16) return launch_norm<T, ADD, kW, 16>(x, add, g, rows, d, eps, q, scale, s);
     rmsnorm_quant_long_kernel<T><<<row_blocks<kW>(rows), kThreads, 0, s>>>(x, add, g, rows, d, eps, q, scale);
@@ -390,6 +394,7 @@ void rows_dispatch(const T* x, int64_t ldx, int rows, int d, int8_t* q, int64_t 
     const int nc = (d - 1) / (kThreads * E) + 1;
     if (nc <= 2) return launch_rows<T, kW, 2>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 4) return launch_rows<T, kW, 4>(x, ldx, rows, d, q, ldq, scale, s);
+    if (nc <= 6) return launch_rows<T, kW, 6>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 8) return launch_rows<T, kW, 8>(x, ldx, rows, d, q, ldq, scale, s);
     if (nc <= 16) return launch_rows<T, kW, 16>(x, ldx, rows, d, q, ldq, scale, s);
     const int nc16 = (d - 1) / (16 * kWave * E) + 1;          // and of one of 16 wavefronts
