@@ -154,6 +154,10 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
         n0 = within / gsz * TN;
     };
     const int nk = (q.K + kQuantStep - 1) / kQuantStep;
+    // Every XCD starts at another eighth of K and goes round, so that not all wait for the same channels of
+    // the memory.  Weights from memory, us together and so: 2926 rows, N 6144, K 4096 81, 73; 2000 rows, N 4096,
+    // K 11008 93, 88; 6000 rows, N 6144, K 5120 166, 160; where the products bound it no difference.
+    const int k_rot = xcd * nk / 8;
     const int tail = q.K % kQuantStep;   // values of the last step, 0: a whole one
 
     // ---- direct memory -> LDS loads: each fills 1 KB = 8 rows x 128 bytes of a slot, lane l landing at
@@ -168,7 +172,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     int voff_a[MB], voff_b[NB];
     // load cursor: the step being requested, into slots l_sa (A) and l_sb (B); l_local >= n_local once the
     // stream is exhausted (its loads are then dead: they read nothing, into slots that are not read again)
-    int l_local = slot, l_kt = 0, l_sa = 0, l_sb = 1, l_k = 0;   // l_k: first value of the step
+    int l_local = slot, l_kt = k_rot, l_sa = 0, l_sb = 1, l_k = min(k_rot * kQuantStep, q.K - kQuantStep);   // l_kt: step of K, l_k: its first value
     __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
     const __amdgpu_buffer_rsrc_t rsrc_0 = quant_rsrc(q.A, 0);
     auto set_cursor_tile = [&]() {
@@ -203,8 +207,8 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     auto advance_cursor = [&]() {
         l_sa = l_sa >= NSLOT - 2 ? l_sa + 2 - NSLOT : l_sa + 2;
         l_sb = l_sb >= NSLOT - 2 ? l_sb + 2 - NSLOT : l_sb + 2;
-        l_wrap = l_kt == nk - 1;
-        l_kt = l_wrap ? 0 : l_kt + 1;
+        l_kt = l_kt == nk - 1 ? 0 : l_kt + 1;
+        l_wrap = l_kt == k_rot;
         l_k = min(l_kt * kQuantStep, q.K - kQuantStep);
     };
     auto advance_tile = [&]() {
@@ -289,7 +293,7 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
         for (int kt = 0; kt < nk; ++kt) {
             const int n_sa = c_sa >= NSLOT - 2 ? c_sa + 2 - NSLOT : c_sa + 2;
             const int n_sb = c_sb >= NSLOT - 2 ? c_sb + 2 - NSLOT : c_sb + 2;
-            const bool cut = tail && kt == nk - 1;
+            const bool cut = tail && kt == nk - 1 - k_rot;
             if (cut) zero_again(0, F0);
             substep(F0, F1, c_sa, c_sb, 1, true);    // A tile of g+2
             if (l_local >= n_local) __builtin_amdgcn_s_waitcnt(quant_wait(0));   // dead loads may end out of turn

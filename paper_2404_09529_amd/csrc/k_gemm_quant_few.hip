@@ -33,13 +33,19 @@ __global__ __launch_bounds__(64 * NW) void gemm_few_kernel(ppk::QuantGemm q) {
 #pragma unroll
     for (int i = 0; i < NB; ++i) rb[i] = min(16 * i + lr, b_rows - 1) * ldb;
 
+    // Where in K the workgroup starts (and goes round), so that not all wait for the same channels of the
+    // memory: in one round of workgroups those of an XCD together, which then find the activations in its
+    // L2, and the XCDs apart; in several all of them apart.  Weights from memory, us without and with: 10
+    // rows, N 4096, K 11008 13.9, 12.4; one row, N 12288, K 4096 13.0, 12.4; N 28672, K 8192 56.4, 51.5.
+    const int k_rot = static_cast<int>((gridDim.x <= 256 ? (blockIdx.x & 7) * 32 : blockIdx.x & 255) * nk >> 8);
+    auto place = [&](int s) { return s + k_rot >= nk ? s + k_rot - nk : s + k_rot; };   // of the s-th step, in K
     struct Step { i32x4 b[2][NB], a[2][MB]; };
     auto load = [&](int s, Step& f) {   // steps past the last read nothing (an empty descriptor) and give zeros
         const __amdgpu_buffer_rsrc_t r_a = quant_rsrc(q.A, s < nk ? bytes_a : 0), r_b = quant_rsrc(B, s < nk ? bytes_b : 0);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             // lanes past K read the row's last 16 values again; the activations are then zeroed
-            const int k = s * kQuantStep + 64 * ks + 16 * g, kc = min(k, q.K - 16);
+            const int k = place(s) * kQuantStep + 64 * ks + 16 * g, kc = min(k, q.K - 16);
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 const int at = rb[i] + kc;
@@ -58,6 +64,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_few_kernel(ppk::QuantGemm q) {
 #pragma unroll
         for (int j = 0; j < MB; ++j) acc[i][j] = i32x4{};
     auto add = [&](int s, Step& f) {
+        s = place(s);
         if ((s + 1) * kQuantStep > q.K) {
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks)

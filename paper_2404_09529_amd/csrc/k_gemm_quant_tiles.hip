@@ -79,6 +79,13 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
     const int nk = EPI == ppk::kPartial ? static_cast<int>(int64_t(all) * (blockIdx.y + 1) / gridDim.y) - k_first : all;
     const int tail = k_first + nk == all ? q.K % kQuantStep : 0;   // values of the last step, 0: a whole one
 
+    // Where in K this workgroup starts (and goes round): every XCD at another eighth.  At rows of some
+    // strides, multiples of 4096 bytes among them, workgroups at the same K wait for the same few channels of
+    // the memory; those of an XCD stay together, for the lines that they share in its L2.  us, all together
+    // and so: 48 rows, N 28672, K 4096 32.3, 26.3; 8192 50.7, 45.5; 11008 78.3, 68.4; 4224 27.3, 27.7; 1309
+    // rows, N 2048, K 5504 35.0, 31.9 (from the 256 MB of last-level cache 29.2, 29.2).
+    const int k_rot = xcd * nk / 8;
+
     // ---- direct memory -> LDS loads: 1 KB = 8 rows x 128 bytes each; every address in range
     const int lda = static_cast<int>(q.lda), ldb = static_cast<int>(q.ldb);
     const int lrow = lane >> 3;
@@ -93,15 +100,15 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
     int voff_a[G::A_LD], voff_b[G::B_LD];
     // the parity of a load's first row group: wavefront w's t-th load starts at row 8 (LD w + t)
     const int odd_a = G::A_LD * wave & 1, odd_b = G::B_LD * wave & 1;
-    auto step_back = [&]() {
+    auto step_back = [&](int sign) {   // sign -1: undone
 #pragma unroll
-        for (int t = 0; t < G::A_LD; ++t) voff_a[t] -= (t + odd_a) & 1 ? back[1] : back[0];
+        for (int t = 0; t < G::A_LD; ++t) voff_a[t] -= sign * ((t + odd_a) & 1 ? back[1] : back[0]);
 #pragma unroll
-        for (int t = 0; t < G::B_LD; ++t) voff_b[t] -= (t + odd_b) & 1 ? back[1] : back[0];
+        for (int t = 0; t < G::B_LD; ++t) voff_b[t] -= sign * ((t + odd_b) & 1 ? back[1] : back[0]);
     };
     // load cursor: the step being requested, into slot l_slot; past the last one its loads go
     // through an empty descriptor (they read nothing and land in slots that are not read again)
-    int l_local = slot0, l_kt = 0, l_slot = 0;
+    int l_local = slot0, l_kt = 0, l_k = k_rot, l_slot = 0;   // (l_kt steps of the tile are done, l_k is the next one in K)
     __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
     const __amdgpu_buffer_rsrc_t rsrc_0 = quant_rsrc(q.A, 0);
     auto set_cursor_tile = [&]() {
@@ -117,7 +124,7 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
 #pragma unroll
             for (int t = 0; t < G::B_LD; ++t)
                 voff_b[t] = min(8 * (G::B_LD * wave + t) + lrow, b_rows - 1) * ldb + ((t + odd_b) & 1 ? chunk_off[1] : chunk_off[0]);
-            if (nk == 1) step_back();
+            if (tail && l_k == nk - 1) step_back(1);
         } else {
             rsrc_a = rsrc_0;
             rsrc_b = rsrc_0;
@@ -129,17 +136,19 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
         char* dst = smem + l_slot * G::SLOT_B + (is_a ? (G::A_LD * wave + t) * 1024
                                                       : BM * ROW_B + (G::B_LD * wave + t - G::A_LD) * 1024);
         const int voff = is_a ? voff_a[is_a ? t : 0] : voff_b[is_a ? 0 : t - G::A_LD];
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rsrc_a : rsrc_b, (lds_void*)dst, 16, voff, (k_first + l_kt) * ROW_B, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rsrc_a : rsrc_b, (lds_void*)dst, 16, voff, (k_first + l_k) * ROW_B, 0, 0);
     };
     auto advance_cursor = [&]() {
         l_slot = l_slot == NS - 1 ? 0 : l_slot + 1;
         if (l_local >= n_local) return;
+        l_k = l_k == nk - 1 ? 0 : l_k + 1;
         if (++l_kt == nk) {
             l_kt = 0;
             l_local += n_slots;
             set_cursor_tile();
-        } else if (l_kt == nk - 1 && tail) {
-            step_back();
+        } else if (tail) {
+            if (l_k == nk - 1) step_back(1);
+            else if (l_k == 0) step_back(-1);
         }
     };
 
@@ -213,7 +222,7 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
         for (int i = 0; i < NB; ++i)
 #pragma unroll
             for (int j = 0; j < MB; ++j) acc[i][j] = i32x4{};
-        const int cut = tail ? nk - 1 : -1;   // the step that K ends in
+        const int cut = tail ? nk - 1 - k_rot : -1;   // the step that K ends in
         int kt = 0;
         for (; kt + 2 <= nk; kt += 2) {
             step(F0, F1, c_slot, kt == cut);
