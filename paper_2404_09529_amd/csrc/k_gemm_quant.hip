@@ -351,25 +351,29 @@ void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
 
 // Which kernel takes which rows.  An estimate in us, for the CU with the most tiles: a launch and its first
 // loads, then each tile's steps of K and its epilogue; at least the time of the call's bytes at the
-// memory's rate (weights at 4.6 .. 4.8 TB/s) and of what the tiles fetch from L2 together.  The
-// constants are fitted to timings of some 260 sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400)
-// on every kernel; over those sizes the choice costs 2% of the best kernel's time on average, 46% at worst.
+// memory's rate and of what the tiles fetch from L2 together.  The constants are fitted to timings of 340
+// sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400) on every kernel, half of them also with weights
+// that come from memory instead of the last-level cache; over these the choice costs 2% of the best kernel's
+// time on average, 42% at worst.
 // The 192-row tiles are for the rounds that 256 x 256 ones leave part empty: 2000 rows, N 4096, K 11008 in
-// 242 of 192 x 192 88 us, in 128 of 256 x 256 113; 2926 rows, N 4096, K 14336 in 256 of 192 x 256 143 and 169 us.
+// 242 of 192 x 192 83 us, in 128 of 256 x 256 113; 2926 rows, N 4096, K 14336 in 256 of 192 x 256 150 and 169 us.
 struct Choice {
     enum Kind { kFew, kTile, k192x192, k192x256, k256x256 } kind;
     int tile, splits;   // kFew: column blocks in `tile`
     int big;            // kTile: 256-row tiles that the 256 x 256 kernel takes before it
 };
 
-constexpr float kStart = 3.0f, kBigEpilogue = 7.0f, kBigStep = 1.36f, kStep192 = 1.12f, kStepSquare192 = 0.80f;
-constexpr float kWeights = 4.6e6f, kMemory = 4.8e6f, kFabric = 90e6f;   // bytes per us
+constexpr float kStart = 3.4f, kBigEpilogue = 6.9f, kBigStep = 1.38f, kStep192 = 1.16f, kStepSquare192 = 0.83f;
+constexpr float kMemory = 6.0e6f, kFabric = 67.5e6f;   // bytes per us
+// few rows: a launch, a round of workgroups, what a CU receives (bytes per us), weights and the activations that
+// all workgroups read
+constexpr float kFewStart = 1.7f, kFewRound = 0.32f, kFewCu = 40e3f, kFewWeights = 5.0e6f, kFewShared = 12e6f;
 // a CU's only tile, and each of several (two or three of the smallest at a time)
-constexpr float kTileAlone[kQuantTiles] = {0.22f, 0.24f, 0.38f, 0.49f, 1.0f};
-constexpr float kTileStep[kQuantTiles] = {0.175f, 0.235f, 0.38f, 0.65f, 1.06f};
-constexpr float kTileEpilogue[kQuantTiles] = {0.6f, 1.1f, 1.5f, 2.6f, 6.0f};
+constexpr float kTileAlone[kQuantTiles] = {0.20f, 0.28f, 0.33f, 0.32f, 0.87f};
+constexpr float kTileStep[kQuantTiles] = {0.175f, 0.25f, 0.345f, 0.59f, 1.08f};
+constexpr float kTileEpilogue[kQuantTiles] = {0.66f, 1.1f, 2.0f, 3.9f, 6.8f};
 // a second launch, and its sums written and read
-constexpr float kFinish = 4.0f, kFinishShare = 0.4f, kFinishBytes = 2.5e6f;
+constexpr float kFinish = 3.4f, kFinishShare = 0.46f, kFinishBytes = 4.6e6f;
 
 // n_mt < 0: every row of M; else the entries of a row-tile list.
 Choice choose(int M, int N, int K, int n_mt) {
@@ -386,14 +390,15 @@ Choice choose(int M, int N, int K, int n_mt) {
             best = c;
         }
     };
-    // up to 16 rows the registers take four column blocks; more rows only where 16 columns per workgroup
-    // make one round (beyond that the tiles read the activations less often)
-    if (rows <= 16 || (rows <= kQuantFewRows && N <= 16 * 8 * wg)) {
-        const int round = 16 * 8 * wg;
-        const int blocks = N <= round ? 1 : (N <= 2 * round || N > 4 * round ? 2 : 4);
-        const int rounds = ceil_div(N, blocks * round), row_blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-        const float time = rounds * (0.75f + 16.f * (blocks + row_blocks) * K / 53e3f);
-        consider(1.3f + std::max(time, bytes / kWeights), Choice{Choice::kFew, blocks, 1, 0});
+    if (rows <= kQuantFewRows) {
+        const int row_blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        for (int blocks : {1, 2, 4}) {
+            if (blocks == 4 && row_blocks > 1) continue;   // (the registers)
+            const int wgs = ceil_div(N, 16 * blocks), rounds = ceil_div(wgs, 8 * wg);
+            const float cu = rounds * (kFewRound + 16.f * (blocks + row_blocks) * K / kFewCu);
+            const float mem = bytes / kFewWeights + float(wgs) * rows * K / kFewShared;
+            consider(kFewStart + std::max(cu, mem), Choice{Choice::kFew, blocks, 1, 0});
+        }
     }
     auto tile_time = [&](int t, int m, int splits) {
         const int64_t tiles = int64_t(ceil_div(m, kQuantTileRows[t])) * ceil_div(N, kQuantTileCols[t]);

@@ -6,10 +6,11 @@
 // of each of its rows), and their int32 sums, exact in any order, are added through LDS.  The activations
 // (16 MB rows, read again by every workgroup) come from L2 the same way.  No workgroup waits for another:
 // no workspace, no second launch.  More steps in flight per wavefront are no faster (10 rows, N 4096,
-// K 11008: 11.0 us, with two steps 11.4, with 16 wavefronts 11.5): the CU's requests are what is bounded.
-// What counts is one round of workgroups: NB is the smallest of 1, 2, 4 that makes at most 256 of them (16
-// rows, N 6144, K 4096: 384 workgroups of 16 columns 10.3 us, 192 of 32 8.1; one row, N 12288: 192 of 64
-// 11.0 us, 4.6 TB/s, 384 of 32 13.1).
+// K 11008: 10.7 us, with two steps 4% more, with 16 wavefronts 5%): the CU's requests are what is bounded.
+// What counts is few rounds of workgroups (16 rows, N 6144, K 4096: 384 workgroups of 16 columns 10.3 us, 192
+// of 32 8.1; one row, N 12288: 192 of 64 10.7 us, 4.7 TB/s, 384 of 32 13.1; one row, N 28672: 896 of 32
+// 23.1, 5.1 TB/s).  Tiles overtake it with the activations that every workgroup reads: 16 rows, N 28672 29 us, on
+// 64 x 128 tiles 25.
 //
 // The weight block is the MFMA's first operand: a lane ends with 4 consecutive columns of one row.
 #include "gemm_quant.h"

@@ -13,11 +13,11 @@
 // the ring takes the LDS, or several of 4 (64 rows, N 4096, K 8192 on 128 x 128 tiles: 43 us with 4
 // wavefronts, 37 with 8).  In the 32 x 64, 64 x 64 and 128 x 128 tiles two wavefronts share a
 // sub-tile, each with half of every step's K, so that they read a third less from LDS (35 us; 64 x 64
-// tiles 19.8 to 17.8); on 64 x 128 and 128 x 256 tiles that gave nothing or lost.  Lines that another CU of the XCD wants too come at up to 98 GB/s, the
-// others at 70.  Deeper rings and other orders of K are no faster.
+// tiles 19.8 to 17.8); on 64 x 128 and 128 x 256 tiles that gave nothing or lost.  Lines that another CU
+// of the XCD wants too come at up to 98 GB/s, the others at 70.  Deeper rings are no faster.
 // Measured (us; 256 x 256 tiles, the tile chosen): 344 rows, N 2048, K 5504: 70, 14.2 (64 x 64); 1309 rows:
-// 72, 29.0 (128 x 128); 100 rows, N 4096, K 4096: 51, 10.9 (32 x 64); 64 rows, N 4096, K 14336: 158, 19.8
-// (32 x 64 in shares of K); 48 rows, N 28672, K 4096: 53, 29.5, 4.0 TB/s (64 x 128).
+// 72, 28.8 (128 x 128); 100 rows, N 4096, K 4096: 51, 10.6 (32 x 64); 64 rows, N 4096, K 14336: 158, 20.8
+// (64 x 64 in shares of K); 48 rows, N 28672, K 4096: 53, 25.2, 4.7 TB/s (64 x 128).
 #include <algorithm>
 
 #include "gemm_quant.h"

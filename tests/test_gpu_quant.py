@@ -210,7 +210,11 @@ SIZES = [(1, 32, 16), (1, 512, 64), (2, 96, 144), (3, 32, 4096), (7, 4096, 688),
          # of them, tiles of 64 x 128 and 128 x 256, 192 x 192 (700 rows above), 192 x 256 and 256 x 256, whole
          # rounds of 256-row tiles with smaller ones after them
          (2800, 1600, 656), (640, 12800, 400), (2500, 2080, 1040), (12, 8192, 1040), (14, 12288, 528), (9, 20000, 144), (3000, 4096, 1040), (3500, 4064, 1040), (5000, 4064, 1040),
-         (8500, 4096, 1040), (33000, 544, 144)]
+         (8500, 4096, 1040), (33000, 544, 144),
+         # and two column blocks for 64 rows, 64 x 128 tiles alone, shares of K of the smaller tiles, 32 x 64 and
+         # 64 x 64 tiles after whole rounds
+         (39, 4160, 80), (257, 3808, 64), (41, 32, 4544), (41, 2784, 6448), (65, 5888, 6464), (520, 23840, 128),
+         (6235, 2656, 240)]
 
 
 def gemm_case(M, N, K, seed=0):
