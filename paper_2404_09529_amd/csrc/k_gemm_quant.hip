@@ -354,7 +354,7 @@ void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
 // memory's rate and of what the tiles fetch from L2 together.  The constants are fitted to timings of 340
 // sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400) on every kernel, half of them also with weights
 // that come from memory instead of the last-level cache; over these the choice costs 2% of the best kernel's
-// time on average, 42% at worst.
+// time on average, 37% at worst.
 // The 192-row tiles are for the rounds that 256 x 256 ones leave part empty: 2000 rows, N 4096, K 11008 in
 // 242 of 192 x 192 83 us, in 128 of 256 x 256 113; 2926 rows, N 4096, K 14336 in 256 of 192 x 256 150 and 169 us.
 struct Choice {
@@ -363,17 +363,18 @@ struct Choice {
     int big;            // kTile: 256-row tiles that the 256 x 256 kernel takes before it
 };
 
-constexpr float kStart = 3.4f, kBigEpilogue = 6.9f, kBigStep = 1.38f, kStep192 = 1.16f, kStepSquare192 = 0.83f;
-constexpr float kMemory = 6.0e6f, kFabric = 67.5e6f;   // bytes per us
-// few rows: a launch, a round of workgroups, what a CU receives (bytes per us), weights and the activations that
-// all workgroups read
-constexpr float kFewStart = 1.7f, kFewRound = 0.32f, kFewCu = 40e3f, kFewWeights = 5.0e6f, kFewShared = 12e6f;
+constexpr float kStart = 3.13f, kBigEpilogue = 6.94f, kBigStep = 1.39f, kStep192 = 1.16f, kStepSquare192 = 0.83f;
+constexpr float kMemory = 6.0e6f, kFabric = 66.4e6f;   // bytes per us
+// few rows: a launch, a round of workgroups, what a CU receives (bytes per us), weights (four column blocks: they
+// have half the wavefronts) and the activations that all workgroups read
+constexpr float kFewStart = 1.99f, kFewRound = 0.218f, kFewCu = 40.1e3f, kFewWeights = 5.16e6f, kFewWeights4 = 4.95e6f,
+                kFewShared = 12.7e6f;
 // a CU's only tile, and each of several (two or three of the smallest at a time)
-constexpr float kTileAlone[kQuantTiles] = {0.20f, 0.28f, 0.33f, 0.32f, 0.87f};
-constexpr float kTileStep[kQuantTiles] = {0.175f, 0.25f, 0.345f, 0.59f, 1.08f};
-constexpr float kTileEpilogue[kQuantTiles] = {0.66f, 1.1f, 2.0f, 3.9f, 6.8f};
+constexpr float kTileAlone[kQuantTiles] = {0.20f, 0.263f, 0.339f, 0.34f, 0.868f};
+constexpr float kTileStep[kQuantTiles] = {0.171f, 0.244f, 0.341f, 0.617f, 1.08f};
+constexpr float kTileEpilogue[kQuantTiles] = {0.677f, 1.09f, 1.99f, 3.39f, 6.75f};
 // a second launch, and its sums written and read
-constexpr float kFinish = 3.4f, kFinishShare = 0.46f, kFinishBytes = 4.6e6f;
+constexpr float kFinish = 4.24f, kFinishShare = 0.457f, kFinishBytes = 4.71e6f;
 
 // n_mt < 0: every row of M; else the entries of a row-tile list.
 Choice choose(int M, int N, int K, int n_mt) {
@@ -396,7 +397,7 @@ Choice choose(int M, int N, int K, int n_mt) {
             if (blocks == 4 && row_blocks > 1) continue;   // (the registers)
             const int wgs = ceil_div(N, 16 * blocks), rounds = ceil_div(wgs, 8 * wg);
             const float cu = rounds * (kFewRound + 16.f * (blocks + row_blocks) * K / kFewCu);
-            const float mem = bytes / kFewWeights + float(wgs) * rows * K / kFewShared;
+            const float mem = bytes / (blocks == 4 ? kFewWeights4 : kFewWeights) + float(wgs) * rows * K / kFewShared;
             consider(kFewStart + std::max(cu, mem), Choice{Choice::kFew, blocks, 1, 0});
         }
     }

@@ -213,7 +213,8 @@ SIZES = [(1, 32, 16), (1, 512, 64), (2, 96, 144), (3, 32, 4096), (7, 4096, 688),
          (8500, 4096, 1040), (33000, 544, 144),
          # and two column blocks for 64 rows, 64 x 128 tiles alone, shares of K of the smaller tiles, 32 x 64 and
          # 64 x 64 tiles after whole rounds
-         (39, 4160, 80), (257, 3808, 64), (41, 32, 4544), (41, 2784, 6448), (65, 5888, 6464), (520, 23840, 128),
+         (39, 4160, 80), (257, 3808, 64), (41, 32, 4544), (41, 2784, 6448), (65, 5888, 6464), (38, 32, 5392),
+         (90, 2240, 12496), (66, 6016, 7824), (520, 23840, 128),
          (6235, 2656, 240)]
 
 
