@@ -5,8 +5,7 @@
 // NS slots (A rows, then B rows of a step) filled NS - 1 steps ahead with direct-to-LDS loads of whole
 // 128-byte row segments.  Per step one barrier, after which a wavefront refills the slot whose fragments
 // it has, requests the next step's fragments, and runs the step's MFMAs meanwhile.  Ragged K and N as
-// in k_gemm_quant.hip, but that any K will do: in the last step lanes past K fetch the row's last
-// 16 values again.
+// in k_gemm_quant.hip, but that any K will do.
 //
 // What bounds it is what a CU receives.  A direct-to-LDS load of 1 KB holds its wavefront's next one back
 // for 140 cycles (17 GB/s a wavefront), so a CU wants 8 wavefronts at work: one workgroup of 8 where
@@ -89,26 +88,19 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
     // ---- direct memory -> LDS loads: 1 KB = 8 rows x 128 bytes each; every address in range
     const int lda = static_cast<int>(q.lda), ldb = static_cast<int>(q.ldb);
     const int lrow = lane >> 3;
-    // chunk fetched by this lane in loads of even and odd groups of 8 rows, and how far it steps back
-    // in the last step
-    int chunk_off[2], back[2];
+    // chunk fetched by this lane in loads of even and odd groups of 8 rows.  The last step of K is its last
+    // 128 values; of a K below that, lanes past it fetch the row's last 16 values again
+    int chunk_off[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        chunk_off[t] = 16 * ((lane & 7) ^ quant_swz(8 * t + lrow));
-        back[t] = tail ? max(0, chunk_off[t] - (tail - 16)) : 0;
-    }
+    for (int t = 0; t < 2; ++t) chunk_off[t] = min(16 * ((lane & 7) ^ quant_swz(8 * t + lrow)), q.K - 16);
     int voff_a[G::A_LD], voff_b[G::B_LD];
     // the parity of a load's first row group: wavefront w's t-th load starts at row 8 (LD w + t)
     const int odd_a = G::A_LD * wave & 1, odd_b = G::B_LD * wave & 1;
-    auto step_back = [&](int sign) {   // sign -1: undone
-#pragma unroll
-        for (int t = 0; t < G::A_LD; ++t) voff_a[t] -= sign * ((t + odd_a) & 1 ? back[1] : back[0]);
-#pragma unroll
-        for (int t = 0; t < G::B_LD; ++t) voff_b[t] -= sign * ((t + odd_b) & 1 ? back[1] : back[0]);
-    };
     // load cursor: the step being requested, into slot l_slot; past the last one its loads go
     // through an empty descriptor (they read nothing and land in slots that are not read again)
-    int l_local = slot0, l_kt = 0, l_k = k_rot, l_slot = 0;   // (l_kt steps of the tile are done, l_k is the next one in K)
+    int l_local = slot0, l_k = k_rot, l_slot = 0, l_off;   // l_k: step of K, l_off: its first value
+    auto set_cursor_step = [&]() { l_off = min((k_first + l_k) * ROW_B, max(q.K - ROW_B, 0)); };
+    set_cursor_step();
     __amdgpu_buffer_rsrc_t rsrc_a, rsrc_b;
     const __amdgpu_buffer_rsrc_t rsrc_0 = quant_rsrc(q.A, 0);
     auto set_cursor_tile = [&]() {
@@ -124,7 +116,6 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
 #pragma unroll
             for (int t = 0; t < G::B_LD; ++t)
                 voff_b[t] = min(8 * (G::B_LD * wave + t) + lrow, b_rows - 1) * ldb + ((t + odd_b) & 1 ? chunk_off[1] : chunk_off[0]);
-            if (tail && l_k == nk - 1) step_back(1);
         } else {
             rsrc_a = rsrc_0;
             rsrc_b = rsrc_0;
@@ -136,32 +127,30 @@ __global__ __launch_bounds__(G::NT, WGS * G::NW / 4) void gemm_quant_tiles_kerne
         char* dst = smem + l_slot * G::SLOT_B + (is_a ? (G::A_LD * wave + t) * 1024
                                                       : BM * ROW_B + (G::B_LD * wave + t - G::A_LD) * 1024);
         const int voff = is_a ? voff_a[is_a ? t : 0] : voff_b[is_a ? 0 : t - G::A_LD];
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rsrc_a : rsrc_b, (lds_void*)dst, 16, voff, (k_first + l_k) * ROW_B, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rsrc_a : rsrc_b, (lds_void*)dst, 16, voff, l_off, 0, 0);
     };
     auto advance_cursor = [&]() {
         l_slot = l_slot == NS - 1 ? 0 : l_slot + 1;
         if (l_local >= n_local) return;
         l_k = l_k == nk - 1 ? 0 : l_k + 1;
-        if (++l_kt == nk) {
-            l_kt = 0;
+        set_cursor_step();
+        if (l_k == k_rot) {
             l_local += n_slots;
             set_cursor_tile();
-        } else if (tail) {
-            if (l_k == nk - 1) step_back(1);
-            else if (l_k == 0) step_back(-1);
         }
     };
 
     const int wn = wave % G::WN, wm = wave / G::WN % G::WM, wk = wave / (G::WN * G::WM);
     int a_lds[KS], b_lds[KS];
-    bool past[KS];   // this lane's 16 values of the last step's half lie past K
+    bool past[KS];   // this lane's 16 values of the last step's half belong to the step before, or lie past K
 #pragma unroll
     for (int h = 0; h < KS; ++h) {
         const int ks = G::WK == 2 ? wk : h;
         const int phys = ((4 * ks + (lane >> 4)) ^ quant_swz(lane & 15)) * 16;
         a_lds[h] = (wm * 16 * MB + (lane & 15)) * ROW_B + phys;
         b_lds[h] = (BM + wn * 16 * NB + (lane & 15)) * ROW_B + phys;
-        past[h] = tail && 64 * ks + 16 * (lane >> 4) >= tail;
+        const int v = 64 * ks + 16 * (lane >> 4);
+        past[h] = tail && (q.K < ROW_B ? v >= tail : v < ROW_B - tail);
     }
     struct Frags { i32x4 w[KS][NB], a[KS][MB]; };   // a whole step's
     auto read_all = [&](int slot, Frags& f) {
