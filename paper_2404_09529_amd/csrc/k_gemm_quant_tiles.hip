@@ -14,8 +14,8 @@
 // sub-tile, each with half of every step's K, so that they read a third less from LDS (35 us; 64 x 64
 // tiles 19.8 to 17.8); on 64 x 128 and 128 x 256 tiles that gave nothing or lost.  Lines that another CU
 // of the XCD wants too come at up to 98 GB/s, the others at 70.  Deeper rings are no faster.
-// Measured (us; 256 x 256 tiles, the tile chosen): 344 rows, N 2048, K 5504: 70, 14.2 (64 x 64); 1309 rows:
-// 72, 28.8 (128 x 128); 100 rows, N 4096, K 4096: 51, 10.6 (32 x 64); 64 rows, N 4096, K 14336: 158, 20.8
+// Measured (us; 256 x 256 tiles, the tile chosen): 344 rows, N 2048, K 5504: 70, 14.4 (64 x 64); 1309 rows:
+// 72, 27.4 (128 x 128); 100 rows, N 4096, K 4096: 51, 10.3 (32 x 64); 64 rows, N 4096, K 14336: 158, 22.3
 // (64 x 64 in shares of K); 48 rows, N 28672, K 4096: 53, 25.2, 4.7 TB/s (64 x 128).
 #include <algorithm>
 
