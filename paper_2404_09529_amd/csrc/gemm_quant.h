@@ -5,12 +5,12 @@
 #include <atomic>
 
 #include "device.h"
+#include "gemm_quant_choice.h"
 #include "kernels.h"
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kQuantListRows = 256;   // rows of one entry of a plan's row-tile list
-constexpr int kQuantStep = 128;       // bytes (= values) of K in a step: whole cache lines, two MFMAs deep
 // Buffer descriptor word 3 for raw (unstructured) 32-bit-offset loads on gfx9-family parts.
 constexpr int kQuantRsrcWord3 = 0x00020000;
 
@@ -111,15 +111,11 @@ inline void quant_allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>
 
 // Up to 64 rows: weights straight from memory to the registers, 16 * blocks columns (blocks 1, 2, or
 // up to 16 rows 4) and all of K per workgroup.
-constexpr int kQuantFewRows = 64;
 void quant_gemm_few(int epi, bool out_f32, int blocks, const QuantGemm& g, hipStream_t s);
 
 // Tiles of kQuantTileRows x kQuantTileCols: entries mt_first .. mt_first + n_mt - 1 of the row-tile list
 // (without one: of the 256-row tiles of M).  splits > 1 (without a list, every row): K in that many
 // shares, whose sums go to g.part [splits][M][N], and a second launch for the epilogue.
-constexpr int kQuantTiles = 5;
-constexpr int kQuantTileRows[kQuantTiles] = {32, 64, 64, 128, 128};
-constexpr int kQuantTileCols[kQuantTiles] = {64, 64, 128, 128, 256};
 void quant_gemm_tiles(int epi, bool out_f32, int tile, const QuantGemm& g, int mt_first, int n_mt, int splits,
                       hipStream_t s);
 

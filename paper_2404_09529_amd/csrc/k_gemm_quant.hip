@@ -1,7 +1,7 @@
 // Projection GEMM of 8-bit codes: C[M, N] = A[M, K] B[N, K]^T with a scale for each row of A (token)
 // and of B (output channel), exact int32 sums on the matrix cores, and the epilogues of a decoder
-// layer.  This file: the 256 x 256, 192 x 256 and 192 x 192 tiles of large batches, and the choice between
-// the kernels.
+// layer.  This file: the 256 x 256, 192 x 256 and 192 x 192 tiles of large batches, and the calls of
+// the kernels that gemm_quant_choice.h picks.
 //
 // The arrangement is k_gemm_bf16.hip's, whose 64-value steps of K are 128 bytes as the 128-value
 // steps here are: one 256-thread workgroup (4 wavefronts, one per SIMD) per tile, a quarter of it to
@@ -318,20 +318,6 @@ __global__ __launch_bounds__(NT, 1) void gemm_quant_kernel(ppk::QuantGemm q, int
     __builtin_amdgcn_s_waitcnt(0);   // no load may still be writing LDS when the workgroup ends
 }
 
-template <typename T>
-T ceil_div(T a, int b) { return a / b + (a % b != 0); }
-
-// Output tiles of the XCD that takes most, by either division of the tile list.
-struct XcdSplit {
-    int balanced;
-    int64_t tiles;
-};
-XcdSplit xcd_split(int tiles_m, int tiles_n, int wg_per_xcd) {
-    const int64_t blocked = int64_t(ceil_div(tiles_m, 8)) * tiles_n, even = ceil_div(int64_t(tiles_m) * tiles_n, 8);
-    const int balanced = ceil_div(even, wg_per_xcd) < ceil_div(blocked, wg_per_xcd) ? 1 : 0;
-    return XcdSplit{balanced, balanced ? even : blocked};
-}
-
 }  // namespace
 
 namespace ppk {
@@ -342,113 +328,24 @@ template <int EPI, typename TO, int MB, int NB>
 void launch(const QuantGemm& g, int n_mt, hipStream_t s) {
     static std::atomic<uint64_t> done{0};
     quant_allow_lds(reinterpret_cast<const void*>(&gemm_quant_kernel<EPI, TO, MB, NB>), LDS_BYTES, done);
-    const int tiles_n = ceil_div(g.N, 32 * NB), wg_per_xcd = cu_count() / 8;
-    const XcdSplit x = xcd_split(n_mt, tiles_n, wg_per_xcd);
+    const int tiles_n = quant_div(g.N, 32 * NB), wg_per_xcd = cu_count() / 8;
+    const QuantXcdSplit x = quant_xcd_split(n_mt, tiles_n, wg_per_xcd);
     QuantGemm q = g;
     if (MB == 8 && !g.mtile_m0) q.M = std::min<int64_t>(g.M, int64_t(n_mt) * BM);
     gemm_quant_kernel<EPI, TO, MB, NB><<<8 * static_cast<int>(std::min<int64_t>(wg_per_xcd, x.tiles)), NT, LDS_BYTES, s>>>(q, n_mt, tiles_n, x.balanced);
 }
 
-// Which kernel takes which rows.  An estimate in us, for the CU with the most tiles: a launch and its first
-// loads, then each tile's steps of K and its epilogue; at least the time of the call's bytes at the
-// memory's rate and of what the tiles fetch from L2 together.  The constants are fitted to timings of 340
-// sizes (1 to 28,000 rows, N 256 to 28,800, K 256 to 14,400) on every kernel, half of them also with weights
-// that come from memory instead of the last-level cache; over these the choice costs 2% of the best kernel's
-// time on average, 37% at worst.
-// The 192-row tiles are for the rounds that 256 x 256 ones leave part empty: 2000 rows, N 4096, K 11008 in
-// 242 of 192 x 192 83 us, in 128 of 256 x 256 113; 2926 rows, N 4096, K 14336 in 256 of 192 x 256 150 and 169 us.
-struct Choice {
-    enum Kind { kFew, kTile, k192x192, k192x256, k256x256 } kind;
-    int tile, splits;   // kFew: column blocks in `tile`
-    int big;            // kTile: 256-row tiles that the 256 x 256 kernel takes before it
-};
-
-constexpr float kStart = 3.13f, kBigEpilogue = 6.94f, kBigStep = 1.39f, kStep192 = 1.16f, kStepSquare192 = 0.83f;
-constexpr float kMemory = 6.0e6f, kFabric = 66.4e6f;   // bytes per us
-// few rows: a launch, a round of workgroups, what a CU receives (bytes per us), weights (four column blocks: they
-// have half the wavefronts) and the activations that all workgroups read
-constexpr float kFewStart = 1.99f, kFewRound = 0.218f, kFewCu = 40.1e3f, kFewWeights = 5.16e6f, kFewWeights4 = 4.95e6f,
-                kFewShared = 12.7e6f;
-// a CU's only tile, and each of several (two or three of the smallest at a time)
-constexpr float kTileAlone[kQuantTiles] = {0.20f, 0.263f, 0.339f, 0.34f, 0.868f};
-constexpr float kTileStep[kQuantTiles] = {0.171f, 0.244f, 0.341f, 0.617f, 1.08f};
-constexpr float kTileEpilogue[kQuantTiles] = {0.677f, 1.09f, 1.99f, 3.39f, 6.75f};
-// a second launch, and its sums written and read
-constexpr float kFinish = 4.24f, kFinishShare = 0.457f, kFinishBytes = 4.71e6f;
-
-// n_mt < 0: every row of M; else the entries of a row-tile list.
-Choice choose(int M, int N, int K, int n_mt) {
-    const bool list = n_mt >= 0;
-    const int wg = cu_count() / 8, nk = ceil_div(K, kQuantStep), tiles_n = ceil_div(N, BN);
-    if (!list) n_mt = ceil_div(M, BM);
-    const int rows = list ? static_cast<int>(std::min<int64_t>(M, int64_t(n_mt) * BM)) : M;
-    const float bytes = (float(rows) + N) * K + 4.f * rows * N;
-    Choice best{Choice::kTile, 0, 1, 0};
-    float best_time = 1e30f;
-    auto consider = [&](float time, const Choice& c) {
-        if (time < best_time) {
-            best_time = time;
-            best = c;
-        }
-    };
-    if (rows <= kQuantFewRows) {
-        const int row_blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-        for (int blocks : {1, 2, 4}) {
-            if (blocks == 4 && row_blocks > 1) continue;   // (the registers)
-            const int wgs = ceil_div(N, 16 * blocks), rounds = ceil_div(wgs, 8 * wg);
-            const float cu = rounds * (kFewRound + 16.f * (blocks + row_blocks) * K / kFewCu);
-            const float mem = bytes / (blocks == 4 ? kFewWeights4 : kFewWeights) + float(wgs) * rows * K / kFewShared;
-            consider(kFewStart + std::max(cu, mem), Choice{Choice::kFew, blocks, 1, 0});
-        }
-    }
-    auto tile_time = [&](int t, int m, int splits) {
-        const int64_t tiles = int64_t(ceil_div(m, kQuantTileRows[t])) * ceil_div(N, kQuantTileCols[t]);
-        const int64_t per_cu = ((tiles * splits + 7) / 8 + wg - 1) / wg;
-        const float fetched = float(tiles) * (kQuantTileRows[t] + kQuantTileCols[t]) * K;
-        const float work = per_cu * kTileEpilogue[t] + ceil_div(nk, splits) * (per_cu == 1 ? kTileAlone[t] : per_cu * kTileStep[t]);
-        const float mem = ((float(m) + N) * K + 4.f * m * N) / kMemory + fetched / kFabric;
-        return kStart + std::max(work, mem) + (splits > 1 ? kFinish + splits * (kFinishShare + 4.f * m * N / kFinishBytes) : 0.f);
-    };
-    for (int t = 0; t < kQuantTiles; ++t) {
-        consider(tile_time(t, rows, 1), Choice{Choice::kTile, t, 1, 0});
-        if (list) continue;
-        const int64_t tiles = int64_t(ceil_div(M, kQuantTileRows[t])) * ceil_div(N, kQuantTileCols[t]);
-        for (int s : {2, 3, 4, 6, 8})   // shares of K, up to three workgroups per CU
-            if (s <= nk && tiles * s <= 24 * wg) consider(tile_time(t, M, s), Choice{Choice::kTile, t, s, 0});
-    }
-    if (rows <= kQuantFewRows || K < kQuantStep) return best;   // (the large tiles need a whole step)
-    auto big_time = [&](int mt, int tile_rows, float step, int tile_cols = BN) {
-        const int64_t per_cu = ceil_div(xcd_split(mt, ceil_div(N, tile_cols), wg).tiles, wg);
-        const float mem = (float(mt) * tile_rows * K + float(N) * K + 4.f * mt * tile_rows * N) / kMemory;
-        return kStart + std::max(per_cu * (nk * step + kBigEpilogue), mem);
-    };
-    if (n_mt == ceil_div(M, BM)) {   // (a list must name every tile: it counts in 256 rows)
-        consider(big_time(ceil_div(M, 192), 192, kStep192), Choice{Choice::k192x256, 0, 1, 0});
-        consider(big_time(ceil_div(M, 192), 192, kStepSquare192, 192), Choice{Choice::k192x192, 0, 1, 0});
-    }
-    consider(big_time(n_mt, BM, kBigStep), Choice{Choice::k256x256, 0, 1, 0});
-    // whole rounds of 256 x 256 tiles and the other rows on small ones; a split has to promise 5%
-    const int64_t rounds = int64_t(n_mt) * tiles_n / (8 * wg);
-    for (int64_t r = rounds; r > 0 && r >= rounds - 1; --r) {
-        const int big = static_cast<int>(r * 8 * wg / tiles_n), rest = rows - big * BM;
-        if (big <= 0 || rest <= 0) continue;
-        for (int t = 0; t < kQuantTiles; ++t)
-            consider((big_time(big, BM, kBigStep) + tile_time(t, rest, 1)) * 1.05f, Choice{Choice::kTile, t, 1, big});
-    }
-    return best;
-}
-
 template <int EPI, typename TO>
 void gemm(QuantGemm g, hipStream_t s) {
     if (g.M <= BM) g.mtile_m0 = nullptr;   // (a list of one tile then, which is all of M)
-    const int n_mt = g.mtile_m0 ? g.n_mtiles : ceil_div(g.M, BM);
-    const Choice c = choose(g.M, g.N, g.K, g.mtile_m0 ? n_mt : -1);
-    if (c.kind == Choice::kFew) return quant_gemm_few(EPI, sizeof(TO) == 4, c.tile, g, s);
-    if (c.kind == Choice::k256x256) return launch<EPI, TO, 8, 8>(g, n_mt, s);
-    if (c.kind == Choice::k192x256 || c.kind == Choice::k192x192) {
+    const int n_mt = g.mtile_m0 ? g.n_mtiles : quant_div(g.M, BM);
+    const QuantChoice c = quant_choose(g.M, g.N, g.K, g.mtile_m0 ? n_mt : -1, cu_count() / 8);
+    if (c.kind == QuantChoice::kFew) return quant_gemm_few(EPI, sizeof(TO) == 4, c.tile, g, s);
+    if (c.kind == QuantChoice::k256x256) return launch<EPI, TO, 8, 8>(g, n_mt, s);
+    if (c.kind == QuantChoice::k192x256 || c.kind == QuantChoice::k192x192) {
         g.mtile_m0 = nullptr;   // (it names every tile)
-        return c.kind == Choice::k192x256 ? launch<EPI, TO, 6, 8>(g, ceil_div(g.M, 192), s)
-                                          : launch<EPI, TO, 6, 6>(g, ceil_div(g.M, 192), s);
+        return c.kind == QuantChoice::k192x256 ? launch<EPI, TO, 6, 8>(g, quant_div(g.M, 192), s)
+                                          : launch<EPI, TO, 6, 6>(g, quant_div(g.M, 192), s);
     }
     if (c.big > 0) launch<EPI, TO, 8, 8>(g, c.big, s);
     quant_gemm_tiles(EPI, sizeof(TO) == 4, c.tile, g, c.big, n_mt - c.big, c.splits, s);
@@ -458,8 +355,8 @@ void gemm(QuantGemm g, hipStream_t s) {
 
 size_t quant_gemm_workspace(int M, int N, int K) {
     if (M == 0) return 0;
-    const Choice c = choose(M, N, K, -1);   // (a row-tile list is never split)
-    return c.kind == Choice::kTile && c.splits > 1 ? size_t(c.splits) * M * N * sizeof(int32_t) : 0;
+    const QuantChoice c = quant_choose(M, N, K, -1, cu_count() / 8);   // (a row-tile list is never split)
+    return c.kind == QuantChoice::kTile && c.splits > 1 ? size_t(c.splits) * M * N * sizeof(int32_t) : 0;
 }
 
 void quant_gemm(int epi, bool out_f32, const QuantGemm& g, hipStream_t s) {
