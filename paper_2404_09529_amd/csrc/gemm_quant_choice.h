@@ -9,6 +9,7 @@ constexpr int kQuantStep = 128;       // bytes (= values) of K in a step: whole 
 namespace ppk {
 
 constexpr int kQuantFewRows = 64;   // most rows of the kernel for few rows
+constexpr int quant_few_waves(int blocks) { return blocks == 4 ? 4 : 8; }   // of a workgroup of `blocks` column blocks
 
 // Tiles of the kernel for medium batches.
 constexpr int kQuantTiles = 5;
@@ -80,6 +81,7 @@ inline QuantChoice quant_choose(int M, int N, int K, int n_mt, int wg) {
         for (int blocks : {1, 2, 4}) {
             if (blocks == 4 && row_blocks > 1) continue;   // (the registers)
             const int wgs = quant_div(N, 16 * blocks), rounds = quant_div(wgs, 8 * wg);
+            if (int64_t(wgs) * 64 * quant_few_waves(blocks) > UINT32_MAX) continue;   // (more than a launch holds)
             const float cu = rounds * (kFewRound + 16.f * (blocks + row_blocks) * K / kFewCu);
             const float mem = bytes / (blocks == 4 ? kFewWeights4 : kFewWeights) + float(wgs) * rows * K / kFewShared;
             consider(kFewStart + std::max(cu, mem), QuantChoice{QuantChoice::kFew, blocks, 1, 0});

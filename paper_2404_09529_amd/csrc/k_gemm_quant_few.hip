@@ -107,20 +107,21 @@ __global__ __launch_bounds__(64 * NW) void gemm_few_kernel(ppk::QuantGemm q) {
     }
 }
 
-template <int EPI, typename TO, int NB, int MB, int NW>
+template <int EPI, typename TO, int NB, int MB>
 void launch(const ppk::QuantGemm& g, hipStream_t s) {
+    constexpr int NW = ppk::quant_few_waves(NB);
     gemm_few_kernel<EPI, TO, NB, MB, NW><<<(g.N + 16 * NB - 1) / (16 * NB), 64 * NW, 0, s>>>(g);
 }
 
 template <int EPI, typename TO, int MB>
 void columns(int blocks, const ppk::QuantGemm& g, hipStream_t s) {
     if constexpr (EPI != ppk::kSwiGLU) {   // (its gate and up blocks go together)
-        if (blocks == 1) return launch<EPI, TO, 1, MB, 8>(g, s);
+        if (blocks == 1) return launch<EPI, TO, 1, MB>(g, s);
     }
     if constexpr (MB == 1) {
-        if (blocks == 4) return launch<EPI, TO, 4, MB, 4>(g, s);
+        if (blocks == 4) return launch<EPI, TO, 4, MB>(g, s);
     }
-    launch<EPI, TO, 2, MB, 8>(g, s);
+    launch<EPI, TO, 2, MB>(g, s);
 }
 
 template <int EPI, typename TO>

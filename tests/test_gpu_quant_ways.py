@@ -128,3 +128,52 @@ def test_rows(way, epi, dtype):
 def test_row_tile_list(way, epi, dtype):
     rows, capacity, length, N, K = LISTS[way]
     run(rows * capacity, N, K, epi, dtype, list_plan(rows, capacity, length))
+
+
+@pytest.mark.parametrize("epi,dtype", [(pp.PP_EPI_STORE, "bf16"), (pp.PP_EPI_SWIGLU, "bf16"), (pp.PP_EPI_RESIDUAL, "f32")])
+@pytest.mark.parametrize("M,N,K", [(17, 2 ** 28 - 32, 16), (17, 2 ** 28, 16), (64, 2 ** 28 + 32, 16), (1, 2 ** 30, 16),
+                                   (3, 2 ** 31 - 512, 16)])
+def test_very_many_columns(M, N, K, epi, dtype):
+    """Up to the most columns there may be: the weights repeat, so the columns must.  (Fewer columns are compared
+    with float64 above; which kernel takes them does not change a bit.)"""
+    code, t = DT[dtype]
+    swiglu = epi == pp.PP_EPI_SWIGLU
+    period = 4096 + 96
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    a = torch.randint(-127, 128, (M, K), generator=g, dtype=torch.int8, device="cuda")
+    b1 = torch.randint(-127, 128, (period, K), generator=g, dtype=torch.int8, device="cuda")
+    sa, sb1 = torch.rand(M, generator=g, device="cuda") / 100, torch.rand(period, generator=g, device="cuda") / 100
+    times = -(-N // period)
+    b, sb = b1.repeat(times, 1), sb1.repeat(times)
+    cols, period_c = (N // 2, period // 2) if swiglu else (N, period)
+    want = torch.ones((M, period_c), dtype=t, device="cuda")
+    pp.pp_gemm_quant(code, epi, a, K, sa, b1, K, sb1, want, period_c, M, period, K)
+    c = torch.ones((M, cols), dtype=t, device="cuda")
+    need = pp.pp_gemm_quant_workspace_size(M, N, K)
+    pp.pp_gemm_quant(code, epi, a, K, sa, b, K, sb, c, cols, M, N, K,
+                     torch.empty(need, dtype=torch.uint8, device="cuda") if need else None)
+    whole = cols // period_c
+    for m in range(M):
+        assert bool((c[m, :whole * period_c].view(whole, period_c) == want[m]).all())
+        assert torch.equal(c[m, whole * period_c:], want[m, :cols - whole * period_c])
+
+
+def test_very_many_rows():
+    """The most rows there may be, on as few columns: the rows repeat too."""
+    M, N, K, period = 2 ** 31 - 512, 16, 16, 4096 + 96
+    g = torch.Generator(device="cuda").manual_seed(9)
+    a1 = torch.randint(-127, 128, (period, K), generator=g, dtype=torch.int8, device="cuda")
+    b = torch.randint(-127, 128, (N, K), generator=g, dtype=torch.int8, device="cuda")
+    sa1, sb = torch.rand(period, generator=g, device="cuda") / 100, torch.rand(N, generator=g, device="cuda") / 100
+    want = torch.empty((period, N), dtype=torch.bfloat16, device="cuda")
+    pp.pp_gemm_quant(pp.PP_BF16, pp.PP_EPI_STORE, a1, K, sa1, b, K, sb, want, N, period, N, K)
+    times = -(-M // period)
+    a, sa = a1.repeat(times, 1), sa1.repeat(times)
+    c = torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    assert pp.pp_gemm_quant_workspace_size(M, N, K) == 0
+    pp.pp_gemm_quant(pp.PP_BF16, pp.PP_EPI_STORE, a, K, sa, b, K, sb, c, N, M, N, K)
+    whole, step = M // period, 50000
+    for i in range(0, whole, step):
+        n = min(step, whole - i)
+        assert bool((c[i * period:(i + n) * period].view(n, period, N) == want).all())
+    assert torch.equal(c[whole * period:], want[:M - whole * period])

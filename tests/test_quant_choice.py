@@ -70,3 +70,18 @@ def test_no_other_way_is_common(choose):
         w = way(c, r)
         seen[w] = seen.get(w, 0) + 1
     assert {w for w, n in seen.items() if n >= 10} <= {*W.ROWS, *W.LISTS}
+
+
+def test_few_rows_fit_a_launch(choose):
+    """A launch holds fewer than 2^32 threads: the kernel for few rows takes no columns past that."""
+    rng = random.Random(4)
+    calls = [(M, N, K, -1) for M in (1, 16, 17, 32, 33, 64) for K in (16, 64, 128, 1024, 131056)
+             for N in (2 ** 27, 2 ** 28 - 32, 2 ** 28, 2 ** 29, 2 ** 30 - 64, 2 ** 30, 2 ** 31 - 512)]
+    calls += [(rng.randint(1, 64), 16 * rng.randint(2 ** 22, 2 ** 27 - 32), 16 * int(2 ** rng.uniform(0, 8)), -1)
+              for _ in range(20000)]
+    few = 0
+    for (M, N, K, _), (kind, blocks, _, _) in zip(calls, choose(calls)):
+        if kind == 0:
+            few += 1
+            assert -(-N // (16 * blocks)) * (256 if blocks == 4 else 512) < 2 ** 32, (M, N, K)
+    assert few > 0
