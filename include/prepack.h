@@ -327,7 +327,8 @@ pp_status pp_dequantize_rows(int32_t dtype, const int8_t* q, int64_t ldq, const 
  * is NULL), y[r] = x[r] / sqrt(mean(x[r]^2) + eps) * gain, and q[r], scale[r] the codes of y[r], which is
  * not itself stored.  x [rows, d] float32, updated in place; add [rows, d] in dtype (the output of a
  * projection; not overlapping x); gain [d] float32; q [rows, d]; scale [rows] float32.  d % 16 == 0; x, add,
- * gain and q 16-byte aligned.  The sum of squares is float32, as pp_rmsnorm's.
+ * gain and q 16-byte aligned.  The sum of squares is float32, as pp_rmsnorm's (float64 over the sums of
+ * four in rows of more than 16,384 values).
  * Errors: PP_ERR_INVALID_ARG (NULL, negative count, eps < 0), PP_ERR_UNSUPPORTED (d or an address that is
  *         no multiple of 16), PP_ERR_HIP. */
 pp_status pp_rmsnorm_quant(int32_t dtype, float* x, const void* add, const float* gain, int32_t rows, int32_t d,

@@ -70,10 +70,12 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
 template <int W>
 constexpr int kBlock = kWave * W > kThreads ? kWave * W : kThreads;
 
-// Over the W wavefronts of a row (W = 1: each wavefront of the workgroup has a row of its own).
-template <int W>
-__device__ __forceinline__ float row_sum(float v, float* lds) {
-    v = wave_sum(v);
+// Over the W wavefronts of a row (W = 1: each wavefront of the workgroup has a row of its own); T: float
+// or double.
+template <int W, typename T>
+__device__ __forceinline__ T row_sum(T v, T* lds) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
     if constexpr (W > 1) {
         if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
         __syncthreads();
@@ -199,19 +201,20 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quant_kernel(float* __restri
 
 // Rows too long for the registers: one workgroup each, a thread's four values at a time, read three times
 // (a thread reads again what it wrote itself; 4096 rows of 28,672 values, bf16 residual: 335 us,
-// 3.9 TB/s).
+// 3.9 TB/s).  Four squares are added in float32 and their sums in float64: a thread has up to 2^23
+// squares, and with float32 sums the scale of 4,000,016 equal values was off by 8e-5 of itself (as fast).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rmsnorm_quant_long_kernel(float* __restrict__ x, const T* __restrict__ add,
                                                                       const float* __restrict__ g, int rows, int d,
                                                                       float eps, int8_t* __restrict__ q,
                                                                       float* __restrict__ scale) {
-    __shared__ float sums[kThreads / kWave];
+    __shared__ double sums[kThreads / kWave];
     __shared__ uint32_t tops[kThreads / kWave];
     const int64_t row = my_row<kThreads / kWave>();
     if (row >= rows) return;
     float* xr = x + row * d;
     const T* ar = add ? add + row * d : nullptr;
-    float ss = 0.f;
+    double ss = 0.0;
 #pragma unroll 4
     for (int64_t e = 4 * threadIdx.x; e < d; e += 4 * kThreads) {
         f32x4 v = load4(xr + e);
@@ -219,11 +222,10 @@ __global__ __launch_bounds__(kThreads) void rmsnorm_quant_long_kernel(float* __r
             v += load4(ar + e);
             *reinterpret_cast<f32x4*>(xr + e) = v;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ss += v[i] * v[i];
+        ss += (v[0] * v[0] + v[1] * v[1]) + (v[2] * v[2] + v[3] * v[3]);
     }
     ss = row_sum<kThreads / kWave>(ss, sums);
-    const float r = rsqrtf(ss / static_cast<float>(d) + eps);
+    const float r = rsqrtf(static_cast<float>(ss / d) + eps);
     uint32_t top = 0;
 #pragma unroll 4
     for (int64_t e = 4 * threadIdx.x; e < d; e += 4 * kThreads) {
