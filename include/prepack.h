@@ -301,7 +301,10 @@ pp_status pp_final_norm_unpack(const float* x, const float* gain, int32_t d, flo
  * bits with a scale for each row (token), weights in 8 bits with a scale for each row (output
  * channel).  A value is its code times the scale of its row, codes are -127 .. 127, and a layer's
  * projections are pp_rmsnorm_quant or pp_quantize_rows followed by pp_gemm_quant; weights take
- * pp_quantize_rows once, when they are loaded.  Same conventions as the single steps.
+ * pp_quantize_rows once, when they are loaded.  Same conventions as the single steps.  A prefill layer
+ * is complete with pp_rope, pp_kv_scatter and pp_attention; for a decode step there is no single step that
+ * appends to the caches or attends from one token, and pp_prefill, pp_decode_step and pp_generate take no 8-bit
+ * weights.
  *
  * The code of a row y of d values: scale = max|y| * (1/127) (the float32 product with the float32 1/127),
  * code = y / scale (the float32 quotient) rounded to the nearest integer, ties to even.  A row of zeros, or

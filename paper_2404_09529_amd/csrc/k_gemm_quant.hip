@@ -11,7 +11,7 @@
 // each), two in flight while a step is read; the workgroup's tiles are one stream of steps, whose loads cross
 // tile boundaries; persistent, one workgroup per CU, every XCD on a compact block of tiles.
 //
-// What bounds it: 27,721 rows, N 22016, K 4096 with SwiGLU take 1.84 to 1.89 ms, 2.65 to 2.72 POP/s (a large int8 product of
+// What bounds it: 27,721 rows, N 22016, K 4096 with SwiGLU take 1.85 to 1.89 ms, 2.65 to 2.70 POP/s (a large int8 product of
 // the vendor's library 2.43); the matrix cores are 67% busy at 1.93 GHz.  The MFMAs alone reach 3.9 POP/s on
 // random codes and 4.75 on zeros: power holds the clock.  A step takes 1.54 us, 1.17 without the
 // loads of operands (zeros: 1.21 and 1.12); with every operand in L2 the call would be 4% faster.  One

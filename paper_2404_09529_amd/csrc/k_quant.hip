@@ -3,12 +3,14 @@
 //
 // scale = max|y| * (1 / 127), code = round(y / scale).  Both need the whole row before the first code
 // is written, so a row stays in registers between its one read and its one write: memory bounds
-// both kernels (27,721 x 4096: quantize_rows of bf16 59 us, 5.8 TB/s; rmsnorm_quant with a bf16 residual 217 us,
-// 5.7 TB/s; and dequantize_rows to bf16 57 to 70 us, 4.9 to 6.0 TB/s).
+// both kernels (27,721 x 4096, back to back: quantize_rows of bf16 59 us, 5.8 TB/s; rmsnorm_quant with a bf16 residual
+// 218, 5.7 TB/s; dequantize_rows to bf16 62, 5.5 TB/s, to float32 144, 3.9 TB/s; quantize_rows behind a kernel that wrote 227 MB
+// 74 us, 4.6 TB/s).
 //
 // A row of up to four 16-byte chunks per lane is one wavefront's, a longer one a workgroup's: 20,000 rows
 // of 688 bf16 values 9.3 us and 19.4, of 4096 46.2 and 43.5.  Six chunks a thread beside eight, for the
-// registers: rmsnorm_quant of 3951 x 5120 20.0 -> 19.0 us, 300 x 5120 5.7 -> 5.1, 27,721 x 5120 1% slower.
+// registers: rmsnorm_quant of 300 x 5120 5.6 -> 5.2 us, 3951 x 5120 21.4 -> 21.1, 27,721 x 5120 127 -> 125 (with a bf16
+// residual 279 -> 282).
 // quantize_rows has workgroups of 16 wavefronts too, for the rows of a wide layer's second weight (up to
 // 65,536 float32 or 131,072 bf16 values): 4096 x 28,672 float32 106 us, 5.5 TB/s, instead of 156 with two reads.
 #include "device.h"
@@ -46,9 +48,9 @@ __device__ __forceinline__ RowCode row_code(uint32_t top) {
 }
 
 // Codes of four values in the bytes of a word.  The quotient is the product with the reciprocal and
-// one correction by its remainder, so that values next to a border fall on the division's side.  Adding 1.5 * 2^23 leaves the nearest integer (ties
-// to even) in the low bits of the sum, as two's complement; the clamp matters only to scales that
-// are themselves denormal.
+// one correction by its remainder, so that values next to a border fall on the division's side (equal to it at
+// 1.9 billion pairs within two float32 steps of a border).  Adding 1.5 * 2^23 leaves the nearest integer (ties to even) in the
+// low bits of the sum, as two's complement; the clamp matters only to scales that are themselves denormal.
 __device__ __forceinline__ uint32_t codes4(const float* v, const RowCode& c) {
     uint32_t b[4];
 #pragma unroll
