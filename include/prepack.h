@@ -505,6 +505,104 @@ pp_status pp_generate(const pp_config* cfg, const pp_weights* w, const pp_gen_dl
                       void* gen_k, void* gen_v, void* workspace, size_t workspace_bytes, int32_t* tokens,
                       void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Serving from a paged key-value cache, for callers that assemble their own decode loop: sequences that
+ * come, grow and go keep their keys and values in pages of a common pool, in the model's type or in 8-bit
+ * codes.  A layer of a decode step is pp_gemm (or pp_gemm_quant) for QKV, pp_paged_append, pp_paged_attention and the
+ * other projections; a prefill's caches enter the pool with pp_paged_write.  Same conventions as the single
+ * steps.  Of the config only the heads, head_dim, dtype and (pp_paged_append) rope_theta matter; it has to be one
+ * that pp_prefill takes.
+ * ---------------------------------------------------------------------------------------- */
+
+/* What a page holds.  PP_KV_F32 and PP_KV_BF16: the config's own dtype.  PP_KV_I8: the keys (and the values)
+ * of one token and one key/value head are a row of D 8-bit codes with a float32 scale, as in pp_quantize_rows (a head with
+ * a NaN or an infinity gets scale NaN); with a config of either dtype. */
+typedef enum pp_kv_type { PP_KV_F32 = 0, PP_KV_BF16 = 1, PP_KV_I8 = 2 } pp_kv_type;
+
+/* The pages of one layer.  Token `pos` of sequence i (0 <= i < k) is row pos % page_size of page
+ * page_table[i * max_pages + pos / page_size].  A page that is none of the pool's (below 0 or from n_pages on), and a
+ * position past the table's end, hold nothing: what would be written there is dropped, and the attention leaves
+ * such keys out.  page_size is a power of two (1: every row a page of its own); n_pages >= 1, and the pool has at most
+ * 2^31 - 1 rows.  Sequences may share pages that none of them writes.
+ *   page_table        device int32 [k][max_pages]
+ *   k_pages, v_pages  device [n_pages][page_size][Hkv * D], 16-byte aligned
+ *   k_scale, v_scale  device float32 [n_pages][page_size][Hkv] (PP_KV_I8; else not read) */
+typedef struct pp_paged_cache {
+    int32_t kv_type, k, page_size, max_pages, n_pages;
+    const int32_t* page_table;
+    void* k_pages;
+    void* v_pages;
+    float* k_scale;
+    float* v_scale;
+} pp_paged_cache;
+
+/* Stores rows of keys (post-RoPE) and values: row r is token pos[r] of sequence seq[r], for instance a
+ * prefill's caches with r = prompt_kv_off[i] + j, seq[r] the sequence that prompt i became and pos[r] = j.
+ * keys, values [rows, Hkv D] in the config's dtype (row strides ldk, ldv elements); seq, pos device int32 [rows].  A row
+ * whose seq is outside [0, k), or that has no place, is skipped.  Two rows of a call have different places.
+ * ldk and ldv multiples of 8, keys and values 16-byte aligned.
+ * Errors: PP_ERR_INVALID_ARG (NULL, negative count, a stride below Hkv D, bad config or cache), PP_ERR_UNSUPPORTED (a
+ *         config or page type outside the above, a stride or address that is not aligned), PP_ERR_HIP. */
+pp_status pp_paged_write(const pp_config* cfg, const pp_paged_cache* cache, const int32_t* seq, const int32_t* pos,
+                         int32_t rows, const void* keys, int64_t ldk, const void* values, int64_t ldv, void* stream);
+
+/* And back: keys and values of the tokens (seq[r], pos[r]) in the config's dtype (8-bit: code times scale, rounded
+ * once).  Rows that pp_paged_write would skip are left as they were.  Buffers, sizes and errors as pp_paged_write. */
+pp_status pp_paged_read(const pp_config* cfg, const pp_paged_cache* cache, const int32_t* seq, const int32_t* pos,
+                        int32_t rows, void* keys, int64_t ldk, void* values, int64_t ldv, void* stream);
+
+/* The newest token of every sequence: lens[i] counts sequence i's tokens, that one included.  Row i of qkv [k,
+ * (H + 2 Hkv) D] (row stride ldqkv) is its projection; its query and key heads are rotated (rotate-half) by position
+ * lens[i] - 1, the query goes to row i of q_out [k, H D] (row stride ldq), key and value to the token's place in the cache.
+ * Where lens[i] <= 0 nothing is read or written.  q_out may be qkv itself with ldq == ldqkv; otherwise they do
+ * not overlap.  The angle's cosine and sine are pp_rope's; the products are summed in float64 and rounded to float32, then
+ * to dtype, or (8-bit keys) to codes.  lens device int32 [k]; qkv, q_out in dtype, 16-byte aligned, strides multiples of 8.
+ * Errors as pp_paged_write. */
+pp_status pp_paged_append(const pp_config* cfg, const pp_paged_cache* cache, const int32_t* lens, const void* qkv,
+                          int64_t ldqkv, void* q_out, int64_t ldq, void* stream);
+
+/* Bytes of device workspace pp_paged_attention needs (they depend on the heads and cache->k alone).
+ * Errors: as pp_paged_attention's checks of cfg and of the cache's sizes. */
+pp_status pp_paged_attention_workspace_size(const pp_config* cfg, const pp_paged_cache* cache, size_t* bytes);
+
+/* Attention of one query row per sequence over its first lens[i] keys: out[i] = softmax(q k^T / sqrt(D)) v, query
+ * head h reading key/value head h / (H / Hkv).  Where no key is left (lens[i] <= 0, or no page of the sequence is one of
+ * the pool's) the row is zeros; lens[i] past the table's end counts what the table reaches.
+ * q [k, H D] in dtype (row stride ldq, a multiple of 8; 16-byte aligned), post-RoPE (pp_paged_append's q_out); out [k, H D]
+ * in dtype, 16-byte aligned, no overlap with q.  workspace: >= pp_paged_attention_workspace_size bytes, 256-byte aligned, not used by
+ * two calls at a time; its contents do not matter.  Scores, softmax and sums are float32; bf16 results are rounded
+ * once.  Deterministic; how the keys are split, and with it the last bits of float32 results, depends on all lengths.
+ * Errors: as pp_paged_write, PP_ERR_INVALID_ARG (misaligned workspace), PP_ERR_BUFFER_TOO_SMALL (workspace). */
+pp_status pp_paged_attention(const pp_config* cfg, const pp_paged_cache* cache, const int32_t* lens, const void* q,
+                             int64_t ldq, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Sampling: a token of every row of logits (pp_first_token's or pp_decode_step's), where those calls choose
+ * greedily.
+ * ---------------------------------------------------------------------------------------- */
+
+/* Bytes of device workspace pp_sample needs (0: none, and the workspace may be NULL).
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (as pp_sample). */
+pp_status pp_sample_workspace_size(int32_t k, int32_t vocab, size_t* bytes);
+
+/* tokens[i] drawn from row i of logits (float32 [k, vocab], row stride ldl) with the given random number u[i] in
+ * [0, 1).  The row's ids are put in order, largest logit first, ties lowest id first, and x_1, x_2 .. are their
+ * logits; w_j = exp((x_j - x_1) / T).  Kept are the first top_k; of these the shortest beginning whose sum reaches top_p
+ * times their sum; of these the ones with w_j >= min_p; one at least.  The token is the first whose sum w_1 + .. + w_j exceeds
+ * u times the sum of the kept; prob (NULL: not wanted) its share of that sum.
+ *   temperature, top_k, top_p, min_p  device [k], float32 but top_k int32; NULL: 1, and no limit.
+ *   T <= 0 (or NaN): the token that pp_first_token chooses, prob 1 (-1 and 0 where every logit is NaN).
+ *   top_k <= 0, top_p >= 1 and min_p <= 0 (or NaN) are no limit; u below 0 or NaN counts as 0, u >= 1 gives the last kept id.
+ *   NaN logits are never chosen, nor is -inf with T > 0 (no other logit: token -1, prob 0); ids of +inf share the sum evenly.
+ *   tokens device int32 [k]; prob device float32 [k]; vocab up to 2^20.
+ * w is computed in float64 and summed exactly, as a multiple of 2^-44 (ids below 2^-45 of the likeliest are never chosen).
+ * workspace: >= pp_sample_workspace_size bytes, 256-byte aligned, not used by two calls at a time.  Deterministic.
+ * Errors: PP_ERR_INVALID_ARG (NULL logits, u or tokens, k < 0, vocab <= 0, ldl < vocab, misaligned workspace),
+ *         PP_ERR_UNSUPPORTED (vocab), PP_ERR_BUFFER_TOO_SMALL (workspace), PP_ERR_HIP. */
+pp_status pp_sample(const float* logits, int64_t ldl, int32_t k, int32_t vocab, const float* temperature,
+                    const int32_t* top_k, const float* top_p, const float* min_p, const float* u, void* workspace,
+                    size_t workspace_bytes, int32_t* tokens, float* prob, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -61,3 +61,10 @@ __device__ __forceinline__ float rope_hi(float x, float y, float c, float s) { r
 // The upper half as pp_rope and the float32 QKV epilogue form it: a float32 prefill's caches are
 // those of pp_gemm, pp_rope and pp_kv_scatter bit for bit.
 __device__ __forceinline__ float rope_hi_step(float x, float y, float c, float s) { return fmaf(y, c, x * s); }
+
+// cos and sin of position * theta^(-2i/D), evaluated in float64.
+__device__ __forceinline__ float2 rope_entry(int64_t position, int i, int D, double theta) {
+    const double inv_freq = pow(theta, -2.0 * i / static_cast<double>(D));
+    const double a = static_cast<double>(position) * inv_freq;
+    return make_float2(static_cast<float>(cos(a)), static_cast<float>(sin(a)));
+}

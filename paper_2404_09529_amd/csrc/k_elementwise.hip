@@ -18,12 +18,6 @@ template <typename T>
 T* at(void* p) { return static_cast<T*>(p); }
 
 // ------------------------------------------------------------------------------- RoPE table
-__device__ __forceinline__ float2 rope_entry(int64_t position, int i, int D, double theta) {
-    const double inv_freq = pow(theta, -2.0 * i / static_cast<double>(D));
-    const double a = static_cast<double>(position) * inv_freq;
-    return make_float2(static_cast<float>(cos(a)), static_cast<float>(sin(a)));
-}
-
 __global__ void rope_table_kernel(float2* __restrict__ table, int64_t n, int half, int D, double theta) {
     const int64_t idx = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
     if (idx >= n) return;

@@ -223,4 +223,42 @@ void decode_gemm(int epi, const void* A, int64_t lda, int k, const void* W, int6
 // The number of K splits decode_gemm's kResidual leaves for k <= 16 rows of an N x K product.
 int decode_gemm_splits(int k, int N, int K);
 
+// ---------------------------------------------------------------------- paged cache
+// A pp_paged_cache with its page size as a shift, and the heads.
+struct PagedCache {
+    int kv_type, k, shift, max_pages, n_pages;
+    const int32_t* table;
+    void *kp, *vp;
+    float *ks, *vs;
+    int H, Hkv, D;
+};
+// Rows (seq[r], pos[r]) of keys and values into the pages, and back (pp_paged_write, pp_paged_read).
+void paged_write(int dtype, const PagedCache& c, const int32_t* seq, const int32_t* pos, int rows, const void* k,
+                 int64_t ldk, const void* v, int64_t ldv, hipStream_t s);
+void paged_read(int dtype, const PagedCache& c, const int32_t* seq, const int32_t* pos, int rows, void* k, int64_t ldk,
+                void* v, int64_t ldv, hipStream_t s);
+// The newest token of every sequence, rotated and stored (pp_paged_append).
+void paged_append(int dtype, const PagedCache& c, const int32_t* lens, const void* qkv, int64_t ldqkv, void* q_out,
+                  int64_t ldq, float theta, hipStream_t s);
+// Attention of one row per sequence (pp_paged_attention); part: paged_attention_workspace(...) bytes.
+size_t paged_attention_workspace(int k, int H, int Hkv, int D);
+void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const void* q, int64_t ldq, void* out,
+                     void* part, hipStream_t s);
+
+// ---------------------------------------------------------------------- sampling
+struct Sample {
+    const float* logits;
+    int64_t ldl;
+    int k, vocab;
+    const float* temperature;   // the four: null, or [k]
+    const int32_t* top_k;
+    const float *top_p, *min_p;
+    const float* u;
+    int32_t* tokens;
+    float* prob;   // or null
+    void* ws;      // sample_workspace(k, vocab) bytes
+};
+size_t sample_workspace(int k, int vocab);
+void sample(const Sample& a, hipStream_t s);
+
 }  // namespace ppk

@@ -22,6 +22,7 @@ LIB_PATH = os.path.join(_HERE, "libprepack.so")
 PP_OK, PP_ERR_INVALID_ARG, PP_ERR_TOO_LONG, PP_ERR_BUFFER_TOO_SMALL, PP_ERR_UNSUPPORTED, PP_ERR_HIP = 0, -1, -2, -3, -4, -5
 PP_F32, PP_BF16 = 0, 1
 PP_EPI_STORE, PP_EPI_RESIDUAL, PP_EPI_SWIGLU = 0, 1, 2
+PP_KV_F32, PP_KV_BF16, PP_KV_I8 = 0, 1, 2
 PP_QTILE = 128
 PP_MTILE = 256
 
@@ -85,6 +86,13 @@ class PPGenDLayout(ctypes.Structure):
                 ("pos0", ctypes.c_void_p), ("gen_off", ctypes.c_void_p)]
 
 
+class PPPagedCache(ctypes.Structure):
+    _fields_ = [("kv_type", ctypes.c_int32), ("k", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_table", ctypes.c_void_p),
+                ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -131,13 +139,22 @@ def lib() -> ctypes.CDLL:
         L.pp_decode_workspace_size.argtypes = [cfgp, gdp, ctypes.POINTER(ctypes.c_size_t)]
         L.pp_decode_step.argtypes = [cfgp, wp, gdp, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp, vp]
         L.pp_generate.argtypes = [cfgp, wp, gdp, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp]
+        pcp, szp = ctypes.POINTER(PPPagedCache), ctypes.POINTER(ctypes.c_size_t)
+        L.pp_paged_write.argtypes = L.pp_paged_read.argtypes = [cfgp, pcp, vp, vp, i32, vp, i64, vp, i64, vp]
+        L.pp_paged_append.argtypes = [cfgp, pcp, vp, vp, i64, vp, i64, vp]
+        L.pp_paged_attention_workspace_size.argtypes = [cfgp, pcp, szp]
+        L.pp_paged_attention.argtypes = [cfgp, pcp, vp, vp, i64, vp, vp, ctypes.c_size_t, vp]
+        L.pp_sample_workspace_size.argtypes = [i32, i32, szp]
+        L.pp_sample.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, vp, vp]
         for name in ("pp_plan_bounds", "pp_pack", "pp_pack_padded", "pp_prefill_workspace_size", "pp_prefill",
                      "pp_embed", "pp_rmsnorm", "pp_gemm", "pp_rope", "pp_kv_scatter", "pp_attention",
                      "pp_final_norm_unpack", "pp_quantize_rows", "pp_dequantize_rows", "pp_rmsnorm_quant",
                      "pp_gemm_quant_workspace_size", "pp_gemm_quant",
                      "pp_first_token_workspace_size", "pp_first_token",
                      "pp_first_token_noalloc",
-                     "pp_gen_layout_make", "pp_decode_workspace_size", "pp_decode_step", "pp_generate"):
+                     "pp_gen_layout_make", "pp_decode_workspace_size", "pp_decode_step", "pp_generate",
+                     "pp_paged_write", "pp_paged_read", "pp_paged_append", "pp_paged_attention_workspace_size",
+                     "pp_paged_attention", "pp_sample_workspace_size", "pp_sample"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -389,6 +406,10 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
+def _nbytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
 def pp_embed(dtype: int, embed, vocab: int, d: int, tokens, dplan: DevicePlan, x, stream=None) -> None:
     _check(lib().pp_embed(dtype, _p(embed), vocab, d, _p(tokens), ctypes.byref(dplan.struct), _p(x),
                           _stream(stream)), "pp_embed")
@@ -632,3 +653,79 @@ class Generation:
     def replay(self):
         self.graph.replay()
         return self.tokens
+
+
+# ----------------------------------------------------------------------------- paged cache
+class PagedCache:
+    """One layer's pages (tensors of the caller's) plus the pp_paged_cache struct that points at them.
+
+    page_table int32 [k, max_pages]; k_pages, v_pages [n_pages, page_size, Hkv * D] in the model's type, or int8 with
+    k_scale, v_scale float32 [n_pages, page_size, Hkv] (kv_type PP_KV_I8).  The layers of a model share one table."""
+
+    def __init__(self, kv_type: int, page_table, k_pages, v_pages, k_scale=None, v_scale=None):
+        torch = _torch()
+        want = {PP_KV_F32: torch.float32, PP_KV_BF16: torch.bfloat16, PP_KV_I8: torch.int8}[kv_type]
+        n_pages, page_size, kvw = k_pages.shape
+        if k_pages.dtype != want or v_pages.dtype != want or v_pages.shape != k_pages.shape:
+            raise ValueError(f"k_pages and v_pages must be {want} of one shape")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2:
+            raise ValueError("page_table must be int32 [k, max_pages]")
+        tensors = [page_table, k_pages, v_pages]
+        if kv_type == PP_KV_I8:
+            for t in (k_scale, v_scale):
+                if t is None or t.dtype != torch.float32 or t.shape[:2] != k_pages.shape[:2] or kvw % t.shape[2]:
+                    raise ValueError("k_scale and v_scale must be float32 [n_pages, page_size, Hkv]")
+            tensors += [k_scale, v_scale]
+        if not all(t.is_contiguous() for t in tensors):
+            raise ValueError("page_table, pages and scales must be contiguous")
+        self.tensors = tensors
+        self.struct = PPPagedCache(kv_type=kv_type, k=page_table.shape[0], page_size=page_size,
+                                   max_pages=page_table.shape[1], n_pages=n_pages, page_table=_p(page_table),
+                                   k_pages=_p(k_pages), v_pages=_p(v_pages), k_scale=_p(k_scale), v_scale=_p(v_scale))
+
+
+def pp_paged_write(cfg: PPConfig, cache: PagedCache, seq, pos, rows: int, keys, ldk: int, values, ldv: int,
+                   stream=None) -> None:
+    """Rows of keys and values into the pages: row r is token pos[r] of sequence seq[r] (int32 device tensors)."""
+    _check(lib().pp_paged_write(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(seq), _p(pos), rows, _p(keys), ldk,
+                                _p(values), ldv, _stream(stream)), "pp_paged_write")
+
+
+def pp_paged_read(cfg: PPConfig, cache: PagedCache, seq, pos, rows: int, keys, ldk: int, values, ldv: int,
+                  stream=None) -> None:
+    """The keys and values of the tokens (seq[r], pos[r]) into dense rows."""
+    _check(lib().pp_paged_read(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(seq), _p(pos), rows, _p(keys), ldk,
+                               _p(values), ldv, _stream(stream)), "pp_paged_read")
+
+
+def pp_paged_append(cfg: PPConfig, cache: PagedCache, lens, qkv, ldqkv: int, q_out, ldq: int, stream=None) -> None:
+    """The newest token of every sequence (position lens[i] - 1): query and key rotated, key and value stored."""
+    _check(lib().pp_paged_append(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(lens), _p(qkv), ldqkv, _p(q_out),
+                                 ldq, _stream(stream)), "pp_paged_append")
+
+
+def pp_paged_attention_workspace_size(cfg: PPConfig, cache: PagedCache) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().pp_paged_attention_workspace_size(ctypes.byref(cfg), ctypes.byref(cache.struct), ctypes.byref(n)),
+           "pp_paged_attention_workspace_size")
+    return n.value
+
+
+def pp_paged_attention(cfg: PPConfig, cache: PagedCache, lens, q, ldq: int, out, workspace, stream=None) -> None:
+    """out [k, H D]: attention of one query row per sequence over its first lens[i] keys."""
+    _check(lib().pp_paged_attention(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(lens), _p(q), ldq, _p(out),
+                                    _p(workspace), _nbytes(workspace), _stream(stream)), "pp_paged_attention")
+
+
+# ----------------------------------------------------------------------------- sampling
+def pp_sample_workspace_size(k: int, vocab: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().pp_sample_workspace_size(k, vocab, ctypes.byref(n)), "pp_sample_workspace_size")
+    return n.value
+
+
+def pp_sample(logits, ldl: int, k: int, vocab: int, temperature, top_k, top_p, min_p, u, tokens, workspace=None,
+              prob=None, stream=None) -> None:
+    """tokens [k] int32 drawn from rows of logits with the random numbers u [k] (see include/prepack.h)."""
+    _check(lib().pp_sample(_p(logits), ldl, k, vocab, _p(temperature), _p(top_k), _p(top_p), _p(min_p), _p(u),
+                           _p(workspace), _nbytes(workspace), _p(tokens), _p(prob), _stream(stream)), "pp_sample")
