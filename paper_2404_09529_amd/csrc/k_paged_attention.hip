@@ -1,8 +1,27 @@
 // Attention of one query row per sequence over a paged cache: out = softmax(q k^T / sqrt(D)) v over the
 // first lens[i] keys of sequence i, in whatever pages they lie.
 //
-// One wavefront per (sequence, query head), keys in tiles of 64: lane j holds key j's score, one maximum and one sum
-// across the lanes per tile, then lane d accumulates dims d (and d + 64).
+// Every key and value is read once and used for the G = H / Hkv query heads that share it, so reading them bounds
+// the kernel.  The sequences are cut into units of whole 128-key tiles (paged.h); a workgroup has one unit of one
+// key/value head, its four wavefronts 32 keys of each tile, each with a softmax of its own (running maximum and
+// sum), joined through LDS at the end.  A sequence of one unit is written right away, the units of a longer one leave
+// (o, maximum, sum) for join_kernel.
+//
+// Nothing passes through LDS on the way: keys go from memory into the registers that the 16 x 16 matrix
+// instructions take them from.  S^T = K Q^T puts key 8 g + 4 t + r of a wavefront's 32 into row 4 g + r of score tile t,
+// so that lane group g (16 lanes) holds the scores of keys 8 g .. 8 g + 7, which is what it has to hold as the operand of
+// O^T = V^T P^T; a lane reads the same 16 (or 8, or 4) columns' part of those 8 rows of V, whole rows per 16 lanes.
+// The query heads are the instructions' columns; with fewer than 16 the rest are zeros (the matrix cores are idle
+// otherwise: a 32-key step of 16 KB takes them 256 cycles of the 6500 that a SIMD's share of the memory needs).
+//
+// bf16 operands hold what is exact in them: bf16 keys, values and queries, and 8-bit codes, whose scales multiply scores
+// and probabilities.  Probabilities (times a value's scale) are two bf16 terms, off by 2^-17, so that the result is as good
+// as its one rounding; with float32 queries over 8-bit pages queries and probabilities are three terms, all of float32's bits.
+// float32 pages take the float32 matrix instructions.
+#include <float.h>
+
+#include <utility>
+
 #include "device.h"
 #include "kernels.h"
 #include "paged.h"
@@ -10,84 +29,528 @@
 
 namespace {
 
-constexpr int kBlock = 256;
+constexpr int kBlock = 256, kSplitWaves = kBlock / kWave;
+constexpr int kStep = 32;   // keys of a wavefront per tile
+constexpr int kRows = 16;   // query heads of a workgroup
+static_assert(kSplitWaves * kStep == ppk::kPagedTile, "a tile is one step of a workgroup");
 
-__device__ __forceinline__ float value(float x) { return x; }
-__device__ __forceinline__ float value(bf16 x) { return static_cast<float>(x); }
-__device__ __forceinline__ float value(int8_t x) { return static_cast<float>(x); }
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-template <int D, typename T, typename P>
-__global__ __launch_bounds__(kBlock) void paged_attention_kernel(ppk::PagedCache c, const int32_t* __restrict__ lens,
-                                                                 const T* __restrict__ q, int64_t ldq,
-                                                                 T* __restrict__ out, float scale) {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t wid = int64_t(blockIdx.x) * (kBlock / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i = static_cast<int>(wid / c.H), h = static_cast<int>(wid % c.H), g = h / (c.H / c.Hkv);
-    if (i >= c.k) return;
-    const int n = ppk::paged_len(lens[i], ppk::paged_span(c.max_pages, c.shift));
-    const T* qr = q + i * ldq + int64_t(h) * D;
-    const P* K = static_cast<const P*>(c.kp) + int64_t(g) * D;
-    const P* V = static_cast<const P*>(c.vp) + int64_t(g) * D + lane;
-    const int64_t ld = int64_t(c.Hkv) * D;
-    float m = -INFINITY, l = 0.f, acc[E] = {};
-    bool any = false;
-    for (int j0 = 0; j0 < n; j0 += 64) {
-        const int j = j0 + lane;
-        const int row = j < n ? ppk::paged_row(c.table[int64_t(i) * c.max_pages + (j >> c.shift)], c.n_pages, j, c.shift) : -1;
-        float s = -INFINITY, vs = 1.f;
-        if (row >= 0) {
-            const P* k = K + row * ld;
-            float d4[4] = {0.f, 0.f, 0.f, 0.f};
-            for (int e = 0; e < D; e += 4)
+// f(0) .. f(N - 1) with constants for arguments.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+    each_of(f, std::make_integer_sequence<int, N>{});
+}
+
+// Lane E's value of every row of 16 lanes.
+template <int E>
+__device__ __forceinline__ int row_lane(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, 0x150 + E, 0xf, 0xf, true);
+}
+template <int E>
+__device__ __forceinline__ float row_lane(float x) {
+    return __int_as_float(row_lane<E>(__float_as_int(x)));
+}
+
+// Over the four lanes that are 16 apart.
+__device__ __forceinline__ float max16(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum16(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// x as N bf16 terms, the largest first.
+template <int N>
+__device__ __forceinline__ void terms(float x, bf16 (&t)[N]) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) d4[u] = fmaf(value(qr[e + u]), value(k[e + u]), d4[u]);
-            s = (d4[0] + d4[1]) + (d4[2] + d4[3]);
-            if constexpr (sizeof(P) == 1) {
-                s *= c.ks[int64_t(row) * c.Hkv + g];
-                vs = c.vs[int64_t(row) * c.Hkv + g];
-            }
-            s *= scale;
+    for (int i = 0; i < N; ++i) {
+        t[i] = static_cast<bf16>(x);
+        x -= static_cast<float>(t[i]);
+    }
+}
+
+__device__ __forceinline__ float code(uint32_t w, int i) { return static_cast<float>(static_cast<int8_t>(w >> (8 * i))); }
+
+// ------------------------------------------------------------------------------- the split
+struct Unit {
+    int seq, len, tile0, tile1, units;   // seq < 0: none
+};
+
+__device__ __forceinline__ int tiles_of(const int32_t* lens, int i, int k, int span) {
+    return i < k ? ppk::paged_tiles(ppk::paged_len(lens[i], span)) : 0;
+}
+
+__device__ __forceinline__ int unit_size(const int32_t* lens, int k, int span, int target) {
+    int64_t all = 0;
+    for (int i = threadIdx.x & 63; i < k; i += kWave) all += tiles_of(lens, i, k, span);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o, kWave);
+    return ppk::paged_unit(all, target);
+}
+
+__device__ __forceinline__ int scan_up(int x) {
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int y = __shfl_up(x, o, kWave);
+        if ((threadIdx.x & 63) >= o) x += y;
+    }
+    return x;
+}
+
+// Unit u of the split, by every wavefront for itself.
+__device__ __forceinline__ Unit find_unit(const int32_t* lens, int k, int span, int target, int u) {
+    const int unit = unit_size(lens, k, span, target), lane = threadIdx.x & 63;
+    int base = 0;
+    for (int i0 = 0; i0 < k; i0 += kWave) {
+        const int i = i0 + lane, len = i < k ? ppk::paged_len(lens[i], span) : 0, t = ppk::paged_tiles(len);
+        const int n = i < k ? ppk::paged_units(t, unit) : 0, end = base + scan_up(n);
+        const uint64_t here = __ballot(u < end && u >= end - n);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            const int first = u - __builtin_amdgcn_readlane(end - n, l), tiles = __builtin_amdgcn_readlane(t, l);
+            return {i0 + l, __builtin_amdgcn_readlane(len, l), first * unit, min(first * unit + unit, tiles),
+                    __builtin_amdgcn_readlane(n, l)};
         }
-        const uint64_t here = __ballot(row >= 0);
-        if (!here) continue;
-        any = true;
-        const float m_new = fmaxf(m, wave_max(s));
-        const float corr = m == m_new ? 1.f : expf(m - m_new);
-        // scores of -inf alone add nothing yet; if none follows, 0 / 0 is no number, as the formula has it
-        const float p = row < 0 || m_new == -INFINITY ? 0.f : expf(s - m_new);
-        l = l * corr + wave_sum(p);
-        m = m_new;
+        base = __builtin_amdgcn_readlane(end, kWave - 1);
+    }
+    return {-1, 0, 0, 0, 0};
+}
+
+// The first unit of sequence i, and how many it has.
+__device__ __forceinline__ int2 units_of(const int32_t* lens, int k, int span, int target, int i) {
+    const int unit = unit_size(lens, k, span, target), lane = threadIdx.x & 63;
+    int base = 0;
+    for (int i0 = 0;; i0 += kWave) {
+        const int n = i0 + lane < k ? ppk::paged_units(tiles_of(lens, i0 + lane, k, span), unit) : 0, end = base + scan_up(n);
+        if (i < i0 + kWave)
+            return make_int2(__builtin_amdgcn_readlane(end - n, i - i0), __builtin_amdgcn_readlane(n, i - i0));
+        base = __builtin_amdgcn_readlane(end, kWave - 1);
+    }
+}
+
+// ------------------------------------------------------------------------------- operands by type
+// A wavefront's 32 rows of K and V in registers, and the products with them.  Lane (g, ln) = (lane / 16, lane % 16).
+// kcol, vcol: byte offsets of this lane's part of a row of K and V.
+template <int D, typename T, typename P>
+struct Tile;
+
+// bf16 pages.  K operand of instruction (t, s): dims 32 s + 8 g .. + 7 of key 8 (ln / 4) + 4 t + ln % 4.  V: dims
+// 8 ln .. + 7 of the lane group's keys; instruction j takes dim 8 ln + j of all of them.
+template <int D>
+struct Tile<D, bf16, bf16> {
+    static constexpr int KS = D / 32, NJ = D / 16;
+    static_assert(D == 128, "a lane's part of a row is 16 bytes");
+    u32x4 k[2][KS], v[8];
+    struct Query {
+        bf16x8 f[KS];
+    };
+
+    static __device__ __forceinline__ int kcol(int g) { return 16 * g; }
+    static __device__ __forceinline__ int vcol(int ln) { return 16 * ln; }
+    static __device__ __forceinline__ int dim(int j, int row) { return 8 * row + j; }
+    static __device__ __forceinline__ void query(Query& q, const bf16* x, int g) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= corr;
-        const float pv = row < 0 ? 0.f : p * vs;
-        for (int t = 0; t < 64; ++t) {
-            const int r = __builtin_amdgcn_readlane(row, t);
-            if (r < 0) continue;
-            const float pt = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pv), t));
+        for (int s = 0; s < KS; ++s) q.f[s] = x ? *reinterpret_cast<const bf16x8*>(x + 32 * s + 8 * g) : bf16x8{};
+    }
+    __device__ __forceinline__ void load_k(int t, const char* p) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(pt, value(V[r * ld + 64 * e]), acc[e]);
+        for (int s = 0; s < KS; ++s) k[t][s] = *reinterpret_cast<const u32x4*>(p + 64 * s);
+    }
+    __device__ __forceinline__ void load_v(int e, const char* p) { v[e] = *reinterpret_cast<const u32x4*>(p); }
+    __device__ __forceinline__ void clear_v(int e) { v[e] = u32x4{}; }
+    __device__ __forceinline__ f32x4 scores(int t, const Query& q) const {
+        f32x4 s = {};
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[t][i]), q.f[i], s, 0, 0, 0);
+        return s;
+    }
+    __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&o)[NJ]) const {
+        bf16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            bf16 t[2];
+            terms(p[e], t);
+            hi[e] = t[0], lo[e] = t[1];
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            u32x4 f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                f[e] = __builtin_amdgcn_perm(v[2 * e + 1][j / 2], v[2 * e][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+            const bf16x8 a = __builtin_bit_cast(bf16x8, f);
+            o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, o[j], 0, 0, 0);
+            o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, o[j], 0, 0, 0);
         }
     }
-    T* o = out + (int64_t(i) * c.H + h) * D + lane;
+};
+
+// 8-bit pages.  K operand of instruction (t, 2 c + h): dims 64 c + 16 g + 8 h .. + 7.  V: dims D / 16 ln ..
+template <int D, typename T>
+struct Tile<D, T, int8_t> {
+    static constexpr int NC = D / 64, KS = 2 * NC, NJ = D / 16, NV = D / 64, QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3;
+    u32x4 k[2][NC];
+    uint32_t v[8][NV];
+    struct Query {
+        bf16x8 f[QT][KS];
+    };
+
+    static __device__ __forceinline__ int kcol(int g) { return 16 * g; }
+    static __device__ __forceinline__ int vcol(int ln) { return NJ * ln; }
+    static __device__ __forceinline__ int dim(int j, int row) { return NJ * row + j; }
+    static __device__ __forceinline__ void query(Query& q, const T* x, int g) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[64 * e] = static_cast<T>(any ? acc[e] / l : 0.f);
+        for (int s = 0; s < KS; ++s) {
+            float y[8] = {};
+            if (x) load8(x + 64 * (s / 2) + 16 * g + 8 * (s % 2), y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                bf16 t[QT];
+                terms(y[e], t);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) q.f[i][s][e] = t[i];
+            }
+        }
+    }
+    __device__ __forceinline__ void load_k(int t, const char* p) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) k[t][c] = *reinterpret_cast<const u32x4*>(p + 64 * c);
+    }
+    __device__ __forceinline__ void load_v(int e, const char* p) {
+        if constexpr (NV == 2) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+            v[e][0] = x[0], v[e][1] = x[1];
+        } else {
+            v[e][0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+    }
+    __device__ __forceinline__ void clear_v(int) {}   // codes are numbers whatever they are
+    __device__ __forceinline__ f32x4 scores(int t, const Query& q) const {
+        f32x4 s = {};
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bf16x8 a;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = static_cast<bf16>(code(k[t][c][2 * h + e / 4], e % 4));
+#pragma unroll
+                for (int i = QT - 1; i >= 0; --i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q.f[i][2 * c + h], s, 0, 0, 0);
+            }
+        return s;
+    }
+    __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&o)[NJ]) const {
+        bf16x8 w[PT];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            bf16 t[PT];
+            terms(p[e], t);
+#pragma unroll
+            for (int i = 0; i < PT; ++i) w[i][e] = t[i];
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            bf16x8 a;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] = static_cast<bf16>(code(v[e][j / 4], j % 4));
+#pragma unroll
+            for (int i = PT - 1; i >= 0; --i) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[i], o[j], 0, 0, 0);
+        }
+    }
+};
+
+// float32 pages.  K operand of instruction (t, 4 c + i): dim 16 c + 4 g + i.  V operand of instruction (4 h + i, e): dim
+// 64 h + 4 ln + i of key 8 g + e.
+template <int D>
+struct Tile<D, float, float> {
+    static constexpr int NC = D / 16, NH = D / 64, NJ = D / 16;
+    f32x4 k[2][NC], v[8][NH];
+    struct Query {
+        f32x4 f[NC];
+    };
+
+    static __device__ __forceinline__ int kcol(int g) { return 16 * g; }
+    static __device__ __forceinline__ int vcol(int ln) { return 16 * ln; }
+    static __device__ __forceinline__ int dim(int j, int row) { return 64 * (j / 4) + 4 * row + j % 4; }
+    static __device__ __forceinline__ void query(Query& q, const float* x, int g) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) q.f[c] = x ? *reinterpret_cast<const f32x4*>(x + 16 * c + 4 * g) : f32x4{};
+    }
+    __device__ __forceinline__ void load_k(int t, const char* p) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) k[t][c] = *reinterpret_cast<const f32x4*>(p + 64 * c);
+    }
+    __device__ __forceinline__ void load_v(int e, const char* p) {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) v[e][h] = *reinterpret_cast<const f32x4*>(p + 256 * h);
+    }
+    __device__ __forceinline__ void clear_v(int e) {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) v[e][h] = f32x4{};
+    }
+    __device__ __forceinline__ f32x4 scores(int t, const Query& q) const {
+        f32x4 s = {};
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][c][i], q.f[c][i], s, 0, 0, 0);
+        return s;
+    }
+    __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&o)[NJ]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][j / 4][j % 4], p[e], o[j], 0, 0, 0);
+    }
+};
+
+// ------------------------------------------------------------------------------- the kernel
+template <int D>
+struct Joined {   // what the wavefronts leave for one another
+    float m[kSplitWaves][kRows], l[kSplitWaves][kRows], o[kSplitWaves][kRows][D + 4];
+};
+
+// Floats of a unit's result for one query head: o[D], maximum, sum.
+template <int D>
+constexpr int kPart = D + 4;
+
+template <int D, typename T, typename P>
+__global__ __launch_bounds__(kBlock, sizeof(P) == 4 ? 1 : 2) void paged_attention_kernel(
+    ppk::PagedCache c, const int32_t* __restrict__ lens, const T* __restrict__ q, int64_t ldq, T* __restrict__ out,
+    float* __restrict__ part, int target, int groups, float scale_log2) {
+    using Tl = Tile<D, T, P>;
+    constexpr bool kCodes = sizeof(P) == 1;
+    __shared__ Joined<D> lds;
+    const ppk::PagedPlace place = ppk::paged_place(blockIdx.x, c.Hkv * groups);
+    const Unit u = find_unit(lens, c.k, ppk::paged_span(c.max_pages, c.shift), target, place.unit);
+    if (u.seq < 0) return;
+    const int lane = threadIdx.x & 63, g = lane >> 4, ln = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int G = c.H / c.Hkv, kvh = place.head / groups, first = place.head % groups * kRows;
+    const int heads = min(G - first, kRows), h0 = kvh * G + first;   // this workgroup's query heads
+
+    typename Tl::Query qf;
+    Tl::query(qf, ln < heads ? q + u.seq * ldq + int64_t(h0 + ln) * D : nullptr, g);
+
+    const uint32_t row_bytes = c.Hkv * D * sizeof(P);
+    const char* kp = static_cast<const char*>(c.kp) + kvh * D * sizeof(P) + Tl::kcol(g);
+    const char* vp = static_cast<const char*>(c.vp) + kvh * D * sizeof(P) + Tl::vcol(ln);
+    const int32_t* table = c.table + int64_t(u.seq) * c.max_pages;
+    // Lane (g, ln) looks after key 8 g + ln % 8 of a step: its page, and (8-bit) the scale of its key or, from ln = 8 on, value.
+    const int at = wave * kStep + 8 * g + (ln & 7);
+    const float* scales = kCodes ? (ln < 8 ? c.ks : c.vs) + kvh : nullptr;
+    auto page = [&](int tile) {
+        const int key = tile * ppk::kPagedTile + at;
+        return tile < u.tile1 && key < u.len ? table[key >> c.shift] : -1;
+    };
+    auto row_of = [&](int tile, int pg) { return ppk::paged_row(pg, c.n_pages, tile * ppk::kPagedTile + at, c.shift); };
+    struct Buffer {
+        Tl t;
+        int row;
+        float scale;
+    };
+    // Rows that hold nothing are read from row 0 and left out below.
+    auto load = [&](Buffer& b, int row) {
+        b.row = row;
+        if (!__any(row >= 0)) return;   // past the sequence's end
+        const int safe = max(row, 0);
+        if constexpr (kCodes) b.scale = scales[int64_t(safe) * c.Hkv];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t r = __shfl(safe, 16 * (ln >> 2) + 4 * t + (ln & 3), kWave);
+            b.t.load_k(t, kp + uint64_t(r) * row_bytes);
+        }
+        each<8>([&](auto e) {
+            const uint32_t r = row_lane<e>(safe);
+            b.t.load_v(e, vp + uint64_t(r) * row_bytes);
+        });
+    };
+
+    f32x4 o[Tl::NJ];
+#pragma unroll
+    for (int j = 0; j < Tl::NJ; ++j) o[j] = f32x4{};
+    // m: a reference that no score exceeds by more than 8 in log2 units, so that the accumulators are rescaled on few
+    // steps; the same for the four lanes of a query head.  l: this lane's keys alone, until the end.
+    float m = -FLT_MAX, l = 0.f;
+    const float lazy = 8.0f / scale_log2;
+    bool any = false;
+    auto step = [&](Buffer& b) {
+        if (!__any(b.row >= 0)) return;
+        any = true;
+        const bool full = __all(b.row >= 0);
+        float s[8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const f32x4 x = b.t.scores(t, qf);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[4 * t + r] = x[r];
+        }
+        if constexpr (kCodes) each<8>([&](auto e) { s[e] *= row_lane<e>(b.scale); });
+        if (!full) {
+            each<8>([&](auto e) {
+                if (row_lane<e>(b.row) < 0) {
+                    s[e] = -INFINITY;
+                    b.t.clear_v(e);   // what lies there may be no number
+                }
+            });
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
+        mx = max16(mx);
+        if (__any(mx > m + lazy)) {
+            const float m_new = fmaxf(m, mx);
+            const float corr = __builtin_amdgcn_exp2f((m - m_new) * scale_log2);
+            l *= corr;
+#pragma unroll
+            for (int j = 0; j < Tl::NJ; ++j) o[j] *= corr;
+            m = m_new;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[e] = __builtin_amdgcn_exp2f((s[e] - m) * scale_log2);
+            l += s[e];
+        }
+        if constexpr (kCodes) {
+            each<8>([&](auto e) {
+                const float w = s[e] * row_lane<8 + e>(b.scale);
+                s[e] = full || row_lane<e>(b.row) >= 0 ? w : 0.f;
+            });
+        }
+        b.t.add(s, o);
+    };
+
+    // Pages two tiles ahead, keys and values one.
+    Buffer a, b;
+    int pg = page(u.tile0), pg_next = page(u.tile0 + 1);
+    load(a, row_of(u.tile0, pg));
+    for (int tile = u.tile0; tile < u.tile1; tile += 2) {
+        pg = page(tile + 2);
+        load(b, row_of(tile + 1, pg_next));
+        step(a);
+        if (tile + 1 >= u.tile1) break;
+        pg_next = page(tile + 3);
+        load(a, row_of(tile + 2, pg));
+        step(b);
+    }
+
+    // Join the wavefronts.  A maximum of -inf stands for no key at all.
+    l = sum16(l);
+    if (ln < heads) {
+        if (g == 0) lds.m[wave][ln] = any ? m : -INFINITY, lds.l[wave][ln] = l;
+#pragma unroll
+        for (int j = 0; j < Tl::NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) lds.o[wave][ln][Tl::dim(j, 4 * g + r)] = o[j][r];
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < heads * D; x += kBlock) {
+        const int h = x / D, d = x % D;
+        float M = -INFINITY, L = 0.f, O = 0.f;
+#pragma unroll
+        for (int w = 0; w < kSplitWaves; ++w) M = fmaxf(M, lds.m[w][h]);
+#pragma unroll
+        for (int w = 0; w < kSplitWaves; ++w) {
+            const float f = lds.m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lds.m[w][h] - M) * scale_log2);
+            L += lds.l[w][h] * f;
+            O += lds.o[w][h][d] * f;
+        }
+        if (u.units == 1) {
+            out[(int64_t(u.seq) * c.H + h0 + h) * D + d] = static_cast<T>(M == -INFINITY ? 0.f : O / L);
+        } else {
+            float* p = part + (int64_t(place.unit) * c.H + h0 + h) * kPart<D>;
+            p[d] = O;
+            if (d == 0) p[D] = M, p[D + 1] = L;
+        }
+    }
 }
+
+// The units of a sequence, in their order: one workgroup per (sequence, query head), D / 4 lanes per unit.
+template <int D, typename T>
+__global__ __launch_bounds__(kBlock) void join_kernel(ppk::PagedCache c, const int32_t* __restrict__ lens,
+                                                      const float* __restrict__ part, T* __restrict__ out, int target,
+                                                      float scale_log2) {
+    constexpr int LANES = D / 4, AT = kBlock / LANES;   // units at a time
+    __shared__ float lm[AT], ll[AT];
+    __shared__ f32x4 lo[AT][LANES];
+    const int i = blockIdx.x / c.H, h = blockIdx.x % c.H;
+    const int2 u = units_of(lens, c.k, ppk::paged_span(c.max_pages, c.shift), target, i);
+    if (u.y <= 1) return;
+    const int w = threadIdx.x / LANES, d = threadIdx.x % LANES;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {};
+    const float* p = part + (int64_t(u.x) * c.H + h) * kPart<D>;
+    const int64_t ld = int64_t(c.H) * kPart<D>;
+#pragma unroll 4
+    for (int n = w; n < u.y; n += AT) {
+        const float* x = p + n * ld;
+        const f32x4 xo = *reinterpret_cast<const f32x4*>(x + 4 * d);
+        const float xm = x[D], xl = x[D + 1], M = fmaxf(m, xm);
+        const float fa = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale_log2);
+        const float fb = xm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm - M) * scale_log2);
+        o = o * fa + xo * fb;
+        l = l * fa + xl * fb;
+        m = M;
+    }
+    lo[w][d] = o;
+    if (d == 0) lm[w] = m, ll[w] = l;
+    __syncthreads();
+    if (threadIdx.x >= LANES) return;
+    float M = -INFINITY, L = 0.f;
+    f32x4 O = {};
+#pragma unroll
+    for (int n = 0; n < AT; ++n) M = fmaxf(M, lm[n]);
+#pragma unroll
+    for (int n = 0; n < AT; ++n) {
+        const float f = lm[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lm[n] - M) * scale_log2);
+        L += ll[n] * f;
+        O += lo[n][d] * f;
+    }
+    T* y = out + (int64_t(i) * c.H + h) * D + 4 * d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = static_cast<T>(M == -INFINITY ? 0.f : O[e] / L);
+}
+
+int groups_of(int H, int Hkv) { return (H / Hkv + kRows - 1) / kRows; }
+
+// Units asked for per head: about 1024 workgroups, four a CU.
+int target_of(int H, int Hkv) { return max(1, 1024 / (Hkv * groups_of(H, Hkv))); }
 
 }  // namespace
 
 namespace ppk {
 
-size_t paged_attention_workspace(int, int, int, int) { return 0; }
+size_t paged_attention_workspace(int k, int H, int Hkv, int D) {
+    return k ? (size_t(target_of(H, Hkv)) + k) * H * (D + 4) * sizeof(float) : 0;
+}
 
-void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const void* q, int64_t ldq, void* out, void*,
-                     hipStream_t s) {
-    const unsigned blocks = static_cast<unsigned>((int64_t(c.k) * c.H + kBlock / kWave - 1) / (kBlock / kWave));
-    const float scale = 1.0f / sqrtf(static_cast<float>(c.D));
+void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const void* q, int64_t ldq, void* out,
+                     void* part, hipStream_t s) {
+    const int groups = groups_of(c.H, c.Hkv), target = target_of(c.H, c.Hkv);
+    const unsigned blocks = (target + c.k + 7u) / 8 * 8 * c.Hkv * groups;
+    const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(c.D));
+    // a table of one tile's positions never has a second unit
+    const bool split = paged_tiles(paged_span(c.max_pages, c.shift)) > 1;
     auto go = [&](auto d, auto t, auto p) {
         using T = decltype(t);
-        paged_attention_kernel<decltype(d)::value, T, decltype(p)><<<blocks, kBlock, 0, s>>>(
-            c, lens, static_cast<const T*>(q), ldq, static_cast<T*>(out), scale);
+        constexpr int D = decltype(d)::value;
+        paged_attention_kernel<D, T, decltype(p)><<<blocks, kBlock, 0, s>>>(
+            c, lens, static_cast<const T*>(q), ldq, static_cast<T*>(out), static_cast<float*>(part), target, groups, scale_log2);
+        if (split)
+            join_kernel<D, T><<<c.k * c.H, kBlock, 0, s>>>(c, lens, static_cast<const float*>(part), static_cast<T*>(out),
+                                                           target, scale_log2);
     };
     const std::integral_constant<int, 64> d64;
     const std::integral_constant<int, 128> d128;
