@@ -35,6 +35,7 @@ constexpr int kRows = 16;   // query heads of a workgroup
 static_assert(kSplitWaves * kStep == ppk::kPagedTile, "a tile is one step of a workgroup");
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // f(0) .. f(N - 1) with constants for arguments.
 template <typename F, int... I>
@@ -80,41 +81,61 @@ __device__ __forceinline__ void terms(float x, bf16 (&t)[N]) {
     }
 }
 
-__device__ __forceinline__ float code(uint32_t w, int i) { return static_cast<float>(static_cast<int8_t>(w >> (8 * i))); }
+// Bits of the float32 form of byte B of w, a signed number: one instruction, which takes the byte where it lies.
+template <int B>
+__device__ __forceinline__ uint32_t byte_value(uint32_t w) {
+    uint32_t f;
+    if constexpr (B == 0)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(w));
+    else if constexpr (B == 1)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(w));
+    else if constexpr (B == 2)
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(w));
+    else
+        asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(w));
+    return f;
+}
 
 // ------------------------------------------------------------------------------- the split
 struct Unit {
     int seq, len, tile0, tile1, units;   // seq < 0: none
 };
 
-__device__ __forceinline__ int tiles_of(const int32_t* lens, int i, int k, int span) {
-    return i < k ? ppk::paged_tiles(ppk::paged_len(lens[i], span)) : 0;
-}
-
-__device__ __forceinline__ int unit_size(const int32_t* lens, int k, int span, int target) {
-    int64_t all = 0;
-    for (int i = threadIdx.x & 63; i < k; i += kWave) all += tiles_of(lens, i, k, span);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) all += __shfl_xor(all, o, kWave);
-    return ppk::paged_unit(all, target);
-}
-
+// Sum over the lanes up to and including this one.
 __device__ __forceinline__ int scan_up(int x) {
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const int y = __shfl_up(x, o, kWave);
-        if ((threadIdx.x & 63) >= o) x += y;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // 1, 2, 4 and 8 lanes up in rows of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row 0's sum to row 1, row 2's to row 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // the first two rows' to the others
     return x;
 }
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(scan_up(x), kWave - 1); }
 
-// Unit u of the split, by every wavefront for itself.
-__device__ __forceinline__ Unit find_unit(const int32_t* lens, int k, int span, int target, int u) {
-    const int unit = unit_size(lens, k, span, target), lane = threadIdx.x & 63;
+struct Split {
+    const int32_t* lens;
+    int k, span, target, least;
+    __device__ __forceinline__ int len(int i) const { return i < k ? ppk::paged_len(lens[i], span) : 0; }
+    // Tiles of a unit, by a wavefront; first: this lane's len(lane).
+    __device__ __forceinline__ int unit(int first) const {
+        int64_t all = ppk::paged_tiles(first);
+        for (int i = (threadIdx.x & 63) + kWave; i < k; i += kWave) all += ppk::paged_tiles(len(i));
+        // at most 2^24 tiles a sequence and 2^16 sequences a lane: two sums of 32 bits
+        const int64_t lo = wave_total(static_cast<int>(all & 0xffffff)), hi = wave_total(static_cast<int>(all >> 24));
+        return ppk::paged_unit((hi << 24) + lo, target, least);
+    }
+};
+
+// Unit u, by every wavefront for itself.
+__device__ __forceinline__ Unit find_unit(const Split& s, int u) {
+    const int lane = threadIdx.x & 63;
+    int len = s.len(lane);
+    const int unit = s.unit(len);
     int base = 0;
-    for (int i0 = 0; i0 < k; i0 += kWave) {
-        const int i = i0 + lane, len = i < k ? ppk::paged_len(lens[i], span) : 0, t = ppk::paged_tiles(len);
-        const int n = i < k ? ppk::paged_units(t, unit) : 0, end = base + scan_up(n);
+    for (int i0 = 0; i0 < s.k; i0 += kWave) {
+        if (i0) len = s.len(i0 + lane);
+        const int t = ppk::paged_tiles(len), n = i0 + lane < s.k ? ppk::paged_units(t, unit) : 0, end = base + scan_up(n);
         const uint64_t here = __ballot(u < end && u >= end - n);
         if (here) {
             const int l = __builtin_ctzll(here);
@@ -128,11 +149,14 @@ __device__ __forceinline__ Unit find_unit(const int32_t* lens, int k, int span, 
 }
 
 // The first unit of sequence i, and how many it has.
-__device__ __forceinline__ int2 units_of(const int32_t* lens, int k, int span, int target, int i) {
-    const int unit = unit_size(lens, k, span, target), lane = threadIdx.x & 63;
+__device__ __forceinline__ int2 units_of(const Split& s, int i) {
+    const int lane = threadIdx.x & 63;
+    int len = s.len(lane);
+    const int unit = s.unit(len);
     int base = 0;
     for (int i0 = 0;; i0 += kWave) {
-        const int n = i0 + lane < k ? ppk::paged_units(tiles_of(lens, i0 + lane, k, span), unit) : 0, end = base + scan_up(n);
+        if (i0) len = s.len(i0 + lane);
+        const int n = i0 + lane < s.k ? ppk::paged_units(ppk::paged_tiles(len), unit) : 0, end = base + scan_up(n);
         if (i < i0 + kWave)
             return make_int2(__builtin_amdgcn_readlane(end - n, i - i0), __builtin_amdgcn_readlane(n, i - i0));
         base = __builtin_amdgcn_readlane(end, kWave - 1);
@@ -197,32 +221,57 @@ struct Tile<D, bf16, bf16> {
     }
 };
 
-// 8-bit pages.  K operand of instruction (t, 2 c + h): dims 64 c + 16 g + 8 h .. + 7.  V: dims D / 16 ln ..
+// 8-bit pages, without turning codes into numbers one by one.
+// Keys: the query as digits of 7 bits (three, for float32 four; value = sum of digit * 128^i * 2^-shift, exact
+// down to 2^-20, 2^-27 of the row's largest), products of int8 in int32.  K operand of instruction (t, c): dims 64 c + 16 g
+// .. + 15.
+// Values: a code is exact in bf16, the upper half of its float32 form.  Lane's part of a row: dims D / 16 ln ..
 template <int D, typename T>
 struct Tile<D, T, int8_t> {
-    static constexpr int NC = D / 64, KS = 2 * NC, NJ = D / 16, NV = D / 64, QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3;
+    static constexpr int NC = D / 64, NJ = D / 16, NV = D / 64, QD = sizeof(T) == 2 ? 3 : 4, PT = sizeof(T) == 2 ? 2 : 3;
     u32x4 k[2][NC];
     uint32_t v[8][NV];
     struct Query {
-        bf16x8 f[QT][KS];
+        i32x4 f[QD][NC];
+        int shift;      // of the row
+        float poison;   // 0; not a number where the row holds no numbers
     };
 
     static __device__ __forceinline__ int kcol(int g) { return 16 * g; }
     static __device__ __forceinline__ int vcol(int ln) { return NJ * ln; }
     static __device__ __forceinline__ int dim(int j, int row) { return NJ * row + j; }
     static __device__ __forceinline__ void query(Query& q, const T* x, int g) {
+        float y[NC][16] = {};
+        uint32_t top = 0;
+        if (x) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            float y[8] = {};
-            if (x) load8(x + 64 * (s / 2) + 16 * g + 8 * (s % 2), y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                bf16 t[QT];
-                terms(y[e], t);
-#pragma unroll
-                for (int i = 0; i < QT; ++i) q.f[i][s][e] = t[i];
+            for (int c = 0; c < NC; ++c) {
+                load8(x + 64 * c + 16 * g, y[c]);
+                load8(x + 64 * c + 16 * g + 8, y[c] + 8);
             }
         }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(y[c][e]) & 0x7fffffffu);
+        const bool finite = max16(top < 0x7f800000u ? 0.f : 1.f) == 0.f;
+        const float m = max16(__uint_as_float(finite ? top : 0u));
+        q.poison = finite ? 0.f : __uint_as_float(0x7fc00000u);
+        q.shift = 7 * QD - 1 - __builtin_amdgcn_frexp_expf(m);   // the largest becomes 2^(7 QD - 2) .. 2^(7 QD - 1)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    int n = static_cast<int>(rintf(finite ? ldexpf(y[c][e + b], q.shift) : 0.f));
+#pragma unroll
+                    for (int i = 0; i < QD; ++i) {
+                        const int d = i + 1 < QD ? (n << 25) >> 25 : n;   // -64 .. 63, the last one up to +-65
+                        n = (n - d) >> 7;
+                        q.f[i][c][e / 4] = (b ? q.f[i][c][e / 4] : 0) | (d & 255) << (8 * b);
+                    }
+                }
     }
     __device__ __forceinline__ void load_k(int t, const char* p) {
 #pragma unroll
@@ -238,18 +287,22 @@ struct Tile<D, T, int8_t> {
     }
     __device__ __forceinline__ void clear_v(int) {}   // codes are numbers whatever they are
     __device__ __forceinline__ f32x4 scores(int t, const Query& q) const {
-        f32x4 s = {};
+        i32x4 s[QD];
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int i = 0; i < QD; ++i) {
+            s[i] = i32x4{};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 a;
+            for (int c = 0; c < NC; ++c)
+                s[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, k[t][c]), q.f[i][c], s[i], 0, 0, 0);
+        }
+        f32x4 f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = static_cast<bf16>(code(k[t][c][2 * h + e / 4], e % 4));
-#pragma unroll
-                for (int i = QT - 1; i >= 0; --i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q.f[i][2 * c + h], s, 0, 0, 0);
-            }
-        return s;
+        for (int r = 0; r < 4; ++r) {   // |s| < 2^21
+            const float lo = static_cast<float>(s[1][r] * 128 + s[0][r]);
+            const float hi = static_cast<float>(QD == 4 ? s[QD - 1][r] * 128 + s[2][r] : s[2][r]);
+            f[r] = ldexpf(fmaf(hi, 16384.f, lo), -q.shift) + q.poison;
+        }
+        return f;
     }
     __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&o)[NJ]) const {
         bf16x8 w[PT];
@@ -260,14 +313,15 @@ struct Tile<D, T, int8_t> {
 #pragma unroll
             for (int i = 0; i < PT; ++i) w[i][e] = t[i];
         }
+        each<NJ>([&](auto j) {
+            u32x4 f;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            bf16x8 a;
+            for (int e = 0; e < 4; ++e)
+                f[e] = __builtin_amdgcn_perm(byte_value<j % 4>(v[2 * e + 1][j / 4]), byte_value<j % 4>(v[2 * e][j / 4]), 0x07060302u);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = static_cast<bf16>(code(v[e][j / 4], j % 4));
-#pragma unroll
-            for (int i = PT - 1; i >= 0; --i) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[i], o[j], 0, 0, 0);
-        }
+            for (int i = PT - 1; i >= 0; --i)
+                o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), w[i], o[j], 0, 0, 0);
+        });
     }
 };
 
@@ -328,13 +382,12 @@ constexpr int kPart = D + 4;
 
 template <int D, typename T, typename P>
 __global__ __launch_bounds__(kBlock, sizeof(P) == 4 ? 1 : 2) void paged_attention_kernel(
-    ppk::PagedCache c, const int32_t* __restrict__ lens, const T* __restrict__ q, int64_t ldq, T* __restrict__ out,
-    float* __restrict__ part, int target, int groups, float scale_log2) {
+    ppk::PagedCache c, const T* __restrict__ q, int64_t ldq, T* __restrict__ out, float* __restrict__ part, Split split, int groups, float scale_log2) {
     using Tl = Tile<D, T, P>;
     constexpr bool kCodes = sizeof(P) == 1;
     __shared__ Joined<D> lds;
     const ppk::PagedPlace place = ppk::paged_place(blockIdx.x, c.Hkv * groups);
-    const Unit u = find_unit(lens, c.k, ppk::paged_span(c.max_pages, c.shift), target, place.unit);
+    const Unit u = find_unit(split, place.unit);
     if (u.seq < 0) return;
     const int lane = threadIdx.x & 63, g = lane >> 4, ln = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -397,7 +450,11 @@ __global__ __launch_bounds__(kBlock, sizeof(P) == 4 ? 1 : 2) void paged_attentio
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[4 * t + r] = x[r];
         }
-        if constexpr (kCodes) each<8>([&](auto e) { s[e] *= row_lane<e>(b.scale); });
+        float scale = 0.f;
+        if constexpr (kCodes) {
+            scale = b.row >= 0 ? b.scale : 0.f;
+            each<8>([&](auto e) { s[e] *= row_lane<e>(scale); });
+        }
         if (!full) {
             each<8>([&](auto e) {
                 if (row_lane<e>(b.row) < 0) {
@@ -424,10 +481,7 @@ __global__ __launch_bounds__(kBlock, sizeof(P) == 4 ? 1 : 2) void paged_attentio
             l += s[e];
         }
         if constexpr (kCodes) {
-            each<8>([&](auto e) {
-                const float w = s[e] * row_lane<8 + e>(b.scale);
-                s[e] = full || row_lane<e>(b.row) >= 0 ? w : 0.f;
-            });
+            each<8>([&](auto e) { s[e] *= row_lane<8 + e>(scale); });
         }
         b.t.add(s, o);
     };
@@ -477,53 +531,59 @@ __global__ __launch_bounds__(kBlock, sizeof(P) == 4 ? 1 : 2) void paged_attentio
     }
 }
 
-// The units of a sequence, in their order: one workgroup per (sequence, query head), D / 4 lanes per unit.
+// The units of a sequence, in their order: a workgroup takes `per` of its query heads one after another, D / 4
+// lanes per unit.
 template <int D, typename T>
-__global__ __launch_bounds__(kBlock) void join_kernel(ppk::PagedCache c, const int32_t* __restrict__ lens,
-                                                      const float* __restrict__ part, T* __restrict__ out, int target,
-                                                      float scale_log2) {
+__global__ __launch_bounds__(kBlock) void join_kernel(const float* __restrict__ part, T* __restrict__ out, Split split, int H,
+                                                      int per, float scale_log2) {
     constexpr int LANES = D / 4, AT = kBlock / LANES;   // units at a time
     __shared__ float lm[AT], ll[AT];
     __shared__ f32x4 lo[AT][LANES];
-    const int i = blockIdx.x / c.H, h = blockIdx.x % c.H;
-    const int2 u = units_of(lens, c.k, ppk::paged_span(c.max_pages, c.shift), target, i);
+    const int chunks = (H + per - 1) / per, i = blockIdx.x / chunks, h0 = blockIdx.x % chunks * per;
+    const int2 u = units_of(split, i);
     if (u.y <= 1) return;
     const int w = threadIdx.x / LANES, d = threadIdx.x % LANES;
-    float m = -INFINITY, l = 0.f;
-    f32x4 o = {};
-    const float* p = part + (int64_t(u.x) * c.H + h) * kPart<D>;
-    const int64_t ld = int64_t(c.H) * kPart<D>;
+    const int64_t ld = int64_t(H) * kPart<D>;
+    for (int h = h0; h < min(h0 + per, H); ++h) {
+        float m = -INFINITY, l = 0.f;
+        f32x4 o = {};
+        const float* p = part + (int64_t(u.x) * H + h) * kPart<D>;
 #pragma unroll 4
-    for (int n = w; n < u.y; n += AT) {
-        const float* x = p + n * ld;
-        const f32x4 xo = *reinterpret_cast<const f32x4*>(x + 4 * d);
-        const float xm = x[D], xl = x[D + 1], M = fmaxf(m, xm);
-        const float fa = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale_log2);
-        const float fb = xm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm - M) * scale_log2);
-        o = o * fa + xo * fb;
-        l = l * fa + xl * fb;
-        m = M;
+        for (int n = w; n < u.y; n += AT) {
+            const float* x = p + n * ld;
+            const f32x4 xo = *reinterpret_cast<const f32x4*>(x + 4 * d);
+            const float xm = x[D], xl = x[D + 1], M = fmaxf(m, xm);
+            const float fa = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale_log2);
+            const float fb = xm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm - M) * scale_log2);
+            o = o * fa + xo * fb;
+            l = l * fa + xl * fb;
+            m = M;
+        }
+        lo[w][d] = o;
+        if (d == 0) lm[w] = m, ll[w] = l;
+        __syncthreads();
+        if (threadIdx.x < LANES) {
+            float M = -INFINITY, L = 0.f;
+            f32x4 O = {};
+#pragma unroll
+            for (int n = 0; n < AT; ++n) M = fmaxf(M, lm[n]);
+#pragma unroll
+            for (int n = 0; n < AT; ++n) {
+                const float f = lm[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lm[n] - M) * scale_log2);
+                L += ll[n] * f;
+                O += lo[n][d] * f;
+            }
+            T* y = out + (int64_t(i) * H + h) * D + 4 * d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = static_cast<T>(M == -INFINITY ? 0.f : O[e] / L);
+        }
+        __syncthreads();
     }
-    lo[w][d] = o;
-    if (d == 0) lm[w] = m, ll[w] = l;
-    __syncthreads();
-    if (threadIdx.x >= LANES) return;
-    float M = -INFINITY, L = 0.f;
-    f32x4 O = {};
-#pragma unroll
-    for (int n = 0; n < AT; ++n) M = fmaxf(M, lm[n]);
-#pragma unroll
-    for (int n = 0; n < AT; ++n) {
-        const float f = lm[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lm[n] - M) * scale_log2);
-        L += ll[n] * f;
-        O += lo[n][d] * f;
-    }
-    T* y = out + (int64_t(i) * c.H + h) * D + 4 * d;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = static_cast<T>(M == -INFINITY ? 0.f : O[e] / L);
 }
 
 int groups_of(int H, int Hkv) { return (H / Hkv + kRows - 1) / kRows; }
+
+constexpr int kAlone = 4, kJoinBlocks = 2048;
 
 // Units asked for per head: about 1024 workgroups, four a CU.
 int target_of(int H, int Hkv) { return max(1, 1024 / (Hkv * groups_of(H, Hkv))); }
@@ -541,16 +601,18 @@ void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const 
     const int groups = groups_of(c.H, c.Hkv), target = target_of(c.H, c.Hkv);
     const unsigned blocks = (target + c.k + 7u) / 8 * 8 * c.Hkv * groups;
     const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(c.D));
-    // a table of one tile's positions never has a second unit
-    const bool split = paged_tiles(paged_span(c.max_pages, c.shift)) > 1;
+    // Sequences that a short table bounds are not split: a second launch costs more than their few tiles in a row.
+    const int span = paged_span(c.max_pages, c.shift), tiles = paged_tiles(span);
+    const Split split{lens, c.k, span, target, tiles <= kAlone ? max(tiles, 1) : 1};
+    const int per = (int64_t(c.k) * c.H + kJoinBlocks - 1) / kJoinBlocks, chunks = (c.H + per - 1) / per;
     auto go = [&](auto d, auto t, auto p) {
         using T = decltype(t);
         constexpr int D = decltype(d)::value;
         paged_attention_kernel<D, T, decltype(p)><<<blocks, kBlock, 0, s>>>(
-            c, lens, static_cast<const T*>(q), ldq, static_cast<T*>(out), static_cast<float*>(part), target, groups, scale_log2);
-        if (split)
-            join_kernel<D, T><<<c.k * c.H, kBlock, 0, s>>>(c, lens, static_cast<const float*>(part), static_cast<T*>(out),
-                                                           target, scale_log2);
+            c, static_cast<const T*>(q), ldq, static_cast<T*>(out), static_cast<float*>(part), split, groups, scale_log2);
+        if (tiles > kAlone)
+            join_kernel<D, T><<<c.k * chunks, kBlock, 0, s>>>(static_cast<const float*>(part), static_cast<T*>(out), split, c.H,
+                                                              per, scale_log2);
     };
     const std::integral_constant<int, 64> d64;
     const std::integral_constant<int, 128> d128;

@@ -20,12 +20,13 @@ constexpr int32_t paged_span(int32_t max_pages, int shift) {
 constexpr int32_t paged_len(int32_t len, int32_t span) { return len < 0 ? 0 : len < span ? len : span; }
 
 // The split of the attention.  A tile is kPagedTile keys, a step of a workgroup.  With T tiles in all sequences,
-// every sequence is cut into units of `unit` = ceil(T / target) tiles, the last one shorter; a sequence without
-// keys has one unit, which writes its zeros.  All sequences together have at most target + k units.
+// every sequence is cut into units of `unit` = ceil(T / target) tiles (`least` at least), the last one shorter; a
+// sequence without keys has one unit, which writes its zeros.  All sequences together have at most target + k units.
 constexpr int kPagedTile = 128;
 constexpr int32_t paged_tiles(int32_t len) { return len / kPagedTile + (len % kPagedTile != 0); }
-constexpr int32_t paged_unit(int64_t tiles, int32_t target) {
-    return tiles <= target ? 1 : static_cast<int32_t>((tiles + target - 1) / target);
+constexpr int32_t paged_unit(int64_t tiles, int32_t target, int32_t least) {
+    const int64_t unit = (tiles + target - 1) / target;
+    return unit < least ? least : static_cast<int32_t>(unit);
 }
 constexpr int32_t paged_units(int32_t tiles, int32_t unit) { return tiles <= unit ? 1 : (tiles + unit - 1) / unit; }
 

@@ -1,5 +1,5 @@
 // Asks csrc/paged.h on the CPU.  Lines in:
-//   split target heads len len ...   -> for every workgroup of the grid that has work: "seq head tile0 tile1 units"
+//   split target least heads len len ...   -> for every workgroup of the grid that has work: "seq head tile0 tile1 units"
 //   rows n_pages shift max_pages page ...  (one sequence's table) -> row of every position up to the span + 2
 #include <cstdio>
 #include <iostream>
@@ -18,12 +18,12 @@ int main() {
         std::string what;
         in >> what;
         if (what == "split") {
-            int target, heads, n;
-            in >> target >> heads;
+            int target, least, heads, n;
+            in >> target >> least >> heads;
             std::vector<int> tiles;
             int64_t all = 0;
             while (in >> n) tiles.push_back(paged_tiles(n)), all += tiles.back();
-            const int unit = paged_unit(all, target);
+            const int unit = paged_unit(all, target, least);
             const uint32_t bound = target + tiles.size();
             for (uint32_t b = 0; b < (bound + 7) / 8 * 8 * heads; ++b) {
                 const PagedPlace p = paged_place(b, heads);

@@ -208,8 +208,9 @@ def test_split_covers_every_key_once(ask):
         k = rng.randrange(1, 40)
         top = rng.choice([1, 200, 5000, 100000])
         cases.append((rng.choice([1, 5, 16, 64, 256]), rng.randrange(1, 9), [rng.choice([0, rng.randrange(1, top + 1)]) for _ in range(k)]))
-    got = ask(["split %d %d %s" % (t, h, " ".join(map(str, lens))) for t, h, lens in cases])
-    for (target, heads, lens), g in zip(cases, got):
+    least = [rng.choice([1, 1, 4]) for _ in cases]
+    got = ask(["split %d %d %d %s" % (t, m, h, " ".join(map(str, lens))) for m, (t, h, lens) in zip(least, cases)])
+    for (target, heads, lens), m, g in zip(cases, least, got):
         units = [tuple(g[i:i + 5]) for i in range(0, len(g), 5)]
         assert len(units) <= (target + len(lens)) * heads
         for i, n in enumerate(lens):
@@ -219,10 +220,11 @@ def test_split_covers_every_key_once(ask):
                 assert all(a[1] == b[0] for a, b in zip(mine, mine[1:]))
                 assert {u[4] for u in units if u[:2] == (i, h)} == {len(mine)}
                 assert n == 0 or all(a < b for a, b in mine)
+                assert len(mine) == 1 or all(b - a >= m for a, b in mine[:-1])
 
 
 def test_split_of_the_largest_lengths(ask):
     big = 2 ** 31 - 1
-    (got,) = ask(["split 3 1 %d %d" % (big, big)])
+    (got,) = ask(["split 3 1 1 %d %d" % (big, big)])
     units = [tuple(got[i:i + 5]) for i in range(0, len(got), 5)]
     assert [sorted(u[2:4] for u in units if u[0] == i)[-1][1] for i in (0, 1)] == [2 ** 24, 2 ** 24]
