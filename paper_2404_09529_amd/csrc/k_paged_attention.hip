@@ -2,17 +2,18 @@
 // first lens[i] keys of sequence i, in whatever pages they lie.
 //
 // Every key and value is read once and used for the G = H / Hkv query heads that share it, so reading them bounds
-// the kernel.  The sequences are cut into units of whole 128-key tiles (paged.h); a workgroup has one unit of one
-// key/value head, its four wavefronts 32 keys of each tile, each with a softmax of its own (running maximum and
-// sum), joined through LDS at the end.  A sequence of one unit is written right away, the units of a longer one leave
-// (o, maximum, sum) for join_kernel.
+// the kernel.  A wavefront has a range of 32-key steps of one key/value head (paged.h), through as many sequences as it
+// spans, with a softmax's running maximum and sum of its own; wavefronts share nothing.  A sequence that lies in one range
+// is written right away, the pieces of others leave (o, maximum, sum) for join_kernel.  256 workgroups of eight wavefronts,
+// which have neighbouring heads of the same keys, read as fast as anything measured (2 x 415 MB of bf16 rows of 8 heads, reads
+// alone: eight heads to a workgroup, 200 of these, 6.4 TB/s; one head to a workgroup of four, 1600 of these, 5.2).
 //
 // Nothing passes through LDS on the way: keys go from memory into the registers that the 16 x 16 matrix
-// instructions take them from.  S^T = K Q^T puts key 8 g + 4 t + r of a wavefront's 32 into row 4 g + r of score tile t,
+// instructions take them from.  S^T = K Q^T puts key 8 g + 4 t + r of a step into row 4 g + r of score tile t,
 // so that lane group g (16 lanes) holds the scores of keys 8 g .. 8 g + 7, which is what it has to hold as the operand of
 // O^T = V^T P^T; a lane reads the same 16 (or 8, or 4) columns' part of those 8 rows of V, whole rows per 16 lanes.
 // The query heads are the instructions' columns; with fewer than 16 the rest are zeros (the matrix cores are idle
-// otherwise: a 32-key step of 16 KB takes them 256 cycles of the 6500 that a SIMD's share of the memory needs).
+// otherwise: a step of 16 KB takes them 384 cycles of the 1600 that a CU's share of the memory needs).
 //
 // bf16 operands hold what is exact in them: bf16 keys, values and queries, and 8-bit codes, whose scales multiply scores
 // and probabilities.  Probabilities (times a value's scale) are two bf16 terms, off by 2^-17, so that the result is as good
@@ -29,10 +30,8 @@
 
 namespace {
 
-constexpr int kBlock = 256, kSplitWaves = kBlock / kWave;
-constexpr int kStep = 32;   // keys of a wavefront per tile
-constexpr int kRows = 16;   // query heads of a workgroup
-static_assert(kSplitWaves * kStep == ppk::kPagedTile, "a tile is one step of a workgroup");
+constexpr int kBlock = ppk::kPagedWaves * kWave;
+constexpr int kRows = 16;   // query heads of a wavefront
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -97,10 +96,6 @@ __device__ __forceinline__ uint32_t byte_value(uint32_t w) {
 }
 
 // ------------------------------------------------------------------------------- the split
-struct Unit {
-    int seq, len, tile0, tile1, units;   // seq < 0: none
-};
-
 // Sum over the lanes up to and including this one.
 __device__ __forceinline__ int scan_up(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // 1, 2, 4 and 8 lanes up in rows of 16
@@ -111,57 +106,81 @@ __device__ __forceinline__ int scan_up(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // the first two rows' to the others
     return x;
 }
-__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(scan_up(x), kWave - 1); }
 
 struct Split {
     const int32_t* lens;
-    int k, span, target, least;
-    __device__ __forceinline__ int len(int i) const { return i < k ? ppk::paged_len(lens[i], span) : 0; }
-    // Tiles of a unit, by a wavefront; first: this lane's len(lane).
-    __device__ __forceinline__ int unit(int first) const {
-        int64_t all = ppk::paged_tiles(first);
-        for (int i = (threadIdx.x & 63) + kWave; i < k; i += kWave) all += ppk::paged_tiles(len(i));
-        // at most 2^24 tiles a sequence and 2^16 sequences a lane: two sums of 32 bits
-        const int64_t lo = wave_total(static_cast<int>(all & 0xffffff)), hi = wave_total(static_cast<int>(all >> 24));
-        return ppk::paged_unit((hi << 24) + lo, target, least);
-    }
+    int k, span, ranges;
+    bool narrow;   // the steps of all sequences, as long as their tables, are below 2^31
 };
 
-// Unit u, by every wavefront for itself.
-__device__ __forceinline__ Unit find_unit(const Split& s, int u) {
-    const int lane = threadIdx.x & 63;
-    int len = s.len(lane);
-    const int unit = s.unit(len);
-    int base = 0;
-    for (int i0 = 0; i0 < s.k; i0 += kWave) {
-        if (i0) len = s.len(i0 + lane);
-        const int t = ppk::paged_tiles(len), n = i0 + lane < s.k ? ppk::paged_units(t, unit) : 0, end = base + scan_up(n);
-        const uint64_t here = __ballot(u < end && u >= end - n);
-        if (here) {
-            const int l = __builtin_ctzll(here);
-            const int first = u - __builtin_amdgcn_readlane(end - n, l), tiles = __builtin_amdgcn_readlane(t, l);
-            return {i0 + l, __builtin_amdgcn_readlane(len, l), first * unit, min(first * unit + unit, tiles),
-                    __builtin_amdgcn_readlane(n, l)};
-        }
-        base = __builtin_amdgcn_readlane(end, kWave - 1);
-    }
-    return {-1, 0, 0, 0, 0};
-}
+// The lengths of sequences first .. first + 255 in a wavefront's registers, lane l those of numbers l, 64 + l, 128 + l
+// and 192 + l (one wait for memory), and the steps up to and including each.
+struct Lens {
+    Split s;
+    int first;
+    int len0, len1, len2, len3;
+    int64_t end0, end1, end2, end3;
 
-// The first unit of sequence i, and how many it has.
-__device__ __forceinline__ int2 units_of(const Split& s, int i) {
-    const int lane = threadIdx.x & 63;
-    int len = s.len(lane);
-    const int unit = s.unit(len);
-    int base = 0;
-    for (int i0 = 0;; i0 += kWave) {
-        if (i0) len = s.len(i0 + lane);
-        const int n = i0 + lane < s.k ? ppk::paged_units(ppk::paged_tiles(len), unit) : 0, end = base + scan_up(n);
-        if (i < i0 + kWave)
-            return make_int2(__builtin_amdgcn_readlane(end - n, i - i0), __builtin_amdgcn_readlane(n, i - i0));
-        base = __builtin_amdgcn_readlane(end, kWave - 1);
+    __device__ __forceinline__ void load(int i0) {
+        first = i0;
+        const int i = i0 + (threadIdx.x & 63);
+        const int n0 = s.lens[min(i, s.k - 1)], n1 = s.lens[min(i + kWave, s.k - 1)],
+                  n2 = s.lens[min(i + 2 * kWave, s.k - 1)], n3 = s.lens[min(i + 3 * kWave, s.k - 1)];
+        len0 = i < s.k ? ppk::paged_len(n0, s.span) : 0;
+        len1 = i + kWave < s.k ? ppk::paged_len(n1, s.span) : 0;
+        len2 = i + 2 * kWave < s.k ? ppk::paged_len(n2, s.span) : 0;
+        len3 = i + 3 * kWave < s.k ? ppk::paged_len(n3, s.span) : 0;
     }
-}
+    __device__ __forceinline__ int64_t scan(int len) const {
+        const int n = ppk::paged_steps(len);
+        if (s.narrow) return scan_up(n);
+        const int lo = scan_up(n & 0xffff), hi = scan_up(n >> 16);   // at most 2^26 steps, 64 times
+        return (int64_t(hi) << 16) + lo;
+    }
+    static __device__ __forceinline__ int64_t of_lane(int64_t x, int l) {
+        return int64_t(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), l))) |
+               int64_t(__builtin_amdgcn_readlane(static_cast<int>(x >> 32), l)) << 32;
+    }
+    // The block from sequence i0 on, `base` steps before it; the steps up to its end.
+    __device__ __forceinline__ int64_t block(int i0, int64_t base) {
+        load(i0);
+        const int n = s.k - i0;
+        end0 = base + scan(len0);
+        base = of_lane(end0, 63);
+        end1 = end2 = end3 = base;
+        if (n > kWave) end1 = base + scan(len1), base = of_lane(end1, 63), end2 = end3 = base;
+        if (n > 2 * kWave) end2 = base + scan(len2), base = of_lane(end2, 63), end3 = base;
+        if (n > 3 * kWave) end3 = base + scan(len3), base = of_lane(end3, 63);
+        return base;
+    }
+    // Steps of all sequences; the first block stays.
+    __device__ __forceinline__ int64_t total() {
+        if (s.k <= 4 * kWave) return block(0, 0);
+        int64_t all = 0;
+        for (int i0 = 4 * kWave; i0 < s.k; i0 += 4 * kWave) all = block(i0, all);
+        return all + block(0, 0);
+    }
+    // Sequence i >= first, the same in all lanes: its length; its last step's number plus one (within the block).
+    __device__ __forceinline__ int length(int i) {
+        if (i >= first + 4 * kWave) load(i);
+        const int c = (i - first) / kWave, l = (i - first) % kWave;
+        const int a = __builtin_amdgcn_readlane(len0, l), b = __builtin_amdgcn_readlane(len1, l),
+                  d = __builtin_amdgcn_readlane(len2, l), e = __builtin_amdgcn_readlane(len3, l);
+        return c == 0 ? a : c == 1 ? b : c == 2 ? d : e;
+    }
+    __device__ __forceinline__ int64_t end(int i) const {
+        const int c = (i - first) / kWave, l = (i - first) % kWave;
+        const int64_t a = of_lane(end0, l), b = of_lane(end1, l), d = of_lane(end2, l), e = of_lane(end3, l);
+        return c == 0 ? a : c == 1 ? b : c == 2 ? d : e;
+    }
+    // The sequence of step s0 < total(); its block stays.
+    __device__ __forceinline__ int holding(int64_t s0) {
+        int64_t base = of_lane(end3, 63);
+        for (int i0 = first; base <= s0; base = block(i0, base)) i0 += 4 * kWave;
+        const uint64_t a = __ballot(end0 > s0), b = __ballot(end1 > s0), c = __ballot(end2 > s0), d = __ballot(end3 > s0);
+        return first + (a ? __builtin_ctzll(a) : b ? kWave + __builtin_ctzll(b) : c ? 2 * kWave + __builtin_ctzll(c) : 3 * kWave + __builtin_ctzll(d));
+    }
+};
 
 // ------------------------------------------------------------------------------- operands by type
 // A wavefront's 32 rows of K and V in registers, and the products with them.  Lane (g, ln) = (lane / 16, lane % 16).
@@ -182,7 +201,12 @@ struct Tile<D, bf16, bf16> {
 
     static __device__ __forceinline__ int kcol(int g) { return 16 * g; }
     static __device__ __forceinline__ int vcol(int ln) { return 16 * ln; }
-    static __device__ __forceinline__ int dim(int j, int row) { return 8 * row + j; }
+    // f(j), j < NJ, are the values of `row` of the products; Y: float, or the type of the result.
+    template <typename Y, typename F>
+    static __device__ __forceinline__ void put(Y* y, int row, F f) {
+        const float v[8] = {f(0), f(1), f(2), f(3), f(4), f(5), f(6), f(7)};
+        store8(y + 8 * row, v);
+    }
     static __device__ __forceinline__ void query(Query& q, const bf16* x, int g) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) q.f[s] = x ? *reinterpret_cast<const bf16x8*>(x + 32 * s + 8 * g) : bf16x8{};
@@ -239,7 +263,16 @@ struct Tile<D, T, int8_t> {
 
     static __device__ __forceinline__ int kcol(int g) { return 16 * g; }
     static __device__ __forceinline__ int vcol(int ln) { return NJ * ln; }
-    static __device__ __forceinline__ int dim(int j, int row) { return NJ * row + j; }
+    template <typename Y, typename F>
+    static __device__ __forceinline__ void put(Y* y, int row, F f) {
+        if constexpr (NJ == 8) {
+            const float v[8] = {f(0), f(1), f(2), f(3), f(4), f(5), f(6), f(7)};
+            store8(y + 8 * row, v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) y[NJ * row + j] = static_cast<Y>(f(j));
+        }
+    }
     static __device__ __forceinline__ void query(Query& q, const T* x, int g) {
         float y[NC][16] = {};
         uint32_t top = 0;
@@ -337,7 +370,14 @@ struct Tile<D, float, float> {
 
     static __device__ __forceinline__ int kcol(int g) { return 16 * g; }
     static __device__ __forceinline__ int vcol(int ln) { return 16 * ln; }
-    static __device__ __forceinline__ int dim(int j, int row) { return 64 * (j / 4) + 4 * row + j % 4; }
+    template <typename Y, typename F>
+    static __device__ __forceinline__ void put(Y* y, int row, F f) {
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            const f32x4 v = {f(4 * h), f(4 * h + 1), f(4 * h + 2), f(4 * h + 3)};
+            *reinterpret_cast<f32x4*>(y + 64 * h + 4 * row) = v;
+        }
+    }
     static __device__ __forceinline__ void query(Query& q, const float* x, int g) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) q.f[c] = x ? *reinterpret_cast<const f32x4*>(x + 16 * c + 4 * g) : f32x4{};
@@ -372,187 +412,283 @@ struct Tile<D, float, float> {
 
 // ------------------------------------------------------------------------------- the kernel
 template <int D>
-struct Joined {   // what the wavefronts leave for one another
-    float m[kSplitWaves][kRows], l[kSplitWaves][kRows], o[kSplitWaves][kRows][D + 4];
+struct Joined {   // what the wavefronts of a workgroup that has one sequence leave for one another
+    float m[ppk::kPagedWaves][kRows], l[ppk::kPagedWaves][kRows], o[ppk::kPagedWaves][kRows][D + 4];
 };
 
-// Floats of a unit's result for one query head: o[D], maximum, sum.
+// Floats of a piece's result for one query head: o[D], maximum (-inf: no key), sum.  A range leaves at most two pieces:
+// number 0 starts with the range, number 1 does not.
 template <int D>
 constexpr int kPart = D + 4;
+template <int D>
+__device__ __forceinline__ int64_t part_at(int range, int piece, int H, int h) {
+    return ((int64_t(range) * 2 + piece) * H + h) * kPart<D>;
+}
 
-template <int D, typename T, typename P>
-__global__ __launch_bounds__(kBlock, sizeof(P) == 4 ? 1 : 2) void paged_attention_kernel(
-    ppk::PagedCache c, const T* __restrict__ q, int64_t ldq, T* __restrict__ out, float* __restrict__ part, Split split, int groups, float scale_log2) {
+// WHOLE: a workgroup has one sequence for one head, its wavefronts every eighth step, joined through LDS.
+template <int D, typename T, typename P, bool WHOLE>
+__global__ __launch_bounds__(kBlock, 2) void paged_attention_kernel(ppk::PagedCache c, const T* __restrict__ q,
+                                                                    int64_t ldq, T* __restrict__ out,
+                                                                    float* __restrict__ part, Split split, int groups,
+                                                                    float scale_log2) {
     using Tl = Tile<D, T, P>;
     constexpr bool kCodes = sizeof(P) == 1;
-    __shared__ Joined<D> lds;
-    const ppk::PagedPlace place = ppk::paged_place(blockIdx.x, c.Hkv * groups);
-    const Unit u = find_unit(split, place.unit);
-    if (u.seq < 0) return;
     const int lane = threadIdx.x & 63, g = lane >> 4, ln = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int G = c.H / c.Hkv, kvh = place.head / groups, first = place.head % groups * kRows;
-    const int heads = min(G - first, kRows), h0 = kvh * G + first;   // this workgroup's query heads
 
-    typename Tl::Query qf;
-    Tl::query(qf, ln < heads ? q + u.seq * ldq + int64_t(h0 + ln) * D : nullptr, g);
+    // Where this wavefront is: step `st` of sequence `seq`, which has `steps`; `left` steps to go after it.
+    struct Where {
+        int seq, st, len, steps;
+    };
+    Lens lens = {split};
+    Where at;
+    int64_t left;
+    int head, range = 0;
+    bool begins = true;      // the piece starts with its sequence
+    int piece = 0;
+    if constexpr (WHOLE) {
+        head = blockIdx.x % (c.Hkv * groups);
+        at.seq = blockIdx.x / (c.Hkv * groups);
+        at.st = wave;
+        at.len = ppk::paged_len(split.lens[at.seq], split.span);
+        at.steps = ppk::paged_steps(at.len);
+        left = (at.steps - wave + ppk::kPagedWaves - 1) / ppk::kPagedWaves;
+    } else {
+        const ppk::PagedPlace place = ppk::paged_place(blockIdx.x, gridDim.x, wave, c.Hkv * groups);
+        head = place.head, range = place.range;
+        if (range >= split.ranges) return;
+        const int64_t all = lens.total(), s0 = ppk::paged_start(range, all, split.ranges);
+        left = ppk::paged_start(range + 1, all, split.ranges) - s0;
+        if (left <= 0) return;
+        at.seq = lens.holding(s0);
+        at.len = lens.length(at.seq);
+        at.steps = ppk::paged_steps(at.len);
+        at.st = at.steps - static_cast<int>(lens.end(at.seq) - s0);
+        begins = at.st == 0;
+    }
+    const int G = c.H / c.Hkv, kvh = head / groups, first = head % groups * kRows;
+    const int heads = min(G - first, kRows), h0 = kvh * G + first;   // this wavefront's query heads
 
     const uint32_t row_bytes = c.Hkv * D * sizeof(P);
     const char* kp = static_cast<const char*>(c.kp) + kvh * D * sizeof(P) + Tl::kcol(g);
     const char* vp = static_cast<const char*>(c.vp) + kvh * D * sizeof(P) + Tl::vcol(ln);
-    const int32_t* table = c.table + int64_t(u.seq) * c.max_pages;
     // Lane (g, ln) looks after key 8 g + ln % 8 of a step: its page, and (8-bit) the scale of its key or, from ln = 8 on, value.
-    const int at = wave * kStep + 8 * g + (ln & 7);
+    const int mine = 8 * g + (ln & 7);
     const float* scales = kCodes ? (ln < 8 ? c.ks : c.vs) + kvh : nullptr;
-    auto page = [&](int tile) {
-        const int key = tile * ppk::kPagedTile + at;
-        return tile < u.tile1 && key < u.len ? table[key >> c.shift] : -1;
+    // (No load of the loop below is behind a branch: the compiler would wait for all of them where the ways join.)
+    auto page = [&](const Where& w) {
+        const int key = max(min(w.st * ppk::kPagedStep + mine, w.len - 1), 0);
+        return c.table[int64_t(w.seq) * c.max_pages + (key >> c.shift)];
     };
-    auto row_of = [&](int tile, int pg) { return ppk::paged_row(pg, c.n_pages, tile * ppk::kPagedTile + at, c.shift); };
-    struct Buffer {
-        Tl t;
-        int row;
-        float scale;
+    auto row_of = [&](const Where& w, int pg) {
+        const int key = w.st * ppk::kPagedStep + mine;
+        return key < w.len ? ppk::paged_row(pg, c.n_pages, key, c.shift) : -1;
+    };
+    auto advance = [&](Where& w) {
+        if constexpr (WHOLE) {
+            w.st += ppk::kPagedWaves;
+        } else if (++w.st >= w.steps) {
+            int n = w.seq + 1, len = 0;
+            while (n < split.k && (len = lens.length(n)) == 0) ++n;
+            if (n < split.k) w = {n, 0, len, ppk::paged_steps(len)};   // (else past the last range's end)
+        }
     };
     // Rows that hold nothing are read from row 0 and left out below.
-    auto load = [&](Buffer& b, int row) {
-        b.row = row;
-        if (!__any(row >= 0)) return;   // past the sequence's end
+    Tl t;
+    auto load_k = [&](int row) {
         const int safe = max(row, 0);
-        if constexpr (kCodes) b.scale = scales[int64_t(safe) * c.Hkv];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint32_t r = __shfl(safe, 16 * (ln >> 2) + 4 * t + (ln & 3), kWave);
-            b.t.load_k(t, kp + uint64_t(r) * row_bytes);
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t r = __shfl(safe, 16 * (ln >> 2) + 4 * i + (ln & 3), kWave);
+            t.load_k(i, kp + uint64_t(r) * row_bytes);
         }
+        return kCodes ? scales[int64_t(safe) * c.Hkv] : 0.f;
+    };
+    auto load_v = [&](int row) {
+        const int safe = max(row, 0);
         each<8>([&](auto e) {
             const uint32_t r = row_lane<e>(safe);
-            b.t.load_v(e, vp + uint64_t(r) * row_bytes);
+            t.load_v(e, vp + uint64_t(r) * row_bytes);
         });
     };
+    typename Tl::Query qf;
+    auto load_q = [&](int seq) { Tl::query(qf, ln < heads ? q + seq * ldq + int64_t(h0 + ln) * D : nullptr, g); };
 
     f32x4 o[Tl::NJ];
-#pragma unroll
-    for (int j = 0; j < Tl::NJ; ++j) o[j] = f32x4{};
     // m: a reference that no score exceeds by more than 8 in log2 units, so that the accumulators are rescaled on few
     // steps; the same for the four lanes of a query head.  l: this lane's keys alone, until the end.
-    float m = -FLT_MAX, l = 0.f;
+    float m, l;
+    bool any;
+    auto clear = [&] {
+#pragma unroll
+        for (int j = 0; j < Tl::NJ; ++j) o[j] = f32x4{};
+        m = -FLT_MAX, l = 0.f, any = false;
+    };
+    clear();
     const float lazy = 8.0f / scale_log2;
-    bool any = false;
-    auto step = [&](Buffer& b) {
-        if (!__any(b.row >= 0)) return;
-        any = true;
-        const bool full = __all(b.row >= 0);
-        float s[8];
+
+    // Write what ends here: a whole sequence, or a piece.
+    auto flush = [&](int seq, bool complete) {
+        const float L = sum16(l);
+        if (ln >= heads) return;
+        if (complete) {
+            T* y = out + (int64_t(seq) * c.H + h0 + ln) * D;
+            const float inv = any ? 1.0f / L : 0.f;   // 0 / 0: scores of -inf alone
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const f32x4 x = b.t.scores(t, qf);
+            for (int r = 0; r < 4; ++r) Tl::put(y, 4 * g + r, [&](int j) { return any ? o[j][r] * inv : 0.f; });
+        } else {
+            float* y = part + part_at<D>(range, piece, c.H, h0 + ln);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[4 * t + r] = x[r];
+            for (int r = 0; r < 4; ++r) Tl::put(y, 4 * g + r, [&](int j) { return o[j][r]; });
+            if (g == 0) y[D] = any ? m : -INFINITY, y[D + 1] = L;
         }
-        float scale = 0.f;
-        if constexpr (kCodes) {
-            scale = b.row >= 0 ? b.scale : 0.f;
-            each<8>([&](auto e) { s[e] *= row_lane<e>(scale); });
-        }
-        if (!full) {
-            each<8>([&](auto e) {
-                if (row_lane<e>(b.row) < 0) {
-                    s[e] = -INFINITY;
-                    b.t.clear_v(e);   // what lies there may be no number
-                }
-            });
-        }
-        float mx = s[0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
-        mx = max16(mx);
-        if (__any(mx > m + lazy)) {
-            const float m_new = fmaxf(m, mx);
-            const float corr = __builtin_amdgcn_exp2f((m - m_new) * scale_log2);
-            l *= corr;
-#pragma unroll
-            for (int j = 0; j < Tl::NJ; ++j) o[j] *= corr;
-            m = m_new;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s[e] = __builtin_amdgcn_exp2f((s[e] - m) * scale_log2);
-            l += s[e];
-        }
-        if constexpr (kCodes) {
-            each<8>([&](auto e) { s[e] *= row_lane<8 + e>(scale); });
-        }
-        b.t.add(s, o);
     };
 
-    // Pages two tiles ahead, keys and values one.
-    Buffer a, b;
-    int pg = page(u.tile0), pg_next = page(u.tile0 + 1);
-    load(a, row_of(u.tile0, pg));
-    for (int tile = u.tile0; tile < u.tile1; tile += 2) {
-        pg = page(tile + 2);
-        load(b, row_of(tile + 1, pg_next));
-        step(a);
-        if (tile + 1 >= u.tile1) break;
-        pg_next = page(tile + 3);
-        load(a, row_of(tile + 2, pg));
-        step(b);
+    if (left > 0) {
+        Where next = at;
+        advance(next);
+        int row = row_of(at, page(at)), page_next = page(next);
+        load_q(at.seq);
+        float scale = load_k(row);
+        load_v(row);
+        // The registers of a step's keys take the next step's as soon as the scores are formed, those of the values after the
+        // second product, and the other wavefronts fill the wait; a page number is read two steps ahead.
+        auto step = [&](auto more) {
+            int row_next = -1;
+            Where then = next;
+            if constexpr (more) {
+                advance(then);
+                row_next = row_of(next, page_next);
+                page_next = page(then);
+            }
+            float s[8], scale_next = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const f32x4 x = t.scores(i, qf);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[4 * i + r] = x[r];
+            }
+            // (Loads are kept from moving up, where they would need registers of their own.)
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more) {
+                if (!WHOLE && next.seq != at.seq) load_q(next.seq);
+                scale_next = load_k(row_next);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            any |= __any(row >= 0);
+            if constexpr (kCodes) {
+                scale = row >= 0 ? scale : 0.f;
+                each<8>([&](auto e) { s[e] *= row_lane<e>(scale); });
+            }
+            if (!__all(row >= 0)) {
+                each<8>([&](auto e) {
+                    if (row_lane<e>(row) < 0) {
+                        s[e] = -INFINITY;
+                        t.clear_v(e);   // what lies there may be no number
+                    }
+                });
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, s[e]);
+            mx = max16(mx);
+            if (__any(mx > m + lazy)) {
+                const float m_new = fmaxf(m, mx);
+                const float corr = __builtin_amdgcn_exp2f((m - m_new) * scale_log2);
+                l *= corr;
+#pragma unroll
+                for (int j = 0; j < Tl::NJ; ++j) o[j] *= corr;
+                m = m_new;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s[e] = __builtin_amdgcn_exp2f((s[e] - m) * scale_log2);
+                l += s[e];
+            }
+            if constexpr (kCodes) each<8>([&](auto e) { s[e] *= row_lane<8 + e>(scale); });
+            t.add(s, o);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (more) load_v(row_next);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (!WHOLE) {
+                const bool ends = at.st + 1 == at.steps;
+                if (!more || ends) {
+                    flush(at.seq, begins && ends);
+                    clear();
+                    begins = true, piece = 1;
+                }
+            }
+            at = next, next = then, row = row_next, scale = scale_next;
+        };
+#pragma unroll 1
+        for (; left > 1; --left) step(std::true_type{});
+        step(std::false_type{});
     }
 
-    // Join the wavefronts.  A maximum of -inf stands for no key at all.
-    l = sum16(l);
-    if (ln < heads) {
-        if (g == 0) lds.m[wave][ln] = any ? m : -INFINITY, lds.l[wave][ln] = l;
+    if constexpr (WHOLE) {
+        __shared__ Joined<D> lds;
+        const float L = sum16(l);
+        if (ln < heads) {
+            if (g == 0) lds.m[wave][ln] = any ? m : -INFINITY, lds.l[wave][ln] = L;
 #pragma unroll
-        for (int j = 0; j < Tl::NJ; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) lds.o[wave][ln][Tl::dim(j, 4 * g + r)] = o[j][r];
-    }
-    __syncthreads();
-    for (int x = threadIdx.x; x < heads * D; x += kBlock) {
-        const int h = x / D, d = x % D;
-        float M = -INFINITY, L = 0.f, O = 0.f;
-#pragma unroll
-        for (int w = 0; w < kSplitWaves; ++w) M = fmaxf(M, lds.m[w][h]);
-#pragma unroll
-        for (int w = 0; w < kSplitWaves; ++w) {
-            const float f = lds.m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lds.m[w][h] - M) * scale_log2);
-            L += lds.l[w][h] * f;
-            O += lds.o[w][h][d] * f;
+            for (int r = 0; r < 4; ++r) Tl::put(lds.o[wave][ln], 4 * g + r, [&](int j) { return o[j][r]; });
         }
-        if (u.units == 1) {
-            out[(int64_t(u.seq) * c.H + h0 + h) * D + d] = static_cast<T>(M == -INFINITY ? 0.f : O / L);
-        } else {
-            float* p = part + (int64_t(place.unit) * c.H + h0 + h) * kPart<D>;
-            p[d] = O;
-            if (d == 0) p[D] = M, p[D + 1] = L;
+        __syncthreads();
+        const int seq = blockIdx.x / (c.Hkv * groups);
+        for (int x = threadIdx.x; x < heads * D; x += kBlock) {
+            const int h = x / D, d = x % D;
+            float M = -INFINITY, S = 0.f, O = 0.f;
+#pragma unroll
+            for (int w = 0; w < ppk::kPagedWaves; ++w) M = fmaxf(M, lds.m[w][h]);
+#pragma unroll
+            for (int w = 0; w < ppk::kPagedWaves; ++w) {
+                const float f = lds.m[w][h] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lds.m[w][h] - M) * scale_log2);
+                S += lds.l[w][h] * f;
+                O += lds.o[w][h][d] * f;
+            }
+            out[(int64_t(seq) * c.H + h0 + h) * D + d] = static_cast<T>(M == -INFINITY ? 0.f : O / S);
         }
     }
 }
 
-// The units of a sequence, in their order: a workgroup takes `per` of its query heads one after another, D / 4
-// lanes per unit.
+// The pieces of a sequence that spans ranges, in their order, and the zeros of one without keys: a workgroup takes `per`
+// query heads one after another, D / 4 lanes per piece.
+constexpr int kJoin = 512;
 template <int D, typename T>
-__global__ __launch_bounds__(kBlock) void join_kernel(const float* __restrict__ part, T* __restrict__ out, Split split, int H,
-                                                      int per, float scale_log2) {
-    constexpr int LANES = D / 4, AT = kBlock / LANES;   // units at a time
+__global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ part, T* __restrict__ out, Split split, int H,
+                                                     int per, float scale_log2) {
+    constexpr int LANES = D / 4, AT = kJoin / LANES;   // pieces at a time
     __shared__ float lm[AT], ll[AT];
     __shared__ f32x4 lo[AT][LANES];
     const int chunks = (H + per - 1) / per, i = blockIdx.x / chunks, h0 = blockIdx.x % chunks * per;
-    const int2 u = units_of(split, i);
-    if (u.y <= 1) return;
+    Lens lens = {split};
+    const int64_t all = lens.total();
+    if (i >= 4 * kWave) {
+        int64_t base = lens.of_lane(lens.end3, 63);
+        for (int i0 = 4 * kWave; i0 <= i; i0 += 4 * kWave) base = lens.block(i0, base);
+    }
+    const int64_t s1 = lens.end(i), s0 = s1 - ppk::paged_steps(lens.length(i));   // the sequence's steps
     const int w = threadIdx.x / LANES, d = threadIdx.x % LANES;
-    const int64_t ld = int64_t(H) * kPart<D>;
+    if (s0 == s1) {
+        for (int x = threadIdx.x; x < (min(h0 + per, H) - h0) * D; x += kJoin)
+            out[(int64_t(i) * H + h0) * D + x] = static_cast<T>(0.f);
+        return;
+    }
+    // With fewer steps than ranges some ranges are empty, and a step is a piece.
+    const bool sparse = all < split.ranges;
+    const int r0 = ppk::paged_range(s0, all, split.ranges);
+    const int n = sparse ? static_cast<int>(s1 - s0) : ppk::paged_range(s1 - 1, all, split.ranges) - r0 + 1;
+    if (n == 1) return;
+    const int piece0 = ppk::paged_start(r0, all, split.ranges) == s0 ? 0 : 1;
     for (int h = h0; h < min(h0 + per, H); ++h) {
         float m = -INFINITY, l = 0.f;
         f32x4 o = {};
-        const float* p = part + (int64_t(u.x) * H + h) * kPart<D>;
 #pragma unroll 4
-        for (int n = w; n < u.y; n += AT) {
-            const float* x = p + n * ld;
-            const f32x4 xo = *reinterpret_cast<const f32x4*>(x + 4 * d);
-            const float xm = x[D], xl = x[D + 1], M = fmaxf(m, xm);
+        for (int x = w; x < n; x += AT) {
+            const int r = sparse ? ppk::paged_range(s0 + x, all, split.ranges) : r0 + x;
+            const float* p = part + part_at<D>(r, x ? 0 : piece0, H, h);
+            const f32x4 xo = *reinterpret_cast<const f32x4*>(p + 4 * d);
+            const float xm = p[D], xl = p[D + 1], M = fmaxf(m, xm);
             const float fa = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale_log2);
             const float fb = xm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((xm - M) * scale_log2);
             o = o * fa + xo * fb;
@@ -566,12 +702,12 @@ __global__ __launch_bounds__(kBlock) void join_kernel(const float* __restrict__ 
             float M = -INFINITY, L = 0.f;
             f32x4 O = {};
 #pragma unroll
-            for (int n = 0; n < AT; ++n) M = fmaxf(M, lm[n]);
+            for (int x = 0; x < AT; ++x) M = fmaxf(M, lm[x]);
 #pragma unroll
-            for (int n = 0; n < AT; ++n) {
-                const float f = lm[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lm[n] - M) * scale_log2);
-                L += ll[n] * f;
-                O += lo[n][d] * f;
+            for (int x = 0; x < AT; ++x) {
+                const float f = lm[x] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lm[x] - M) * scale_log2);
+                L += ll[x] * f;
+                O += lo[x][d] * f;
             }
             T* y = out + (int64_t(i) * H + h) * D + 4 * d;
 #pragma unroll
@@ -581,38 +717,39 @@ __global__ __launch_bounds__(kBlock) void join_kernel(const float* __restrict__ 
     }
 }
 
-int groups_of(int H, int Hkv) { return (H / Hkv + kRows - 1) / kRows; }
+int heads_of(int H, int Hkv) { return Hkv * ((H / Hkv + kRows - 1) / kRows); }
 
-constexpr int kAlone = 4, kJoinBlocks = 2048;
-
-// Units asked for per head: about 1024 workgroups, four a CU.
-int target_of(int H, int Hkv) { return max(1, 1024 / (Hkv * groups_of(H, Hkv))); }
+// Sequences that a table of kWhole positions bounds are a workgroup's each, if the workgroups find room at once.
+constexpr int kWhole = 512, kWholeBlocks = 256, kJoinBlocks = 2048;
 
 }  // namespace
 
 namespace ppk {
 
 size_t paged_attention_workspace(int k, int H, int Hkv, int D) {
-    return k ? (size_t(target_of(H, Hkv)) + k) * H * (D + 4) * sizeof(float) : 0;
+    return k ? size_t(paged_ranges(heads_of(H, Hkv))) * 2 * H * (D + 4) * sizeof(float) : 0;
 }
 
 void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const void* q, int64_t ldq, void* out,
                      void* part, hipStream_t s) {
-    const int groups = groups_of(c.H, c.Hkv), target = target_of(c.H, c.Hkv);
-    const unsigned blocks = (target + c.k + 7u) / 8 * 8 * c.Hkv * groups;
+    const int heads = heads_of(c.H, c.Hkv), groups = heads / c.Hkv, span = paged_span(c.max_pages, c.shift);
     const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(c.D));
-    // Sequences that a short table bounds are not split: a second launch costs more than their few tiles in a row.
-    const int span = paged_span(c.max_pages, c.shift), tiles = paged_tiles(span);
-    const Split split{lens, c.k, span, target, tiles <= kAlone ? max(tiles, 1) : 1};
+    const Split split{lens, c.k, span, paged_ranges(heads), int64_t(c.k) * paged_steps(span) <= INT32_MAX};
+    const bool whole = span <= kWhole && int64_t(c.k) * heads <= kWholeBlocks;
     const int per = (int64_t(c.k) * c.H + kJoinBlocks - 1) / kJoinBlocks, chunks = (c.H + per - 1) / per;
     auto go = [&](auto d, auto t, auto p) {
         using T = decltype(t);
+        using P = decltype(p);
         constexpr int D = decltype(d)::value;
-        paged_attention_kernel<D, T, decltype(p)><<<blocks, kBlock, 0, s>>>(
-            c, static_cast<const T*>(q), ldq, static_cast<T*>(out), static_cast<float*>(part), split, groups, scale_log2);
-        if (tiles > kAlone)
-            join_kernel<D, T><<<c.k * chunks, kBlock, 0, s>>>(static_cast<const float*>(part), static_cast<T*>(out), split, c.H,
-                                                              per, scale_log2);
+        const T* x = static_cast<const T*>(q);
+        T* y = static_cast<T*>(out);
+        float* f = static_cast<float*>(part);
+        if (whole) {
+            paged_attention_kernel<D, T, P, true><<<c.k * heads, kBlock, 0, s>>>(c, x, ldq, y, f, split, groups, scale_log2);
+            return;
+        }
+        paged_attention_kernel<D, T, P, false><<<paged_groups(heads), kBlock, 0, s>>>(c, x, ldq, y, f, split, groups, scale_log2);
+        join_kernel<D, T><<<c.k * chunks, kJoin, 0, s>>>(f, y, split, c.H, per, scale_log2);
     };
     const std::integral_constant<int, 64> d64;
     const std::integral_constant<int, 128> d128;

@@ -19,24 +19,36 @@ constexpr int32_t paged_span(int32_t max_pages, int shift) {
 // Keys that a sequence of stated length has in reach of its table.
 constexpr int32_t paged_len(int32_t len, int32_t span) { return len < 0 ? 0 : len < span ? len : span; }
 
-// The split of the attention.  A tile is kPagedTile keys, a step of a workgroup.  With T tiles in all sequences,
-// every sequence is cut into units of `unit` = ceil(T / target) tiles (`least` at least), the last one shorter; a
-// sequence without keys has one unit, which writes its zeros.  All sequences together have at most target + k units.
-constexpr int kPagedTile = 128;
-constexpr int32_t paged_tiles(int32_t len) { return len / kPagedTile + (len % kPagedTile != 0); }
-constexpr int32_t paged_unit(int64_t tiles, int32_t target, int32_t least) {
-    const int64_t unit = (tiles + target - 1) / target;
-    return unit < least ? least : static_cast<int32_t>(unit);
+// The split of the attention.  A step is kPagedStep keys of one sequence for one key/value head, the work of one
+// wavefront; all S steps of all sequences, one sequence after the other, are dealt to W ranges of equal length, range w
+// starting with step w S / W, and a wavefront has one range of one head.
+constexpr int kPagedStep = 32, kPagedWaves = 8;   // keys; wavefronts of a workgroup
+constexpr int32_t paged_steps(int32_t len) { return len / kPagedStep + (len % kPagedStep != 0); }
+// (Operands fit 63 bits: a sequence has at most 2^26 steps, there are at most 2^22 sequences and 2^14 ranges.)
+constexpr int64_t paged_quotient(int64_t a, int64_t b) {
+    return (uint64_t(a) | uint64_t(b)) >> 32 ? int64_t(uint64_t(a) / uint64_t(b)) : int64_t(uint32_t(a) / uint32_t(b));
 }
-constexpr int32_t paged_units(int32_t tiles, int32_t unit) { return tiles <= unit ? 1 : (tiles + unit - 1) / unit; }
+constexpr int64_t paged_start(int32_t w, int64_t S, int32_t W) { return paged_quotient(w * S, W); }
+// The range that holds step s.
+constexpr int32_t paged_range(int64_t s, int64_t S, int32_t W) {
+    return static_cast<int32_t>(paged_quotient((s + 1) * W - 1, S));
+}
 
-// Workgroups are dealt to the 8 XCDs in turn.  All heads of a unit go to one XCD: the keys of neighbouring heads
-// lie side by side in a row, and an XCD's L2 then fetches whole rows.  Unit and head of workgroup b:
+// Workgroups and ranges for `heads` key/value heads (each counted once per 16 query heads): about 256 workgroups.
+constexpr int32_t paged_groups(int32_t heads) {
+    return heads <= 256 * kPagedWaves ? 256 : (heads + kPagedWaves * 8 - 1) / (kPagedWaves * 8) * 8;
+}
+constexpr int32_t paged_ranges(int32_t heads) { return paged_groups(heads) * kPagedWaves / heads; }
+
+// Workgroups are dealt to the 8 XCDs in turn.  Wavefronts side by side have neighbouring heads of one range, whose
+// rows lie side by side in memory, and an XCD has consecutive ranges.  Range and head of wavefront `wave` of workgroup b
+// of n (a multiple of 8); range >= W: none.
 struct PagedPlace {
-    int32_t unit, head;
+    int32_t range, head;
 };
-constexpr PagedPlace paged_place(uint32_t b, int32_t heads) {
-    return {static_cast<int32_t>(b / 8 / heads * 8 + b % 8), static_cast<int32_t>(b / 8 % heads)};
+constexpr PagedPlace paged_place(uint32_t b, uint32_t n, uint32_t wave, int32_t heads) {
+    const uint32_t q = (b % 8 * (n / 8) + b / 8) * kPagedWaves + wave;
+    return {static_cast<int32_t>(q / heads), static_cast<int32_t>(q % heads)};
 }
 
 }  // namespace ppk

@@ -1,5 +1,7 @@
 // Asks csrc/paged.h on the CPU.  Lines in:
-//   split target least heads len len ...   -> for every workgroup of the grid that has work: "seq head tile0 tile1 units"
+//   split W len len ...   -> of every range its first step, then -1 and for every sequence with keys the ranges of its
+//                            first and last step
+//   places heads          -> groups, ranges, then "range head" of every wavefront of the grid
 //   rows n_pages shift max_pages page ...  (one sequence's table) -> row of every position up to the span + 2
 #include <cstdio>
 #include <iostream>
@@ -18,25 +20,29 @@ int main() {
         std::string what;
         in >> what;
         if (what == "split") {
-            int target, least, heads, n;
-            in >> target >> least >> heads;
-            std::vector<int> tiles;
-            int64_t all = 0;
-            while (in >> n) tiles.push_back(paged_tiles(n)), all += tiles.back();
-            const int unit = paged_unit(all, target, least);
-            const uint32_t bound = target + tiles.size();
-            for (uint32_t b = 0; b < (bound + 7) / 8 * 8 * heads; ++b) {
-                const PagedPlace p = paged_place(b, heads);
-                int first = 0;
-                for (size_t i = 0; i < tiles.size(); ++i) {
-                    const int u = paged_units(tiles[i], unit);
-                    if (p.unit >= first && p.unit < first + u) {
-                        const int t0 = (p.unit - first) * unit;
-                        std::printf("%zu %d %d %d %d ", i, p.head, t0, std::min(t0 + unit, tiles[i]), u);
-                    }
-                    first += u;
-                }
+            int W, n;
+            in >> W;
+            std::vector<int> steps;
+            int64_t S = 0;
+            while (in >> n) steps.push_back(paged_steps(n)), S += steps.back();
+            for (int w = 0; w <= W; ++w) std::printf("%lld ", static_cast<long long>(paged_start(w, S, W)));
+            std::printf("-1 ");
+            int64_t s0 = 0;
+            for (int t : steps) {
+                if (t) std::printf("%d %d ", paged_range(s0, S, W), paged_range(s0 + t - 1, S, W));
+                s0 += t;
             }
+            std::printf("\n");
+        } else if (what == "places") {
+            int heads;
+            in >> heads;
+            const int n = paged_groups(heads);
+            std::printf("%d %d ", n, paged_ranges(heads));
+            for (int b = 0; b < n; ++b)
+                for (int w = 0; w < kPagedWaves; ++w) {
+                    const PagedPlace p = paged_place(b, n, w, heads);
+                    std::printf("%d %d ", p.range, p.head);
+                }
             std::printf("\n");
         } else {
             int n_pages, shift, max_pages, page;

@@ -109,7 +109,7 @@ def test_attention_workspace():
     assert pp.lib().pp_paged_attention_workspace_size(ctypes.byref(_cfg()), ctypes.byref(_cache()), None) == INV
     for k in (1, 3, 64, 1000):
         st, need = _attend_bytes(cache=dict(k=k))
-        assert st == OK and need <= 4 * (4096 + k) * 4 * 136
+        assert st == OK and need <= 2 * 2048 * 4 * 4 * 136
         if need:
             assert _attend(cache=dict(k=k), ws=None) == INV
             assert _attend(cache=dict(k=k), ws=0x10010) == INV
@@ -201,30 +201,33 @@ def test_rows_of_pages(ask):
         assert all(-1 <= r < n_pages << shift for r in g[:-3])
 
 
-def test_split_covers_every_key_once(ask):
+def test_ranges_cover_every_step_once(ask):
+    """Ranges follow one another from the first step to the last, differ by one step at most, and the joining kernel's
+    view of a sequence, the ranges of its first and last step, is the ranges' own."""
     rng = random.Random(2)
-    cases = [(16, 1, [1]), (1, 3, [0]), (7, 2, [0, 0, 0]), (1, 1, [100000, 0, 3])]
+    cases = [(16, [1]), (1, [5]), (7, [0, 0, 3]), (256, [100000, 0, 3]), (3, [2 ** 31 - 1] * 5), (16384, [2 ** 31 - 1] * 40)]
     for _ in range(150):
-        k = rng.randrange(1, 40)
         top = rng.choice([1, 200, 5000, 100000])
-        cases.append((rng.choice([1, 5, 16, 64, 256]), rng.randrange(1, 9), [rng.choice([0, rng.randrange(1, top + 1)]) for _ in range(k)]))
-    least = [rng.choice([1, 1, 4]) for _ in cases]
-    got = ask(["split %d %d %d %s" % (t, m, h, " ".join(map(str, lens))) for m, (t, h, lens) in zip(least, cases)])
-    for (target, heads, lens), m, g in zip(cases, least, got):
-        units = [tuple(g[i:i + 5]) for i in range(0, len(g), 5)]
-        assert len(units) <= (target + len(lens)) * heads
-        for i, n in enumerate(lens):
-            for h in range(heads):
-                mine = sorted(u[2:4] for u in units if u[:2] == (i, h))
-                assert mine[0][0] == 0 and mine[-1][1] == -(-n // 128)
-                assert all(a[1] == b[0] for a, b in zip(mine, mine[1:]))
-                assert {u[4] for u in units if u[:2] == (i, h)} == {len(mine)}
-                assert n == 0 or all(a < b for a, b in mine)
-                assert len(mine) == 1 or all(b - a >= m for a, b in mine[:-1])
+        cases.append((rng.choice([1, 5, 16, 51, 256, 2048]), [rng.choice([0, rng.randrange(1, top + 1)]) for _ in range(rng.randrange(1, 40))] + [1]))
+    got = ask(["split %d %s" % (w, " ".join(map(str, lens))) for w, lens in cases])
+    for (W, lens), g in zip(cases, got):
+        starts, ends = g[:W + 1], g[W + 2:]
+        steps = [-(-n // 32) for n in lens if n]
+        S = sum(steps)
+        assert starts[0] == 0 and starts[W] == S and g[W + 1] == -1
+        sizes = [b - a for a, b in zip(starts, starts[1:])]
+        assert min(sizes) >= 0 and max(sizes) - min(sizes) <= 1
+        at = 0
+        for i, n in enumerate(steps):
+            for s, r in ((at, ends[2 * i]), (at + n - 1, ends[2 * i + 1])):
+                assert starts[r] <= s < starts[r + 1]
+                assert S >= W or sizes[r] == 1
+            at += n
 
 
-def test_split_of_the_largest_lengths(ask):
-    big = 2 ** 31 - 1
-    (got,) = ask(["split 3 1 1 %d %d" % (big, big)])
-    units = [tuple(got[i:i + 5]) for i in range(0, len(got), 5)]
-    assert [sorted(u[2:4] for u in units if u[0] == i)[-1][1] for i in (0, 1)] == [2 ** 24, 2 ** 24]
+@pytest.mark.parametrize("heads", [1, 2, 3, 8, 10, 32, 40, 64, 100, 257, 2048, 2049, 5000])
+def test_every_range_and_head_has_a_wavefront(ask, heads):
+    (got,) = ask(["places %d" % heads])
+    groups, ranges, places = got[0], got[1], list(zip(got[2::2], got[3::2]))
+    assert groups % 8 == 0 and ranges >= 1 and len(places) == groups * 8
+    assert sorted(p for p in places if p[0] < ranges) == [(r, h) for r in range(ranges) for h in range(heads)]
