@@ -425,11 +425,21 @@ __device__ __forceinline__ int64_t part_at(int range, int piece, int H, int h) {
     return ((int64_t(range) * 2 + piece) * H + h) * kPart<D>;
 }
 
+// What a range leaves for the joining workgroup of its number: the sequence that it continues, of `pieces` pieces, is
+// joined by pieces - 1 workgroups, and this one is number `turn`.  Piece x is in range `first` + x, but with fewer steps
+// than ranges (steps > 0: their number) a step is a piece, and `first` the first one.  The first piece is number p0 there.
+struct Join {
+    int seq, pieces, turn, first, p0, steps;   // seq < 0: nothing to join
+};
+constexpr size_t kJoinBytes = 32;
+static_assert(sizeof(Join) <= kJoinBytes, "room in the workspace");
+
 // WHOLE: a workgroup has one sequence for one head, its wavefronts every eighth step, joined through LDS.
 template <int D, typename T, typename P, bool WHOLE>
 __global__ __launch_bounds__(kBlock, 2) void paged_attention_kernel(ppk::PagedCache c, const T* __restrict__ q,
                                                                     int64_t ldq, T* __restrict__ out,
-                                                                    float* __restrict__ part, Split split, int groups,
+                                                                    float* __restrict__ part, char* __restrict__ joins,
+                                                                    Split split, int groups,
                                                                     float scale_log2) {
     using Tl = Tile<D, T, P>;
     constexpr bool kCodes = sizeof(P) == 1;
@@ -441,33 +451,56 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attention_kernel(ppk::PagedCa
         int seq, st, len, steps;
     };
     Lens lens = {split};
-    Where at;
+    Where at = {};
     int64_t left;
-    int head, range = 0;
+    const int all_heads = c.Hkv * groups;
+    const ppk::PagedPlace place = WHOLE ? ppk::PagedPlace{0, static_cast<int32_t>(blockIdx.x % all_heads)}
+                                        : ppk::paged_place(blockIdx.x, gridDim.x, wave, all_heads);
+    const int head = place.head, range = place.range;
+    if (!WHOLE && range >= split.ranges) return;
+    const int G = c.H / c.Hkv, kvh = head / groups, first = head % groups * kRows;
+    const int heads = min(G - first, kRows), h0 = kvh * G + first;   // this wavefront's query heads
+    auto zero = [&](int seq) {
+        if (ln >= heads) return;
+        T* y = out + (int64_t(seq) * c.H + h0 + ln) * D;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) Tl::put(y, 4 * g + r, [](int) { return 0.f; });
+    };
     bool begins = true;      // the piece starts with its sequence
     int piece = 0;
     if constexpr (WHOLE) {
-        head = blockIdx.x % (c.Hkv * groups);
-        at.seq = blockIdx.x / (c.Hkv * groups);
+        at.seq = blockIdx.x / all_heads;
         at.st = wave;
         at.len = ppk::paged_len(split.lens[at.seq], split.span);
         at.steps = ppk::paged_steps(at.len);
         left = (at.steps - wave + ppk::kPagedWaves - 1) / ppk::kPagedWaves;
     } else {
-        const ppk::PagedPlace place = ppk::paged_place(blockIdx.x, gridDim.x, wave, c.Hkv * groups);
-        head = place.head, range = place.range;
-        if (range >= split.ranges) return;
         const int64_t all = lens.total(), s0 = ppk::paged_start(range, all, split.ranges);
         left = ppk::paged_start(range + 1, all, split.ranges) - s0;
+        Join join = {-1, 0, 0, 0, 0, 0};
+        if (left > 0) {
+            at.seq = lens.holding(s0);
+            at.len = lens.length(at.seq);
+            at.steps = ppk::paged_steps(at.len);
+            at.st = at.steps - static_cast<int>(lens.end(at.seq) - s0);
+            if (at.st > 0) {
+                const int64_t begin = s0 - at.st;
+                const int r0 = ppk::paged_range(begin, all, split.ranges);
+                if (all < split.ranges)
+                    join = {at.seq, at.steps, at.st - 1, static_cast<int>(begin), 0, static_cast<int>(all)};
+                else
+                    join = {at.seq, ppk::paged_range(begin + at.steps - 1, all, split.ranges) - r0 + 1, range - r0 - 1, r0,
+                            ppk::paged_start(r0, all, split.ranges) == begin ? 0 : 1, 0};
+            }
+        }
+        if (head == 0 && lane == 0) *reinterpret_cast<Join*>(joins + range * kJoinBytes) = join;
+        if (range == 0) {   // sequences without keys: those before the first step here, the others behind the sequence before them
+            const int n = all > 0 ? lens.holding(0) : split.k;   // (this range may be empty itself)
+            for (int i = 0; i < n; ++i) zero(i);
+        }
         if (left <= 0) return;
-        at.seq = lens.holding(s0);
-        at.len = lens.length(at.seq);
-        at.steps = ppk::paged_steps(at.len);
-        at.st = at.steps - static_cast<int>(lens.end(at.seq) - s0);
         begins = at.st == 0;
     }
-    const int G = c.H / c.Hkv, kvh = head / groups, first = head % groups * kRows;
-    const int heads = min(G - first, kRows), h0 = kvh * G + first;   // this wavefront's query heads
 
     const uint32_t row_bytes = c.Hkv * D * sizeof(P);
     const char* kp = static_cast<const char*>(c.kp) + kvh * D * sizeof(P) + Tl::kcol(g);
@@ -614,6 +647,8 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attention_kernel(ppk::PagedCa
                 const bool ends = at.st + 1 == at.steps;
                 if (!more || ends) {
                     flush(at.seq, begins && ends);
+                    if (ends)
+                        for (int i = at.seq + 1; i < split.k && lens.length(i) == 0; ++i) zero(i);
                     clear();
                     begins = true, piece = 1;
                 }
@@ -634,7 +669,7 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attention_kernel(ppk::PagedCa
             for (int r = 0; r < 4; ++r) Tl::put(lds.o[wave][ln], 4 * g + r, [&](int j) { return o[j][r]; });
         }
         __syncthreads();
-        const int seq = blockIdx.x / (c.Hkv * groups);
+        const int seq = blockIdx.x / all_heads;
         for (int x = threadIdx.x; x < heads * D; x += kBlock) {
             const int h = x / D, d = x % D;
             float M = -INFINITY, S = 0.f, O = 0.f;
@@ -651,42 +686,27 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attention_kernel(ppk::PagedCa
     }
 }
 
-// The pieces of a sequence that spans ranges, in their order, and the zeros of one without keys: a workgroup takes `per`
-// query heads one after another, D / 4 lanes per piece.
+// The pieces of sequences that span ranges, in their order.  Workgroup r joins heads of the sequence that range r
+// continues, every (pieces - 1)th of them, so that all workgroups have about as much to read.
 constexpr int kJoin = 512;
 template <int D, typename T>
-__global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ part, T* __restrict__ out, Split split, int H,
-                                                     int per, float scale_log2) {
-    constexpr int LANES = D / 4, AT = kJoin / LANES;   // pieces at a time
+__global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ part, const char* __restrict__ joins,
+                                                     T* __restrict__ out, int ranges, int H, float scale_log2) {
+    constexpr int LANES = D / 4, AT = kJoin / LANES, PER = kWave / LANES;   // lanes of a piece; pieces at a time
     __shared__ float lm[AT], ll[AT];
     __shared__ f32x4 lo[AT][LANES];
-    const int chunks = (H + per - 1) / per, i = blockIdx.x / chunks, h0 = blockIdx.x % chunks * per;
-    Lens lens = {split};
-    const int64_t all = lens.total();
-    if (i >= 4 * kWave) {
-        int64_t base = lens.of_lane(lens.end3, 63);
-        for (int i0 = 4 * kWave; i0 <= i; i0 += 4 * kWave) base = lens.block(i0, base);
-    }
-    const int64_t s1 = lens.end(i), s0 = s1 - ppk::paged_steps(lens.length(i));   // the sequence's steps
-    const int w = threadIdx.x / LANES, d = threadIdx.x % LANES;
-    if (s0 == s1) {
-        for (int x = threadIdx.x; x < (min(h0 + per, H) - h0) * D; x += kJoin)
-            out[(int64_t(i) * H + h0) * D + x] = static_cast<T>(0.f);
-        return;
-    }
-    // With fewer steps than ranges some ranges are empty, and a step is a piece.
-    const bool sparse = all < split.ranges;
-    const int r0 = ppk::paged_range(s0, all, split.ranges);
-    const int n = sparse ? static_cast<int>(s1 - s0) : ppk::paged_range(s1 - 1, all, split.ranges) - r0 + 1;
-    if (n == 1) return;
-    const int piece0 = ppk::paged_start(r0, all, split.ranges) == s0 ? 0 : 1;
-    for (int h = h0; h < min(h0 + per, H); ++h) {
-        float m = -INFINITY, l = 0.f;
-        f32x4 o = {};
+    const Join j = *reinterpret_cast<const Join*>(joins + blockIdx.x * kJoinBytes);
+    if (j.seq < 0 || j.turn >= H) return;
+    const int d = threadIdx.x % LANES;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {};
+    // pieces from x0 on, every `step`th, of head h into m, l and o
+    auto gather = [&](int h, int x0, int step) {
+        m = -INFINITY, l = 0.f, o = f32x4{};
 #pragma unroll 4
-        for (int x = w; x < n; x += AT) {
-            const int r = sparse ? ppk::paged_range(s0 + x, all, split.ranges) : r0 + x;
-            const float* p = part + part_at<D>(r, x ? 0 : piece0, H, h);
+        for (int x = x0; x < j.pieces; x += step) {
+            const int r = j.steps ? ppk::paged_range(j.first + x, j.steps, ranges) : j.first + x;
+            const float* p = part + part_at<D>(r, x ? 0 : j.p0, H, h);
             const f32x4 xo = *reinterpret_cast<const f32x4*>(p + 4 * d);
             const float xm = p[D], xl = p[D + 1], M = fmaxf(m, xm);
             const float fa = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale_log2);
@@ -695,6 +715,32 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ p
             l = l * fa + xl * fb;
             m = M;
         }
+    };
+    auto write = [&](int h, float M, float L, const f32x4& O) {
+        T* y = out + (int64_t(j.seq) * H + h) * D + 4 * d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = static_cast<T>(M == -INFINITY ? 0.f : O[e] / L);
+    };
+    if (j.pieces <= 8 * PER) {   // a wavefront joins a head's few pieces by itself
+        const int w = threadIdx.x % kWave / LANES;
+        for (int h = j.turn + threadIdx.x / kWave * (j.pieces - 1); h < H; h += kJoin / kWave * (j.pieces - 1)) {
+            gather(h, w, PER);
+#pragma unroll
+            for (int s = LANES; s < kWave; s *= 2) {
+                const float M = fmaxf(m, __shfl_xor(m, s, kWave));
+                const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * scale_log2);
+                o *= f, l *= f, m = M;
+                l += __shfl_xor(l, s, kWave);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s, kWave);
+            }
+            if (w == 0) write(h, m, l, o);
+        }
+        return;
+    }
+    const int w = threadIdx.x / LANES;
+    for (int h = j.turn; h < H; h += j.pieces - 1) {
+        gather(h, w, AT);
         lo[w][d] = o;
         if (d == 0) lm[w] = m, ll[w] = l;
         __syncthreads();
@@ -709,9 +755,7 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ p
                 L += ll[x] * f;
                 O += lo[x][d] * f;
             }
-            T* y = out + (int64_t(i) * H + h) * D + 4 * d;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = static_cast<T>(M == -INFINITY ? 0.f : O[e] / L);
+            write(h, M, L, O);
         }
         __syncthreads();
     }
@@ -720,14 +764,14 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ p
 int heads_of(int H, int Hkv) { return Hkv * ((H / Hkv + kRows - 1) / kRows); }
 
 // Sequences that a table of kWhole positions bounds are a workgroup's each, if the workgroups find room at once.
-constexpr int kWhole = 512, kWholeBlocks = 256, kJoinBlocks = 2048;
+constexpr int kWhole = 512, kWholeBlocks = 256;
 
 }  // namespace
 
 namespace ppk {
 
 size_t paged_attention_workspace(int k, int H, int Hkv, int D) {
-    return k ? size_t(paged_ranges(heads_of(H, Hkv))) * 2 * H * (D + 4) * sizeof(float) : 0;
+    return k ? size_t(paged_ranges(heads_of(H, Hkv))) * (2 * H * (D + 4) * sizeof(float) + kJoinBytes) : 0;
 }
 
 void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const void* q, int64_t ldq, void* out,
@@ -736,7 +780,7 @@ void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const 
     const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(c.D));
     const Split split{lens, c.k, span, paged_ranges(heads), int64_t(c.k) * paged_steps(span) <= INT32_MAX};
     const bool whole = span <= kWhole && int64_t(c.k) * heads <= kWholeBlocks;
-    const int per = (int64_t(c.k) * c.H + kJoinBlocks - 1) / kJoinBlocks, chunks = (c.H + per - 1) / per;
+    char* joins = static_cast<char*>(part) + split.ranges * (2 * c.H * (c.D + 4) * sizeof(float));
     auto go = [&](auto d, auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
@@ -745,11 +789,11 @@ void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const 
         T* y = static_cast<T*>(out);
         float* f = static_cast<float*>(part);
         if (whole) {
-            paged_attention_kernel<D, T, P, true><<<c.k * heads, kBlock, 0, s>>>(c, x, ldq, y, f, split, groups, scale_log2);
+            paged_attention_kernel<D, T, P, true><<<c.k * heads, kBlock, 0, s>>>(c, x, ldq, y, f, joins, split, groups, scale_log2);
             return;
         }
-        paged_attention_kernel<D, T, P, false><<<paged_groups(heads), kBlock, 0, s>>>(c, x, ldq, y, f, split, groups, scale_log2);
-        join_kernel<D, T><<<c.k * chunks, kJoin, 0, s>>>(f, y, split, c.H, per, scale_log2);
+        paged_attention_kernel<D, T, P, false><<<paged_groups(heads), kBlock, 0, s>>>(c, x, ldq, y, f, joins, split, groups, scale_log2);
+        if (split.ranges > 1) join_kernel<D, T><<<split.ranges, kJoin, 0, s>>>(f, joins, y, split.ranges, c.H, scale_log2);
     };
     const std::integral_constant<int, 64> d64;
     const std::integral_constant<int, 128> d128;
