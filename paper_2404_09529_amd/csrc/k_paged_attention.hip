@@ -763,8 +763,11 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ p
 
 int heads_of(int H, int Hkv) { return Hkv * ((H / Hkv + kRows - 1) / kRows); }
 
-// Sequences that a table of kWhole positions bounds are a workgroup's each, if the workgroups find room at once.
-constexpr int kWhole = 512, kWholeBlocks = 256;
+// Sequences that a short table bounds are a workgroup's each, in one launch, if the workgroups find room at once.  Ranges
+// and their join, and this, in us: one sequence of 500 keys, 8 heads in bf16 10.5 and 8.0, of 1000 12.3 and 12.2, of 2000
+// 12.6 and 22.0; 8 bits, 1000: 13.4 and 11.5; eight sequences of up to 485 keys, 2 heads of 64 in float32, 9.1 and 9.3, of up
+// to 895 10.1 and 13.5.
+constexpr int kWhole = 1024, kWholeF32 = 512, kWholeBlocks = 256;
 
 }  // namespace
 
@@ -779,7 +782,7 @@ void paged_attention(int dtype, const PagedCache& c, const int32_t* lens, const 
     const int heads = heads_of(c.H, c.Hkv), groups = heads / c.Hkv, span = paged_span(c.max_pages, c.shift);
     const float scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(c.D));
     const Split split{lens, c.k, span, paged_ranges(heads), int64_t(c.k) * paged_steps(span) <= INT32_MAX};
-    const bool whole = span <= kWhole && int64_t(c.k) * heads <= kWholeBlocks;
+    const bool whole = span <= (c.kv_type == PP_KV_F32 ? kWholeF32 : kWhole) && int64_t(c.k) * heads <= kWholeBlocks;
     char* joins = static_cast<char*>(part) + split.ranges * (2 * c.H * (c.D + 4) * sizeof(float));
     auto go = [&](auto d, auto t, auto p) {
         using T = decltype(t);
