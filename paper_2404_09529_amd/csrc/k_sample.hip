@@ -8,8 +8,9 @@
 //   hist_kernel    a part of a row: its largest logit, E = ceil of its y, and the sum (and for top-k the count) of
 //                  every bin.  E is the part's own: parts differ by whole octaves, that is by shifts, so no pass over the
 //                  row has to come before to find its largest logit.
-//   gather_kernel  the parts' bins together; the bins in which the bounds are passed, or several where one bound depends
-//                  on another's exact place; the part's ids in these bins into the row's list.
+//   sum_kernel     the parts' bins together; the bins in which the bounds are passed, or several where one bound depends
+//                  on another's exact place.
+//   gather_kernel  a part's ids in these bins.
 //   pick_kernel    the list in order, running sums behind what the bins before hold, and the places themselves.  A list that is
 //                  too long (thousands of nearly equal logits) is resolved by descent through the logit's bits instead.
 // Rows are split into up to 16 parts, so that a few rows fill the chip: the logits are read three times, twice of them
@@ -25,9 +26,10 @@ namespace {
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
 constexpr int kUnitBits = 44, kPerOctave = 32;
 constexpr int kBins = 46 * kPerOctave;          // weights below 2^-45 are none
-constexpr int kScan = 3 * kThreads;             // bins as the threads hold them, three each
+constexpr int kWide = 1024;                     // threads of the kernels that have a workgroup per row
+constexpr int kScan = 2 * kWide;                // bins as they hold them, two each
 constexpr int kList = 4096, kMaxParts = 16;
-static_assert(kScan >= kBins, "three bins a thread");
+static_assert(kScan >= kBins, "two bins a thread");
 typedef unsigned long long u64;
 
 // Integers ordered as the logits are (NaN excepted); both zeros are one.
@@ -46,42 +48,72 @@ struct Powers {
     }
 };
 
+// How far an id's y is below the exponent E, in 64ths of an octave: a whole number, and what is left of it (|rest| <= 1/2).
+struct Depth {
+    int whole;
+    double rest;
+};
+constexpr int kNone = 1 << 30;   // as `whole`: NaN, -inf, or too far below
+constexpr double kRound = 0x1.8p52;   // added to a number it leaves the nearest whole one in the low bits
+
+// Rounded wherever E is large: unrounded in a fused operation it would not be E's own y.
+__device__ __forceinline__ double y_of(float x, double c) {
+#pragma clang fp contract(off)
+    const double y = static_cast<double>(x) * c;
+    return y;
+}
+__device__ __forceinline__ double exponent_of(float top, double c) { return top == INFINITY ? INFINITY : ceil(y_of(top, c)); }
+// Where one rounding instead of two makes no difference to whole octaves.  Rows beyond go by descent, parts beyond in other
+// rows have nothing that may be chosen.
+__device__ __forceinline__ bool near(double E) { return fabs(E) < 0x1p30; }
+
 struct Scale {
-    double c;   // log2(e) / T
-    double E;   // exponent of the unit's 2^44
-    // How far x's y is below E, in octaves; NaN and -inf and what is too far below give no number below 46.
-    __device__ __forceinline__ double depth(float x) const {
-#pragma clang fp contract(off)
-        if (E == INFINITY) return x == INFINITY ? 0.0 : 64.0;
-        return E - y_of(x, c);
+    double e64, c64;   // 64 E, -64 c with c = log2(e) / T
+    __device__ __forceinline__ Scale(double c, double E) : e64(64.0 * E), c64(-64.0 * c) {}
+    __device__ __forceinline__ double at(float x) const { return fma(static_cast<double>(x), c64, e64); }
+    // (beyond 46 octaves the low bits are not asked for; -inf times 0 is no number, and dropped by the first comparison)
+    __device__ __forceinline__ int whole(float x) const {
+        const double d = at(x);
+        return x > -INFINITY && d < 46.0 * 64.0 ? static_cast<int>(__double_as_longlong(d + kRound)) : kNone;
     }
-    // Rounded, here and in E: one unrounded in a fused operation would not be E's own y where that is large.
-    static __device__ __forceinline__ double y_of(float x, double c) {
-#pragma clang fp contract(off)
-        const double y = static_cast<double>(x) * c;
-        return y;
+    __device__ __forceinline__ Depth depth(float x) const {
+        const double d = at(x), z = d + kRound;
+        return {x > -INFINITY && d < 46.0 * 64.0 ? static_cast<int>(__double_as_longlong(z)) : kNone, d - (z - kRound)};
     }
 };
-__device__ __forceinline__ double exponent_of(float top, double c) { return top == INFINITY ? INFINITY : ceil(Scale::y_of(top, c)); }
+// The same for any E.
+struct AnyScale {
+    double c, E;
+    __device__ __forceinline__ Depth depth(float x) const {
+        if (near(E)) return Scale(c, E).depth(x);
+        if (E == INFINITY) return {x == INFINITY ? 0 : kNone, 0.0};
+        const double d = 64.0 * (E - y_of(x, c)), n = rint(d);
+        return {d < 46.0 * 64.0 ? static_cast<int>(n) : kNone, d - n};
+    }
+};
 __device__ __forceinline__ double scale_of(float t) { return 1.4426950408889634 / static_cast<double>(t); }
-__device__ __forceinline__ int bin_of(double depth) { return static_cast<int>(depth * kPerOctave); }
-__device__ __forceinline__ bool live(double depth) { return depth < 45.0; }   // false for NaN
+constexpr int kLive = 45 * 64;
+__device__ __forceinline__ bool live(const Depth& d) { return d.whole < kLive; }
+__device__ __forceinline__ int bin_of(const Depth& d) { return d.whole >> 1; }   // of a live id
 
-// 2^(44 - depth) rounded: a 64th of an octave from the table, the rest, |r| <= ln 2 / 128, by the exponential's
-// series to the fifth power (the next term is below 2^-54); adding 2^52 leaves the integer in the low bits.
-__device__ __forceinline__ double power(double depth, const Powers& p) {
-    const double z = -64.0 * depth, n = rint(z), r = (z - n) * (0.69314718055994531 / 64.0);
-    const int i = static_cast<int>(n);
-    double s = fma(r, 1.0 / 120.0, 1.0 / 24.0);
-    s = fma(s, r, 1.0 / 6.0);
-    s = fma(s, r, 0.5);
-    s = fma(s, r, 1.0);
-    const double t = p.at[i & 63];
-    return ldexp(fma(t, s * r, t), i >> 6);   // 2^-depth
+// 2^-depth as `scaled` times a power of two: a 64th of an octave from the table, the rest, |r| <= ln 2 / 128, by the
+// exponential's series to the fifth power (the next term is below 2^-54).
+__device__ __forceinline__ double series(const Depth& d, const Powers& p) {
+    constexpr double r = -0.69314718055994531 / 64.0;   // the rest times r is the exponent
+    double s = fma(d.rest, r * r * r * r * r / 120.0, r * r * r * r / 24.0);
+    s = fma(s, d.rest, r * r * r / 6.0);
+    s = fma(s, d.rest, r * r / 2.0);
+    s = fma(s, d.rest, r);
+    const double t = p.at[-d.whole & 63];
+    return fma(t, s * d.rest, t);
 }
-__device__ __forceinline__ u64 weight(double depth, const Powers& p) {
-    const double w = fma(power(depth, p), static_cast<double>(1ull << kUnitBits), 0x1p52);
-    return static_cast<u64>(__double_as_longlong(w)) & ((1ull << 52) - 1);
+// whole = 64 q - i with 0 <= i < 64: 2^-(whole / 64) = 2^(i / 64) 2^-q
+__device__ __forceinline__ int octave_of(const Depth& d) { return (d.whole + 63) >> 6; }
+__device__ __forceinline__ double power(const Depth& d, const Powers& p) { return ldexp(series(d, p), -octave_of(d)); }
+// 2^(44 - depth) rounded: adding 2^52 leaves the whole number in the low bits.
+__device__ __forceinline__ u64 weight(const Depth& d, const Powers& p) {
+    const double unit = __hiloint2double((1023 + kUnitBits - octave_of(d)) << 20, 0);   // 2^(44 - octave)
+    return static_cast<u64>(__double_as_longlong(fma(series(d, p), unit, 0x1p52))) & ((1ull << 52) - 1);
 }
 
 // ------------------------------------------------------------------------------- a row's settings and workspace
@@ -102,6 +134,10 @@ __device__ __forceinline__ Settings settings_of(const ppk::Sample& a, int row) {
     s.u = u >= 0.f ? static_cast<double>(u) : 0.0;
     return s;
 }
+// exp((x - top) / T), as min-p asks for it.
+__device__ __forceinline__ double share_of(float x, float top, const Settings& s) {
+    return x == top ? 1.0 : exp((static_cast<double>(x) - static_cast<double>(top)) / static_cast<double>(s.t));
+}
 // The bound that the chosen id's running sum exceeds; it is below the sum.
 __device__ __forceinline__ double choice_bound(double u, double sum) {
     const double below = nextafter(sum, 0.0);
@@ -116,49 +152,63 @@ struct Part {   // of a row, by hist_kernel
 struct Plan {   // of a row, by gather_kernel
     double E;
     float top;
-    int listed;       // ids in the list, also those that found no room; cleared by hist_kernel
     int k_bin;        // top-k's bin (-1: no limit), and the ids before it
     int k_before;
-    int m_bin;        // first bin in which min_p's border may lie
+    int p0, p1, m0, m1, s0, s1;   // first and last bin in which top-p's, min-p's and the choice's place may lie
     u64 all;
     u64 before[kBins];
-    u64 list[kList];
 };
 struct Space {
     u64* sum;         // [k][parts][kBins]
     uint32_t* count;  // [k][parts][kBins]
     Part* part;       // [k][parts]
     Plan* plan;       // [k]
+    u64* list;        // [k][parts][room]: a part's ids in the bins that matter
+    int* listed;      // [k][parts]: how many there are, also those that found no room
 };
+// Room for a part's ids: a quarter of what pick_kernel takes, or all of it for a row that is one part.
+__host__ __device__ constexpr int room_of(int parts) { return parts == 1 ? kList : kList / 4; }
+
 size_t space_bytes(int k, int parts) {
-    return size_t(k) * parts * (kBins * 12 + sizeof(Part)) + size_t(k) * sizeof(Plan);
+    return size_t(k) * parts * (kBins * 12 + sizeof(Part) + room_of(parts) * 8 + 4) + size_t(k) * sizeof(Plan);
 }
 Space space_at(void* ws, int k, int parts) {
     Space s;
     s.plan = static_cast<Plan*>(ws);
     s.sum = reinterpret_cast<u64*>(s.plan + k);
-    s.part = reinterpret_cast<Part*>(s.sum + size_t(k) * parts * kBins);
+    s.list = s.sum + size_t(k) * parts * kBins;
+    s.part = reinterpret_cast<Part*>(s.list + size_t(k) * parts * room_of(parts));
     s.count = reinterpret_cast<uint32_t*>(s.part + size_t(k) * parts);
+    s.listed = reinterpret_cast<int*>(s.count + size_t(k) * parts * kBins);
     return s;
 }
 
-// f(x, id) for the ids v0 <= id < v1 of a row, eight loads of a thread in flight.
-template <typename F>
+// U logits of a thread of N, ids v0 + threadIdx.x + i N, all in flight at once; NaN, which is never chosen, from v1 on.
+template <int U, int N = kThreads>
+__device__ __forceinline__ void read(const float* x, int v0, int v1, float (&y)[U]) {
+    const int v = v0 + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < U; ++i) y[i] = x[min(v + i * N, v1 - 1)];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+        if (v + i * N >= v1) y[i] = __uint_as_float(0x7fc00000u);
+}
+// f(x, id) for these ids, and some NaN.
+template <int U, int N = kThreads, typename F>
 __device__ __forceinline__ void over(const float* x, int v0, int v1, F f) {
-    int v = v0 + threadIdx.x;
-    for (; v + 7 * kThreads < v1; v += 8 * kThreads) {
-        float y[8];
+    for (; v0 < v1; v0 += U * N) {
+        float y[U];
+        read<U, N>(x, v0, v1, y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[v + i * kThreads];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f(y[i], v + i * kThreads);
+        for (int i = 0; i < U; ++i) f(y[i], v0 + static_cast<int>(threadIdx.x) + i * N);
     }
-    for (; v < v1; v += kThreads) f(x[v], v);
 }
 
 __device__ __forceinline__ bool above(float t, int i, float u, int j) { return t > u || (t == u && i < j); }
 
-__global__ __launch_bounds__(kThreads) void hist_kernel(ppk::Sample a, Space s, int parts, int size) {
+// A part of up to U kThreads ids is read once.
+template <int U>
+__global__ __launch_bounds__(kThreads, 4) void hist_kernel(ppk::Sample a, Space s, int parts, int size) {
     __shared__ u64 sum[kBins];
     __shared__ uint32_t count[kBins];
     __shared__ Powers powers;
@@ -171,7 +221,18 @@ __global__ __launch_bounds__(kThreads) void hist_kernel(ppk::Sample a, Space s, 
     powers.fill();
     float top = -INFINITY;
     int id = INT32_MAX;
-    over(x, v0, v1, [&](float y, int v) {
+    float held[U];
+    const bool once = v1 - v0 <= U * kThreads;
+    auto each = [&](auto f) {
+        if (once) {
+#pragma unroll
+            for (int i = 0; i < U; ++i) f(held[i], v0 + tid + i * kThreads);
+        } else {
+            over<U>(x, v0, v1, f);
+        }
+    };
+    if (once) read(x, v0, v1, held);
+    each([&](float y, int v) {
         if (y > top || (y == top && id == INT32_MAX)) top = y, id = v;   // (a thread's ids ascend)
     });
 #pragma unroll
@@ -187,15 +248,13 @@ __global__ __launch_bounds__(kThreads) void hist_kernel(ppk::Sample a, Space s, 
         if (above(tops[w], ids[w], top, id)) top = tops[w], id = ids[w];
     const double c = scale_of(set.t);
     const bool none = set.greedy || top == -INFINITY;
-    const Scale sc = {c, none ? -INFINITY : exponent_of(top, c)};
-    if (tid == 0) {
-        s.part[blockIdx.x] = {sc.E, top, id};
-        if (blockIdx.x % parts == 0) s.plan[row].listed = 0;
-    }
-    if (none) return;
+    const double E = none ? -INFINITY : exponent_of(top, c);
+    if (tid == 0) s.part[blockIdx.x] = {E, top, id};
+    if (!near(E)) return;
+    const Scale sc(c, E);
     const bool counted = set.top_k > 0;
-    over(x, v0, v1, [&](float y, int) {
-        const double d = sc.depth(y);
+    each([&](float y, int) {
+        const Depth d = sc.depth(y);
         if (!live(d)) return;
         const u64 w = weight(d, powers);
         atomicAdd(&sum[bin_of(d)], w);
@@ -210,8 +269,8 @@ __global__ __launch_bounds__(kThreads) void hist_kernel(ppk::Sample a, Space s, 
 }
 
 // ------------------------------------------------------------------------------- scans of a workgroup
-template <typename T>
-__device__ __forceinline__ T block_scan(T mine, T* waves) {   // up to and including this thread
+template <int W, typename T>
+__device__ __forceinline__ T block_scan(T mine, T* waves) {   // up to and including this thread of W wavefronts
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
@@ -222,7 +281,7 @@ __device__ __forceinline__ T block_scan(T mine, T* waves) {   // up to and inclu
     if (lane == kWave - 1) waves[w] = mine;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i)
+    for (int i = 0; i < W; ++i)
         if (i < w) mine += waves[i];
     return mine;
 }
@@ -233,83 +292,98 @@ struct Whole {
     float top;
     int id;
 };
-__device__ __forceinline__ Whole whole_of(const Part* p, int parts) {
-    Whole w = {-INFINITY, -INFINITY, INT32_MAX};
-    for (int i = 0; i < parts; ++i) {
-        const Part q = p[i];
-        if (above(q.top, q.id, w.top, w.id)) w.top = q.top, w.id = q.id;
-        w.E = fmax(w.E, q.E);
+__device__ __forceinline__ Whole whole_of(const Part* p, int parts) {   // by every wavefront for itself
+    const Part q = p[min(static_cast<int>(threadIdx.x % kMaxParts), parts - 1)];
+    Whole w = {q.E, q.top, q.id};
+#pragma unroll
+    for (int o = kMaxParts / 2; o > 0; o >>= 1) {
+        const float t = __shfl_xor(w.top, o, kWave);
+        const int i = __shfl_xor(w.id, o, kWave);
+        if (above(t, i, w.top, w.id)) w.top = t, w.id = i;
+        w.E = fmax(w.E, __shfl_xor(w.E, o, kWave));
     }
     return w;
 }
 // Octaves from one exponent down to another, both whole numbers.
 __device__ __forceinline__ int octaves(double E, double part) { return E == part ? 0 : static_cast<int>(fmin(E - part, 64.0)); }
 
-__global__ __launch_bounds__(kThreads) void gather_kernel(ppk::Sample a, Space s, int parts, int size) {
+__global__ __launch_bounds__(kWide) void sum_kernel(ppk::Sample a, Space s, int parts) {
     __shared__ u64 sums[kScan + 1];        // of the bins before each
     __shared__ uint32_t counts[kScan + 1];
-    __shared__ u64 found[kList / 2];
-    __shared__ u64 wave_sums[kWaves];
-    __shared__ uint32_t wave_counts[kWaves];
-    __shared__ int at[6], listed, base;
-    const int row = blockIdx.x / parts, part = blockIdx.x % parts, tid = threadIdx.x;
+    __shared__ u64 wave_sums[kWide / kWave];
+    __shared__ uint32_t wave_counts[kWide / kWave];
+    __shared__ int at[5], shifts[kMaxParts];
+    const int row = blockIdx.x, tid = threadIdx.x;
     const Settings set = settings_of(a, row);
-    if (set.greedy) return;
     const Part* ps = s.part + int64_t(row) * parts;
     const Whole w = whole_of(ps, parts);
-    if (w.E == -INFINITY) return;
-    // the bins of all parts: three neighbours a thread
-    u64 sum[3] = {0, 0, 0};
-    uint32_t count[3] = {0, 0, 0};
-    for (int p = 0; p < parts; ++p) {
-        if (ps[p].E == -INFINITY) continue;
-        const int shift = octaves(w.E, ps[p].E);
-        const int64_t src = (int64_t(row) * parts + p) * kBins - kPerOctave * shift;
+    Plan* plan = s.plan + row;
+    if (tid == 0) plan->E = w.E, plan->top = w.top;
+    if (set.greedy || !near(w.E)) return;
+    if (tid < parts) shifts[tid] = near(ps[tid].E) ? octaves(w.E, ps[tid].E) : 64;
+    if (tid < 5) at[tid] = kBins - 1;
+    __syncthreads();
+    // the bins of all parts, one wait for memory
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            const int b = 3 * tid + i;
-            if (shift >= 46 || b >= kBins || b < kPerOctave * shift) continue;
-            sum[i] += s.sum[src + b] >> shift;
-            if (set.top_k) count[i] += s.count[src + b];
+    for (int i = 0; i < 2; ++i) {
+        const int b = tid + i * kWide;
+        u64 x[kMaxParts], t = 0;
+        uint32_t c[kMaxParts], n = 0;
+        const int64_t src = int64_t(row) * parts * kBins;
+#pragma unroll
+        for (int p = 0; p < kMaxParts; ++p) {
+            if (p >= parts) break;
+            const int64_t from = src + p * kBins + min(max(b - kPerOctave * shifts[p], 0), kBins - 1);
+            x[p] = s.sum[from];
+            c[p] = set.top_k ? s.count[from] : 0;
         }
+#pragma unroll
+        for (int p = 0; p < kMaxParts; ++p) {
+            if (p >= parts) break;
+            const int from = b - kPerOctave * shifts[p];   // (a part without anything, 64 octaves down, has written no bins)
+            if (from >= 0 && from < kBins) t += x[p] >> shifts[p], n += c[p];
+        }
+        sums[b] = t, counts[b] = n;
     }
-    const u64 se = block_scan(sum[0] + sum[1] + sum[2], wave_sums);
-    const uint32_t ce = block_scan(count[0] + count[1] + count[2], wave_counts);
-    sums[3 * tid + 3] = se, sums[3 * tid + 2] = se - sum[2], sums[3 * tid + 1] = se - sum[2] - sum[1];
-    counts[3 * tid + 3] = ce, counts[3 * tid + 2] = ce - count[2], counts[3 * tid + 1] = ce - count[2] - count[1];
-    if (tid == 0) sums[0] = 0, counts[0] = 0, listed = 0;
-    if (tid < 6) at[tid] = kBins - 1;
+    __syncthreads();
+    // two neighbours a thread
+    const u64 sum0 = sums[2 * tid], sum1 = sums[2 * tid + 1];
+    const uint32_t count0 = counts[2 * tid], count1 = counts[2 * tid + 1];
+    const u64 se = block_scan<kWide / kWave>(sum0 + sum1, wave_sums);
+    const uint32_t ce = set.top_k ? block_scan<kWide / kWave>(count0 + count1, wave_counts) : 0;
+    sums[2 * tid + 2] = se, sums[2 * tid + 1] = se - sum1;
+    counts[2 * tid + 2] = ce, counts[2 * tid + 1] = ce - count1;
+    if (tid == 0) sums[0] = 0, counts[0] = 0;
     __syncthreads();
     const u64 all = sums[kScan];
-    // at[slot]: the bin in which the sum (or count) passes the bound
+    // at[slot]: the bin in which the sum (or count) passes the bound; a barrier follows
     auto passing = [&](int slot, auto before, auto bound) {
 #pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            const int b = 3 * tid + i;
+        for (int i = 0; i < 2; ++i) {
+            const int b = 2 * tid + i;
             if (!bound(before[b]) && bound(before[b + 1])) at[slot] = b;   // one thread
         }
-        __syncthreads();
     };
-    // bins: top-k's; top-p's first and last; min-p's first and last; the choice's first and last
-    const bool has_k = set.top_k > 0 && static_cast<uint32_t>(set.top_k) < counts[kScan], has_p = set.top_p < 1.0;
     u64 lo = all, hi = all;   // of what is kept
     int bk = -1;
-    if (has_k) {
+    if (set.top_k > 0 && static_cast<uint32_t>(set.top_k) < counts[kScan]) {
         passing(0, counts, [&](uint32_t n) { return n >= static_cast<uint32_t>(set.top_k); });
+        __syncthreads();
         bk = at[0];
         lo = sums[bk], hi = sums[bk + 1];
     }
     int p0 = 0, p1 = -1, m0 = 0, m1 = -1;
-    if (has_p) {
+    if (set.top_p < 1.0) {
         const double t0 = fmax(set.top_p * static_cast<double>(lo), 1.0), t1 = fmax(set.top_p * static_cast<double>(hi), 1.0);
         passing(1, sums, [&](u64 n) { return static_cast<double>(n) >= t0; });
         passing(2, sums, [&](u64 n) { return static_cast<double>(n) >= t1; });
+        __syncthreads();
         p0 = at[1], p1 = at[2];
         lo = min(lo, sums[p0]), hi = min(hi, sums[p1 + 1]);
     }
     if (set.min_p > 0.0) {
         // 2^-depth = min_p 2^-depth(top), one bin more on both sides
-        const double d = Scale{scale_of(set.t), w.E}.depth(w.top) - log2(set.min_p);
+        const double d = Scale(scale_of(set.t), w.E).at(w.top) / 64.0 - log2(set.min_p);
         const int b = static_cast<int>(fmin(d, 46.0) * kPerOctave);
         m0 = min(max(b - 1, 0), kBins - 1), m1 = min(b + 1, kBins - 1);
         lo = min(lo, sums[m0]), hi = min(hi, sums[m1 + 1]);
@@ -317,36 +391,71 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(ppk::Sample a, Space s
     const double u0 = choice_bound(set.u, fmax(static_cast<double>(lo), 1.0)), u1 = choice_bound(set.u, static_cast<double>(hi));
     passing(3, sums, [&](u64 n) { return static_cast<double>(n) > u0; });
     passing(4, sums, [&](u64 n) { return static_cast<double>(n) > u1; });
-    const int s0 = at[3], s1 = at[4];
+    __syncthreads();
+    for (int b = tid; b < kBins; b += kWide) plan->before[b] = sums[b];
+    if (tid == 0) {
+        plan->k_bin = bk, plan->k_before = bk >= 0 ? static_cast<int>(counts[bk]) : 0;
+        plan->p0 = p0, plan->p1 = p1, plan->m0 = m0, plan->m1 = m1, plan->s0 = at[3], plan->s1 = at[4];
+        plan->all = all;
+    }
+}
 
-    Plan* plan = s.plan + row;
-    if (part == 0) {
-        for (int b = tid; b < kBins; b += kThreads) plan->before[b] = sums[b];
-        if (tid == 0) {
-            plan->E = w.E, plan->top = w.top, plan->m_bin = m0, plan->all = all;
-            plan->k_bin = bk, plan->k_before = bk >= 0 ? static_cast<int>(counts[bk]) : 0;
+template <int U>
+__global__ __launch_bounds__(kThreads, 4) void gather_kernel(ppk::Sample a, Space s, int parts, int size) {
+    __shared__ int listed;
+    const int row = blockIdx.x / parts, tid = threadIdx.x, v0 = blockIdx.x % parts * size, v1 = min(v0 + size, a.vocab);
+    const float* x = a.logits + row * a.ldl;
+    float held[U];
+    read(x, v0, v1, held);
+    const float t = a.temperature ? a.temperature[row] : 1.f;
+    const Plan* plan = s.plan + row;
+    const double E = plan->E, part_E = s.part[blockIdx.x].E;
+    const int bk = plan->k_bin, p0 = plan->p0, p1 = plan->p1, m0 = plan->m0, m1 = plan->m1, s0 = plan->s0, s1 = plan->s1;
+    if (!(t > 0.f)) return;   // (greedy: of the plan nothing is there but E)
+    if (!near(E)) {
+        if (tid == 0) s.listed[blockIdx.x] = kList + 1;
+        return;
+    }
+    if (tid == 0) listed = 0;
+    __syncthreads();
+    const int room = room_of(parts);
+    u64* list = s.list + int64_t(blockIdx.x) * room;
+    if (near(part_E)) {
+        const Scale sc(scale_of(t), part_E);
+        const int shift = octaves(E, part_E) * kPerOctave, lane = tid % kWave;
+        // A thread's hits of U ids as bits, the wavefront's in one reservation.
+        auto chunk = [&](const float (&y)[U], int first) {
+            uint32_t hits = 0;
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int whole = sc.whole(y[i]), b = (whole >> 1) + shift;
+                const bool hit = b == bk || (b >= p0 && b <= p1) || (b >= m0 && b <= m1) || (b >= s0 && b <= s1);
+                hits |= uint32_t(whole < kLive && hit) << i;
+            }
+            int n = __popc(hits), end = n;
+#pragma unroll
+            for (int o = 1; o < kWave; o <<= 1) {
+                const int up = __shfl_up(end, o, kWave);
+                if (lane >= o) end += up;
+            }
+            int base = 0;
+            if (lane == kWave - 1 && end) base = atomicAdd(&listed, end);
+            int to = __shfl(base, kWave - 1, kWave) + end - n;
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                if (hits >> i & 1) {
+                    if (to < room) list[to] = u64(~key_of(y[i])) << 32 | static_cast<uint32_t>(first + i * kThreads);
+                    ++to;
+                }
+        };
+        for (int v = v0;;) {
+            chunk(held, v + tid);
+            if ((v += U * kThreads) >= v1) break;
+            read(x, v, v1, held);
         }
     }
-    if (ps[part].E == -INFINITY) return;
-    const Scale sc = {scale_of(set.t), ps[part].E};
-    const int shift = octaves(w.E, sc.E) * kPerOctave;
-    const int v0 = part * size;
-    over(a.logits + row * a.ldl, v0, min(v0 + size, a.vocab), [&](float y, int v) {
-        const double d = sc.depth(y);
-        if (!live(d)) return;
-        const int b = bin_of(d) + shift;
-        if (b == bk || (b >= p0 && b <= p1) || (b >= m0 && b <= m1) || (b >= s0 && b <= s1)) {
-            const int n = atomicAdd(&listed, 1);
-            if (n < kList / 2) found[n] = u64(~key_of(y)) << 32 | static_cast<uint32_t>(v);
-        }
-    });
     __syncthreads();
-    // a part with more than half the list's room: the list is too long, or is taken to be
-    const int n = listed;
-    if (tid == 0 && n) base = atomicAdd(&plan->listed, n > kList / 2 ? kList + 1 : n);
-    __syncthreads();
-    for (int i = tid; i < min(n, kList / 2); i += kThreads)
-        if (base + i < kList) plan->list[base + i] = found[i];
+    if (tid == 0) s.listed[blockIdx.x] = listed;
 }
 
 // ------------------------------------------------------------------------------- descent
@@ -366,15 +475,15 @@ struct Place {
 struct Descent {
     u64 sum[256];
     uint32_t count[256];
-    u64 wave_sum[kWaves];
-    uint32_t wave_count[kWaves];
+    u64 wave_sum[kWide / kWave];
+    uint32_t wave_count[kWide / kWave];
     int digit, found;
     u64 above_sum;
     uint32_t above_count;
 };
 
 // The first place, in order, where the running count or sum passes the bound; there is one.
-__device__ Place find(const float* x, int vocab, const Scale& sc, const Powers& powers, Bound what, double bound, Descent& lds) {
+__device__ Place find(const float* x, int vocab, const AnyScale& sc, const Powers& powers, Bound what, double bound, Descent& lds) {
     const int tid = threadIdx.x, lane = tid % kWave;
     uint32_t prefix = 0, mask = 0, above_n = 0;
     u64 above_s = 0;
@@ -382,10 +491,10 @@ __device__ Place find(const float* x, int vocab, const Scale& sc, const Powers& 
         __syncthreads();
         if (tid < 256) lds.sum[tid] = 0, lds.count[tid] = 0;
         __syncthreads();
-        over(x, 0, vocab, [&](float y, int) {
+        over<4, kWide>(x, 0, vocab, [&](float y, int) {
             const uint32_t k = key_of(y);
             if ((k & mask) != prefix) return;
-            const double d = sc.depth(y);
+            const Depth d = sc.depth(y);
             if (!live(d)) return;
             atomicAdd(&lds.sum[(k >> shift) & 255], weight(d, powers));
             atomicAdd(&lds.count[(k >> shift) & 255], 1u);
@@ -393,8 +502,8 @@ __device__ Place find(const float* x, int vocab, const Scale& sc, const Powers& 
         __syncthreads();
         const u64 s = tid < 256 ? lds.sum[255 - tid] : 0;   // digits from 255 down
         const uint32_t n = tid < 256 ? lds.count[255 - tid] : 0;
-        const u64 es = above_s + block_scan(s, lds.wave_sum);
-        const uint32_t en = above_n + block_scan(n, lds.wave_count);
+        const u64 es = above_s + block_scan<kWide / kWave>(s, lds.wave_sum);
+        const uint32_t en = above_n + block_scan<kWide / kWave>(n, lds.wave_count);
         if (tid < 256 && !passes(what, es - s, en - n, bound) && passes(what, es, en, bound))
             lds.digit = 255 - tid, lds.above_sum = es - s, lds.above_count = en - n;
         __syncthreads();
@@ -411,14 +520,14 @@ __device__ Place find(const float* x, int vocab, const Scale& sc, const Powers& 
         else lo = mid + 1;
     }
     uint32_t before = 0;
-    for (int v0 = 0; v0 < vocab; v0 += kThreads) {
+    for (int v0 = 0; v0 < vocab; v0 += kWide) {
         const bool is = v0 + tid < vocab && x[v0 + tid] == v;
         const u64 here = __ballot(is);
         __syncthreads();
         if (lane == 0) lds.wave_count[tid / kWave] = __popcll(here);
         __syncthreads();
         uint32_t mine = before, all = 0;
-        for (int i = 0; i < kWaves; ++i) {
+        for (int i = 0; i < (kWide / kWave); ++i) {
             if (i < tid / kWave) mine += lds.wave_count[i];
             all += lds.wave_count[i];
         }
@@ -432,21 +541,21 @@ __device__ Place find(const float* x, int vocab, const Scale& sc, const Powers& 
     return {id, above_s + w * lo, v};
 }
 
-__device__ Place descend(const float* x, int vocab, const Settings& set, const Scale& sc, float top, const Powers& powers,
+__device__ Place descend(const float* x, int vocab, const Settings& set, const AnyScale& sc, float top, const Powers& powers,
                          Descent& lds) {
     u64 all = 0, likely = 0;
     uint32_t count = 0;
-    over(x, 0, vocab, [&](float y, int) {
-        const double d = sc.depth(y);
+    over<4, kWide>(x, 0, vocab, [&](float y, int) {
+        const Depth d = sc.depth(y);
         if (!live(d)) return;
         const u64 w = weight(d, powers);
         all += w, ++count;
-        if (y == top || power(d - sc.depth(top), powers) >= set.min_p) likely += w;
+        if (share_of(y, top, set) >= set.min_p) likely += w;
     });
     auto total = [&](auto v, auto* waves) {
-        v = block_scan(v, waves);
+        v = block_scan<kWide / kWave>(v, waves);
         __syncthreads();
-        if (threadIdx.x == kThreads - 1) waves[0] = v;
+        if (threadIdx.x == kWide - 1) waves[0] = v;
         __syncthreads();
         v = waves[0];
         __syncthreads();
@@ -465,15 +574,16 @@ __device__ Place descend(const float* x, int vocab, const Settings& set, const S
 }
 
 // ------------------------------------------------------------------------------- the choice
-__global__ __launch_bounds__(kThreads) void pick_kernel(ppk::Sample a, Space s, int parts) {
+__global__ __launch_bounds__(kWide) void pick_kernel(ppk::Sample a, Space s, int parts) {
     __shared__ u64 list[kList];   // what of the order stands in the id's stead: ~key, id
-    __shared__ u64 run[kList];    // running sums of the list's weights
+    __shared__ u64 run[kList];    // running sums
+    __shared__ uint16_t bins[kList];
     __shared__ union {
         Descent descent;
-        u64 waves[kWaves];
+        u64 waves[kWide / kWave];
     } lds;
     __shared__ Powers powers;
-    __shared__ int first;
+    __shared__ int first, starts[kMaxParts + 1];
     __shared__ u64 likely;
     const int row = blockIdx.x, tid = threadIdx.x;
     const Settings set = settings_of(a, row);
@@ -489,9 +599,20 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(ppk::Sample a, Space s, 
     }
     powers.fill();
     const Plan* plan = s.plan + row;
-    const Scale sc = {scale_of(set.t), plan->E};
+    const AnyScale sc = {scale_of(set.t), plan->E};
     const float top = plan->top;
-    const int n = plan->listed;
+    // the parts' lists, one behind the other
+    if (tid == 0) {
+        int all = 0;
+        for (int p = 0; p < parts; ++p) {
+            const int c = s.listed[int64_t(row) * parts + p];
+            starts[p] = all;
+            all = c > room_of(parts) || all + c > kList ? kList + 1 : all + c;
+        }
+        starts[parts] = all;
+    }
+    __syncthreads();
+    const int n = starts[parts];
     auto write = [&](int id, float x, u64 kept) {   // by one thread
         a.tokens[row] = id;
         if (a.prob)
@@ -503,49 +624,70 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(ppk::Sample a, Space s, 
         if (tid == 0) write(p.id, p.x, p.sum);
         return;
     }
-    // bitonic sort of the next power of two, two values a thread and step at most kList / kThreads / 2 times
+    // Bitonic sort of the next power of two.  Pairs up to 64 apart lie within a wavefront's own 128 values, which it
+    // writes and reads in order: only the wider ones wait for the others.
     int m = 64;
     while (m < n) m *= 2;
-    for (int i = tid; i < m; i += kThreads) list[i] = i < n ? plan->list[i] : ~0ull;
+    for (int i = n + tid; i < m; i += kWide) list[i] = ~0ull;
+    for (int p = tid / kWave; p < parts; p += (kWide / kWave))   // a wavefront copies a part's
+        for (int i = starts[p] + tid % kWave; i < starts[p + 1]; i += kWave)
+            list[i] = s.list[(int64_t(row) * parts + p) * room_of(parts) + i - starts[p]];
+    __syncthreads();
+    bool wide = false;
     for (int size = 2; size <= m; size *= 2)
         for (int stride = size / 2; stride > 0; stride /= 2) {
-            __syncthreads();
-            for (int i = tid; i < m / 2; i += kThreads) {
+            if (stride > kWave || wide) __syncthreads();
+            wide = stride > kWave;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int i = tid; i < m / 2; i += kWide) {
                 const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
                 const u64 x = list[lo], y = list[hi];
                 if ((x > y) == ((lo & size) == 0)) list[lo] = y, list[hi] = x;
             }
         }
     __syncthreads();
-    // running sums: eight neighbours a thread
-    const int per = (m + kThreads - 1) / kThreads;
+    // Sums of all ids up to each entry: the bins before its own, and the list's entries of its bin.  Eight neighbours a
+    // thread at most: where its first bin started is a thread before's to know.
+    const int per = (m + kWide - 1) / kWide, i0 = tid * per, i1 = min(i0 + per, n);
     auto x_of = [&](int i) { return of_key(~static_cast<uint32_t>(list[i] >> 32)); };
     u64 mine = 0;
-    for (int i = tid * per; i < min(tid * per + per, n); ++i) mine += weight(sc.depth(x_of(i)), powers);
-    u64 sum = block_scan(mine, lds.waves) - mine;
-    for (int i = tid * per; i < min(tid * per + per, n); ++i) run[i] = sum += weight(sc.depth(x_of(i)), powers);
-    if (tid == 0) likely = plan->before[plan->m_bin];
+    for (int i = i0; i < i1; ++i) {
+        const Depth d = sc.depth(x_of(i));
+        run[i] = mine += weight(d, powers);
+        bins[i] = static_cast<uint16_t>(min(bin_of(d), kBins - 1));
+    }
+    const u64 ahead = block_scan<kWide / kWave>(mine, lds.waves) - mine;
+    for (int i = i0; i < i1; ++i) run[i] += ahead;
+    if (tid == 0) likely = plan->before[plan->m0];
     __syncthreads();
-    struct Sum {
-        u64 sum;    // of all ids up to list entry i: the bins before its own, and the list's entries of its bin
-        int bin, rank;   // among the bin's
-    };
-    auto upto = [&](int i) {
-        const int b = bin_of(sc.depth(x_of(i)));
-        int lo = 0, hi = i;   // the first entry of the bin
+    // the first entry of entry i's bin
+    auto start = [&](int i) {
+        int lo = 0, hi = i;
         while (lo < hi) {
             const int mid = (lo + hi) / 2;
-            if (bin_of(sc.depth(x_of(mid))) < b) lo = mid + 1;
+            if (bins[mid] < bins[i]) lo = mid + 1;
             else hi = mid;
         }
-        return Sum{plan->before[min(b, kBins - 1)] + run[i] - (lo ? run[lo - 1] : 0), b, i - lo};
+        return lo;
     };
+    u64 total[kList / kWide];
+#pragma unroll
+    for (int j = 0; j < kList / kWide; ++j) {
+        const int i = tid + j * kWide;
+        if (i >= n) break;
+        const int lo = start(i);
+        total[j] = plan->before[bins[i]] + run[i] - (lo ? run[lo - 1] : 0);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kList / kWide; ++j)
+        if (tid + j * kWide < n) run[tid + j * kWide] = total[j];
     // The first entry that passes; the last one if a sum of parts and one of ids differ in their last bits just here.
     auto place = [&](auto bound) {
         __syncthreads();
         if (tid == 0) first = n - 1;
         __syncthreads();
-        for (int i = tid; i < n; i += kThreads)
+        for (int i = tid; i < n; i += kWide)
             if (bound(i)) {
                 atomicMin(&first, i);
                 break;
@@ -555,24 +697,21 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(ppk::Sample a, Space s, 
     };
     u64 kept = plan->all;
     if (plan->k_bin >= 0) {
-        const int rank = set.top_k - plan->k_before - 1;
-        kept = upto(place([&](int i) {
-            const Sum e = upto(i);
-            return e.bin == plan->k_bin && e.rank == rank;
-        })).sum;
+        const int rank = set.top_k - plan->k_before - 1, bin = plan->k_bin;
+        kept = run[place([&](int i) { return bins[i] == bin && i - start(i) == rank; })];
     }
     if (set.top_p < 1.0) {
         const double bound = fmax(set.top_p * static_cast<double>(kept), 1.0);
-        kept = upto(place([&](int i) { return static_cast<double>(upto(i).sum) >= bound; })).sum;
+        kept = run[place([&](int i) { return static_cast<double>(run[i]) >= bound; })];
     }
     if (set.min_p > 0.0) {
-        for (int i = tid; i < n; i += kThreads)
-            if (power(sc.depth(x_of(i)) - sc.depth(top), powers) >= set.min_p) atomicMax(&likely, upto(i).sum);
+        for (int i = tid; i < n; i += kWide)
+            if (share_of(x_of(i), top, set) >= set.min_p) atomicMax(&likely, run[i]);
         __syncthreads();
         kept = min(kept, likely);
     }
     const double bound = choice_bound(set.u, static_cast<double>(kept));
-    const int i = place([&](int j) { return static_cast<double>(upto(j).sum) > bound; });
+    const int i = place([&](int j) { return static_cast<double>(run[j]) > bound; });
     if (tid == 0) write(static_cast<int>(static_cast<uint32_t>(list[i])), x_of(i), kept);
 }
 
@@ -603,9 +742,16 @@ void sample(const Sample& all, hipStream_t s) {
         if (a.min_p) a.min_p += r;
         a.u += r, a.tokens += r;
         if (a.prob) a.prob += r;
-        hist_kernel<<<a.k * parts, kThreads, 0, s>>>(a, space, parts, size);
-        gather_kernel<<<a.k * parts, kThreads, 0, s>>>(a, space, parts, size);
-        pick_kernel<<<a.k, kThreads, 0, s>>>(a, space, parts);
+        if (size <= 8 * kThreads) {
+            hist_kernel<8><<<a.k * parts, kThreads, 0, s>>>(a, space, parts, size);
+            sum_kernel<<<a.k, kWide, 0, s>>>(a, space, parts);
+            gather_kernel<8><<<a.k * parts, kThreads, 0, s>>>(a, space, parts, size);
+        } else {
+            hist_kernel<32><<<a.k * parts, kThreads, 0, s>>>(a, space, parts, size);
+            sum_kernel<<<a.k, kWide, 0, s>>>(a, space, parts);
+            gather_kernel<32><<<a.k * parts, kThreads, 0, s>>>(a, space, parts, size);
+        }
+        pick_kernel<<<a.k, kWide, 0, s>>>(a, space, parts);
     }
 }
 
