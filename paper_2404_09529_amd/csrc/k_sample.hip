@@ -26,8 +26,9 @@ namespace {
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
 constexpr int kUnitBits = 44, kPerOctave = 32;
 constexpr int kBins = 46 * kPerOctave;          // weights below 2^-45 are none
-constexpr int kWide = 1024;                     // threads of the kernels that have a workgroup per row
+constexpr int kWide = 1024;                     // threads that sum a row's parts
 constexpr int kScan = 2 * kWide;                // bins as they hold them, two each
+constexpr int kPick = 512;                      // threads that choose
 constexpr int kList = 4096, kMaxParts = 16;
 static_assert(kScan >= kBins, "two bins a thread");
 typedef unsigned long long u64;
@@ -320,31 +321,40 @@ __global__ __launch_bounds__(kWide) void sum_kernel(ppk::Sample a, Space s, int 
     Plan* plan = s.plan + row;
     if (tid == 0) plan->E = w.E, plan->top = w.top;
     if (set.greedy || !near(w.E)) return;
-    if (tid < parts) shifts[tid] = near(ps[tid].E) ? octaves(w.E, ps[tid].E) : 64;
+    if (tid < kMaxParts) shifts[tid] = tid < parts && near(ps[tid].E) ? octaves(w.E, ps[tid].E) : 64;
     if (tid < 5) at[tid] = kBins - 1;
     __syncthreads();
-    // the bins of all parts, one wait for memory
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int b = tid + i * kWide;
-        u64 x[kMaxParts], t = 0;
-        uint32_t c[kMaxParts], n = 0;
+    // the bins of all parts, eight parts in one wait for memory (without branches: a part too many is the last one again)
+    u64 t[2] = {0, 0};
+    uint32_t n[2] = {0, 0};
+    for (int p0 = 0; p0 < parts; p0 += 8) {
         const int64_t src = int64_t(row) * parts * kBins;
+        u64 x[2][8];
+        uint32_t c[2][8];
+        auto from = [&](int i, int p) { return tid + i * kWide - kPerOctave * shifts[p0 + p]; };
+        auto at_of = [&](int i, int p) { return src + min(p0 + p, parts - 1) * kBins + min(max(from(i, p), 0), kBins - 1); };
 #pragma unroll
-        for (int p = 0; p < kMaxParts; ++p) {
-            if (p >= parts) break;
-            const int64_t from = src + p * kBins + min(max(b - kPerOctave * shifts[p], 0), kBins - 1);
-            x[p] = s.sum[from];
-            c[p] = set.top_k ? s.count[from] : 0;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int p = 0; p < 8; ++p) x[i][p] = s.sum[at_of(i, p)], c[i][p] = 0;
+        if (set.top_k) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int p = 0; p < 8; ++p) c[i][p] = s.count[at_of(i, p)];
         }
 #pragma unroll
-        for (int p = 0; p < kMaxParts; ++p) {
-            if (p >= parts) break;
-            const int from = b - kPerOctave * shifts[p];   // (a part without anything, 64 octaves down, has written no bins)
-            if (from >= 0 && from < kBins) t += x[p] >> shifts[p], n += c[p];
-        }
-        sums[b] = t, counts[b] = n;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                // (a part without anything, 64 octaves down, has written no bins)
+                const bool has = from(i, p) >= 0 && from(i, p) < kBins;
+                t[i] += has ? x[i][p] >> (shifts[p0 + p] & 63) : 0;
+                n[i] += has ? c[i][p] : 0;
+            }
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sums[tid + i * kWide] = t[i], counts[tid + i * kWide] = n[i];
     __syncthreads();
     // two neighbours a thread
     const u64 sum0 = sums[2 * tid], sum1 = sums[2 * tid + 1];
@@ -475,8 +485,8 @@ struct Place {
 struct Descent {
     u64 sum[256];
     uint32_t count[256];
-    u64 wave_sum[kWide / kWave];
-    uint32_t wave_count[kWide / kWave];
+    u64 wave_sum[kPick / kWave];
+    uint32_t wave_count[kPick / kWave];
     int digit, found;
     u64 above_sum;
     uint32_t above_count;
@@ -491,7 +501,7 @@ __device__ Place find(const float* x, int vocab, const AnyScale& sc, const Power
         __syncthreads();
         if (tid < 256) lds.sum[tid] = 0, lds.count[tid] = 0;
         __syncthreads();
-        over<4, kWide>(x, 0, vocab, [&](float y, int) {
+        over<4, kPick>(x, 0, vocab, [&](float y, int) {
             const uint32_t k = key_of(y);
             if ((k & mask) != prefix) return;
             const Depth d = sc.depth(y);
@@ -502,8 +512,8 @@ __device__ Place find(const float* x, int vocab, const AnyScale& sc, const Power
         __syncthreads();
         const u64 s = tid < 256 ? lds.sum[255 - tid] : 0;   // digits from 255 down
         const uint32_t n = tid < 256 ? lds.count[255 - tid] : 0;
-        const u64 es = above_s + block_scan<kWide / kWave>(s, lds.wave_sum);
-        const uint32_t en = above_n + block_scan<kWide / kWave>(n, lds.wave_count);
+        const u64 es = above_s + block_scan<kPick / kWave>(s, lds.wave_sum);
+        const uint32_t en = above_n + block_scan<kPick / kWave>(n, lds.wave_count);
         if (tid < 256 && !passes(what, es - s, en - n, bound) && passes(what, es, en, bound))
             lds.digit = 255 - tid, lds.above_sum = es - s, lds.above_count = en - n;
         __syncthreads();
@@ -520,14 +530,14 @@ __device__ Place find(const float* x, int vocab, const AnyScale& sc, const Power
         else lo = mid + 1;
     }
     uint32_t before = 0;
-    for (int v0 = 0; v0 < vocab; v0 += kWide) {
+    for (int v0 = 0; v0 < vocab; v0 += kPick) {
         const bool is = v0 + tid < vocab && x[v0 + tid] == v;
         const u64 here = __ballot(is);
         __syncthreads();
         if (lane == 0) lds.wave_count[tid / kWave] = __popcll(here);
         __syncthreads();
         uint32_t mine = before, all = 0;
-        for (int i = 0; i < (kWide / kWave); ++i) {
+        for (int i = 0; i < (kPick / kWave); ++i) {
             if (i < tid / kWave) mine += lds.wave_count[i];
             all += lds.wave_count[i];
         }
@@ -545,7 +555,7 @@ __device__ Place descend(const float* x, int vocab, const Settings& set, const A
                          Descent& lds) {
     u64 all = 0, likely = 0;
     uint32_t count = 0;
-    over<4, kWide>(x, 0, vocab, [&](float y, int) {
+    over<4, kPick>(x, 0, vocab, [&](float y, int) {
         const Depth d = sc.depth(y);
         if (!live(d)) return;
         const u64 w = weight(d, powers);
@@ -553,9 +563,9 @@ __device__ Place descend(const float* x, int vocab, const Settings& set, const A
         if (share_of(y, top, set) >= set.min_p) likely += w;
     });
     auto total = [&](auto v, auto* waves) {
-        v = block_scan<kWide / kWave>(v, waves);
+        v = block_scan<kPick / kWave>(v, waves);
         __syncthreads();
-        if (threadIdx.x == kWide - 1) waves[0] = v;
+        if (threadIdx.x == kPick - 1) waves[0] = v;
         __syncthreads();
         v = waves[0];
         __syncthreads();
@@ -574,16 +584,44 @@ __device__ Place descend(const float* x, int vocab, const Settings& set, const A
 }
 
 // ------------------------------------------------------------------------------- the choice
-__global__ __launch_bounds__(kWide) void pick_kernel(ppk::Sample a, Space s, int parts) {
+// An id in a list: ~key, id; in the order of these the likeliest comes first.
+__device__ __forceinline__ float logit_of(u64 entry) { return of_key(~static_cast<uint32_t>(entry >> 32)); }
+__device__ __forceinline__ u64 better_of(u64 x, u64 y, bool least) { return (x < y) == least ? x : y; }
+template <int S>
+__device__ __forceinline__ u64 lane_xor(u64 x) {
+    if constexpr (S == 32) {
+        return __shfl_xor(x, 32, kWave);
+    } else {
+        const uint32_t lo = __builtin_amdgcn_ds_swizzle(static_cast<int>(x), S << 10 | 0x1f);
+        const uint32_t hi = __builtin_amdgcn_ds_swizzle(static_cast<int>(x >> 32), S << 10 | 0x1f);
+        return u64(hi) << 32 | lo;
+    }
+}
+// The last steps of a bitonic merge, partners S, S / 2 .. 1 lanes apart.
+template <int S>
+__device__ __forceinline__ u64 merge_lanes(u64 x, bool up) {
+    x = better_of(x, lane_xor<S>(x), ((threadIdx.x & S) == 0) == up);
+    if constexpr (S > 1) return merge_lanes<S / 2>(x, up);
+    return x;
+}
+// A wavefront's 64 entries in order, ascending where bit 6 of their number is 0.
+template <int SIZE = 2>
+__device__ __forceinline__ u64 sort_lanes(u64 x, int i) {
+    x = merge_lanes<SIZE / 2>(x, (i & SIZE) == 0);
+    if constexpr (SIZE < kWave) return sort_lanes<2 * SIZE>(x, i);
+    return x;
+}
+
+__global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int parts) {
     __shared__ u64 list[kList];   // what of the order stands in the id's stead: ~key, id
     __shared__ u64 run[kList];    // running sums
     __shared__ uint16_t bins[kList];
     __shared__ union {
         Descent descent;
-        u64 waves[kWide / kWave];
+        u64 waves[kPick / kWave];
     } lds;
     __shared__ Powers powers;
-    __shared__ int first, starts[kMaxParts + 1];
+    __shared__ int first[3], starts[kMaxParts + 1];
     __shared__ u64 likely;
     const int row = blockIdx.x, tid = threadIdx.x;
     const Settings set = settings_of(a, row);
@@ -602,14 +640,16 @@ __global__ __launch_bounds__(kWide) void pick_kernel(ppk::Sample a, Space s, int
     const AnyScale sc = {scale_of(set.t), plan->E};
     const float top = plan->top;
     // the parts' lists, one behind the other
-    if (tid == 0) {
-        int all = 0;
-        for (int p = 0; p < parts; ++p) {
-            const int c = s.listed[int64_t(row) * parts + p];
-            starts[p] = all;
-            all = c > room_of(parts) || all + c > kList ? kList + 1 : all + c;
+    if (tid < kWave) {
+        const int c = tid < parts ? s.listed[int64_t(row) * parts + tid] : 0;
+        int end = c > room_of(parts) ? kList + 1 : c;   // (sixteen of these stay small)
+#pragma unroll
+        for (int o = 1; o < kMaxParts; o <<= 1) {
+            const int up = __shfl_up(end, o, kWave);
+            if (tid >= o) end += up;
         }
-        starts[parts] = all;
+        if (tid < kMaxParts) starts[tid + 1] = end;
+        if (tid == 0) starts[0] = 0;
     }
     __syncthreads();
     const int n = starts[parts];
@@ -624,95 +664,133 @@ __global__ __launch_bounds__(kWide) void pick_kernel(ppk::Sample a, Space s, int
         if (tid == 0) write(p.id, p.x, p.sum);
         return;
     }
-    // Bitonic sort of the next power of two.  Pairs up to 64 apart lie within a wavefront's own 128 values, which it
-    // writes and reads in order: only the wider ones wait for the others.
-    int m = 64;
-    while (m < n) m *= 2;
-    for (int i = n + tid; i < m; i += kWide) list[i] = ~0ull;
-    for (int p = tid / kWave; p < parts; p += (kWide / kWave))   // a wavefront copies a part's
+    for (int p = tid / kWave; p < parts; p += kPick / kWave)   // a wavefront copies a part's
         for (int i = starts[p] + tid % kWave; i < starts[p + 1]; i += kWave)
             list[i] = s.list[(int64_t(row) * parts + p) * room_of(parts) + i - starts[p]];
     __syncthreads();
-    bool wide = false;
-    for (int size = 2; size <= m; size *= 2)
-        for (int stride = size / 2; stride > 0; stride /= 2) {
-            if (stride > kWave || wide) __syncthreads();
-            wide = stride > kWave;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            for (int i = tid; i < m / 2; i += kWide) {
-                const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
-                const u64 x = list[lo], y = list[hi];
-                if ((x > y) == ((lo & size) == 0)) list[lo] = y, list[hi] = x;
+    // Bitonic sort of the next power of two in registers, entry tid + kPick j in register j: partners less than 64 apart are
+    // lanes, others less than kPick apart come through LDS.
+    constexpr int kHeld = kList / kPick;
+    int m = kWave;
+    while (m < n) m *= 2;
+    const int held = (m + kPick - 1) / kPick;
+    const bool takes_part = tid / kWave * kWave < m;
+    u64 v[kHeld];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) v[j] = tid + j * kPick < n ? list[tid + j * kPick] : ~0ull;
+    if (takes_part) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (j < held) v[j] = sort_lanes(v[j], tid + j * kPick);
+    }
+    for (int size = 2 * kWave; size <= m; size *= 2) {
+        for (int stride = size / 2; stride >= kWave; stride /= 2) {
+            if (stride >= kPick) {
+#pragma unroll
+                for (int s2 = 1; s2 < kHeld; s2 *= 2)
+                    if (stride == s2 * kPick) {
+#pragma unroll
+                        for (int j = 0; j < kHeld; ++j)
+                            if (!(j & s2) && j + s2 < kHeld) {
+                                const u64 x = v[j], y = v[j + s2];
+                                const bool up = ((tid + j * kPick) & size) == 0;
+                                v[j] = (x < y) == up ? x : y, v[j + s2] = (x < y) == up ? y : x;
+                            }
+                    }
+                continue;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j)
+                if (tid + j * kPick < m) list[tid + j * kPick] = v[j];
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                const int i = tid + j * kPick;
+                if (i < m) v[j] = better_of(v[j], list[i ^ stride], ((i & stride) == 0) == ((i & size) == 0));
             }
         }
-    __syncthreads();
-    // Sums of all ids up to each entry: the bins before its own, and the list's entries of its bin.  Eight neighbours a
-    // thread at most: where its first bin started is a thread before's to know.
-    const int per = (m + kWide - 1) / kWide, i0 = tid * per, i1 = min(i0 + per, n);
-    auto x_of = [&](int i) { return of_key(~static_cast<uint32_t>(list[i] >> 32)); };
-    u64 mine = 0;
-    for (int i = i0; i < i1; ++i) {
-        const Depth d = sc.depth(x_of(i));
-        run[i] = mine += weight(d, powers);
-        bins[i] = static_cast<uint16_t>(min(bin_of(d), kBins - 1));
+        if (takes_part) {
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j)
+                if (j < held) v[j] = merge_lanes<kWave / 2>(v[j], ((tid + j * kPick) & size) == 0);
+        }
     }
-    const u64 ahead = block_scan<kWide / kWave>(mine, lds.waves) - mine;
-    for (int i = i0; i < i1; ++i) run[i] += ahead;
+    // Sums of the entries up to each, in order.
+    u64 carry = 0;
+    int bin[kHeld];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        if (j >= held) break;
+        const int i = tid + j * kPick;
+        const Depth d = sc.depth(logit_of(v[j]));
+        const u64 w = i < n ? weight(d, powers) : 0;
+        bin[j] = i < n ? min(bin_of(d), kBins - 1) : kBins;
+        const u64 sum = carry + block_scan<kPick / kWave>(w, lds.waves);
+        if (i < m) list[i] = v[j], run[i] = sum, bins[i] = static_cast<uint16_t>(bin[j]);
+        if (held > 1) {   // (the scan's next barriers are between this and its next use)
+            __syncthreads();
+            carry = run[min((j + 1) * kPick, m) - 1];
+        }
+    }
+    if (tid < 3) first[tid] = n - 1;
     if (tid == 0) likely = plan->before[plan->m0];
     __syncthreads();
-    // the first entry of entry i's bin
-    auto start = [&](int i) {
-        int lo = 0, hi = i;
+    // Of all ids up to each: the bins before its own, and the list's entries of its bin.  `rank`: among these.
+    u64 total[kHeld];
+    int rank[kHeld];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        const int i = tid + j * kPick;
+        total[j] = 0, rank[j] = -1;
+        if (j >= held || i >= n) continue;
+        int lo = 0, hi = i;   // the first entry of the bin
         while (lo < hi) {
             const int mid = (lo + hi) / 2;
-            if (bins[mid] < bins[i]) lo = mid + 1;
+            if (bins[mid] < bin[j]) lo = mid + 1;
             else hi = mid;
         }
-        return lo;
-    };
-    u64 total[kList / kWide];
-#pragma unroll
-    for (int j = 0; j < kList / kWide; ++j) {
-        const int i = tid + j * kWide;
-        if (i >= n) break;
-        const int lo = start(i);
-        total[j] = plan->before[bins[i]] + run[i] - (lo ? run[lo - 1] : 0);
+        rank[j] = i - lo;
+        total[j] = plan->before[bin[j]] + run[i] - (lo ? run[lo - 1] : 0);
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kList / kWide; ++j)
-        if (tid + j * kWide < n) run[tid + j * kWide] = total[j];
+    for (int j = 0; j < kHeld; ++j)
+        if (tid + j * kPick < n && j < held) run[tid + j * kPick] = total[j];
     // The first entry that passes; the last one if a sum of parts and one of ids differ in their last bits just here.
-    auto place = [&](auto bound) {
+    auto place = [&](int slot, auto passes) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            if (j >= held) break;
+            const int i = tid + j * kPick;
+            const u64 here = __ballot(i < n && passes(total[j], bin[j], rank[j]));
+            if (here && tid % kWave == 0) atomicMin(&first[slot], i + __builtin_ctzll(here));
+        }
         __syncthreads();
-        if (tid == 0) first = n - 1;
-        __syncthreads();
-        for (int i = tid; i < n; i += kWide)
-            if (bound(i)) {
-                atomicMin(&first, i);
-                break;
-            }
-        __syncthreads();
-        return first;
+        return first[slot];
     };
     u64 kept = plan->all;
     if (plan->k_bin >= 0) {
-        const int rank = set.top_k - plan->k_before - 1, bin = plan->k_bin;
-        kept = run[place([&](int i) { return bins[i] == bin && i - start(i) == rank; })];
+        const int last = set.top_k - plan->k_before - 1, of = plan->k_bin;
+        kept = run[place(0, [&](u64, int b, int r) { return b == of && r == last; })];
     }
     if (set.top_p < 1.0) {
         const double bound = fmax(set.top_p * static_cast<double>(kept), 1.0);
-        kept = run[place([&](int i) { return static_cast<double>(run[i]) >= bound; })];
+        kept = run[place(1, [&](u64 sum, int, int) { return static_cast<double>(sum) >= bound; })];
     }
     if (set.min_p > 0.0) {
-        for (int i = tid; i < n; i += kWide)
-            if (share_of(x_of(i), top, set) >= set.min_p) atomicMax(&likely, run[i]);
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (j < held && tid + j * kPick < n && bin[j] >= plan->m0 && bin[j] <= plan->m1 &&
+                share_of(logit_of(v[j]), top, set) >= set.min_p)
+                atomicMax(&likely, total[j]);
         __syncthreads();
         kept = min(kept, likely);
     }
     const double bound = choice_bound(set.u, static_cast<double>(kept));
-    const int i = place([&](int j) { return static_cast<double>(run[j]) > bound; });
-    if (tid == 0) write(static_cast<int>(static_cast<uint32_t>(list[i])), x_of(i), kept);
+    const int i = place(2, [&](u64 sum, int, int) { return static_cast<double>(sum) > bound; });
+    if (tid == 0) write(static_cast<int>(static_cast<uint32_t>(list[i])), logit_of(list[i]), kept);
 }
 
 constexpr int kRowsAtOnce = 1024;   // rows of a set of launches: the workspace's bound
@@ -751,7 +829,7 @@ void sample(const Sample& all, hipStream_t s) {
             sum_kernel<<<a.k, kWide, 0, s>>>(a, space, parts);
             gather_kernel<32><<<a.k * parts, kThreads, 0, s>>>(a, space, parts, size);
         }
-        pick_kernel<<<a.k, kWide, 0, s>>>(a, space, parts);
+        pick_kernel<<<a.k, kPick, 0, s>>>(a, space, parts);
     }
 }
 
