@@ -19,9 +19,14 @@ __device__ __forceinline__ RowCode head_code(const float (&v)[N]) {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) top = max(top, magnitude(v[i]));
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1)
-        top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o, kWave)));
+    // the neighbour, the other pair, then the lane opposite in 8 and in 16
+    auto with = [&](auto control) {
+        top = max(top, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(top), control(), 0xf, 0xf, true)));
+    };
+    with([] { return 0xb1; });
+    with([] { return 0x4e; });
+    if constexpr (LANES >= 8) with([] { return 0x141; });
+    if constexpr (LANES >= 16) with([] { return 0x140; });
     return row_code(top);
 }
 
@@ -39,43 +44,65 @@ __device__ __forceinline__ void load_row8(const int8_t* pages, const float* scal
     }
 }
 
+// (The table is read at a place that exists, whatever is asked for: a load behind a branch is waited for at once.)
 __device__ __forceinline__ int32_t place(const ppk::PagedCache& c, int32_t seq, int32_t pos) {
-    if (seq < 0 || seq >= c.k || pos < 0 || (pos >> c.shift) >= c.max_pages) return -1;
-    return ppk::paged_row(c.table[int64_t(seq) * c.max_pages + (pos >> c.shift)], c.n_pages, pos, c.shift);
+    const bool in = seq >= 0 && seq < c.k && pos >= 0 && (pos >> c.shift) < c.max_pages;
+    const int32_t page = c.table[in ? int64_t(seq) * c.max_pages + (pos >> c.shift) : 0];
+    return in ? ppk::paged_row(page, c.n_pages, pos, c.shift) : -1;
 }
 
-// Item = (row, keys or values, 8 values); one thread each.
+// A thread has 8 values of a row (one of 2 Hkv D / 8 columns, those of the keys first) and kAhead rows on the way at
+// once; a workgroup has `wide` columns of kBlock / wide rows, kAhead times.
+constexpr int kAhead = 4;
 template <int D, typename T, typename P, bool WRITE>
 __global__ __launch_bounds__(kBlock) void paged_rows_kernel(ppk::PagedCache c, const int32_t* __restrict__ seq,
-                                                            const int32_t* __restrict__ pos, int64_t items, T* k,
-                                                            int64_t ldk, T* v, int64_t ldv) {
+                                                            const int32_t* __restrict__ pos, int rows, T* k, int64_t ldk,
+                                                            T* v, int64_t ldv, int wide, int col_blocks) {
     constexpr int LANES = D / 8;
-    const int per = c.Hkv * LANES;   // threads of a row of keys
-    const int64_t step = int64_t(gridDim.x) * kBlock;
-    for (int64_t i = int64_t(blockIdx.x) * kBlock + threadIdx.x; i < items; i += step) {
-        const int64_t r2 = i / per;
-        const int at = static_cast<int>(i - r2 * per), head = at / LANES;
-        const int64_t r = r2 >> 1;
-        const bool val = r2 & 1;
-        const int32_t row = place(c, seq[r], pos[r]);
-        if (row < 0) continue;   // the lanes of a head's row go together
-        T* x = (val ? v + r * ldv : k + r * ldk) + at * 8;
-        P* pages = static_cast<P*>(val ? c.vp : c.kp);
-        float* scales = val ? c.vs : c.ks;
-        const int64_t off = int64_t(row) * c.Hkv * D + at * 8, head_row = int64_t(row) * c.Hkv + head;
-        float y[8];
-        if constexpr (WRITE) {
-            load8(x, y);
-            if constexpr (sizeof(P) == 1) {
-                const RowCode rc = head_code<LANES>(y);
-                *reinterpret_cast<uint2*>(pages + off) = make_uint2(codes4(y, rc), codes4(y + 4, rc));
-                if (at % LANES == 0) scales[head_row] = rc.scale;
-            } else {
-                store8(pages + off, y);
-            }
+    const int half = c.Hkv * LANES, tall = kBlock / wide, local = threadIdx.x / wide;
+    const int col = blockIdx.x % col_blocks * wide + threadIdx.x - local * wide;
+    const int64_t first = int64_t(blockIdx.x / col_blocks) * tall * kAhead + local;
+    if (local >= tall || col >= 2 * half || first >= rows) return;   // (heads as a whole)
+    const bool val = col >= half;
+    const int in_row = val ? col - half : col;
+    T* dense = val ? v : k;
+    const int64_t ld = val ? ldv : ldk;
+    P* pages = static_cast<P*>(val ? c.vp : c.kp) + in_row * 8;
+    float* scales = (val ? c.vs : c.ks) + in_row / LANES;
+    float y[kAhead][8];
+    int32_t s[kAhead], p[kAhead], row[kAhead];
+    int64_t r[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        r[u] = min(first + int64_t(u) * tall, int64_t(rows) - 1);   // (loads stay in range)
+        s[u] = seq[r[u]];
+        p[u] = pos[r[u]];
+    }
+    if constexpr (WRITE) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) load8(dense + r[u] * ld + in_row * 8, y[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) row[u] = place(c, s[u], p[u]);
+    if constexpr (!WRITE) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t at = int64_t(max(row[u], 0)) * c.Hkv;
+            load_row8(pages, scales, at * D, at, y[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        if (row[u] < 0 || first + int64_t(u) * tall >= rows) continue;
+        const int64_t at = int64_t(row[u]) * c.Hkv;
+        if constexpr (!WRITE) {
+            store8(dense + r[u] * ld + in_row * 8, y[u]);
+        } else if constexpr (sizeof(P) == 1) {
+            const RowCode rc = head_code<LANES>(y[u]);
+            *reinterpret_cast<uint2*>(pages + at * D) = make_uint2(codes4(y[u], rc), codes4(y[u] + 4, rc));
+            if (in_row % LANES == 0) scales[at] = rc.scale;
         } else {
-            load_row8(pages, scales, off, head_row, y);
-            store8(x, y);
+            store8(pages + at * D, y[u]);
         }
     }
 }
@@ -138,13 +165,16 @@ __global__ __launch_bounds__(kBlock) void paged_append_kernel(ppk::PagedCache c,
 template <bool WRITE>
 void rows(int dtype, const ppk::PagedCache& c, const int32_t* seq, const int32_t* pos, int n, void* k, int64_t ldk,
           void* v, int64_t ldv, hipStream_t s) {
-    const int64_t items = int64_t(n) * 2 * c.Hkv * (c.D / 8);
-    const unsigned blocks = static_cast<unsigned>(min((items + kBlock - 1) / kBlock, int64_t(1) << 22));
+    if (n == 0 || c.k == 0 || c.max_pages == 0 || c.n_pages == 0) return;   // (no row has a place)
+    // columns of a workgroup: whole heads
+    const int lanes = c.D / 8, cols = 2 * c.Hkv * lanes, wide = min(cols, kBlock), col_blocks = (cols + wide - 1) / wide;
+    const int64_t per_block = int64_t(kBlock / wide) * kAhead;
+    const unsigned blocks = static_cast<unsigned>((n + per_block - 1) / per_block * col_blocks);
     auto go = [&](auto d, auto t, auto p) {
         using T = decltype(t);
         using P = decltype(p);
         paged_rows_kernel<decltype(d)::value, T, P, WRITE><<<blocks, kBlock, 0, s>>>(
-            c, seq, pos, items, static_cast<T*>(k), ldk, static_cast<T*>(v), ldv);
+            c, seq, pos, n, static_cast<T*>(k), ldk, static_cast<T*>(v), ldv, wide, col_blocks);
     };
     const std::integral_constant<int, 64> d64;
     const std::integral_constant<int, 128> d128;
