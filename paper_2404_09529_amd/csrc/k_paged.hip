@@ -44,7 +44,8 @@ __device__ __forceinline__ void load_row8(const int8_t* pages, const float* scal
     }
 }
 
-// (The table is read at a place that exists, whatever is asked for: a load behind a branch is waited for at once.)
+// The table has an entry.  (It is read at a place that exists, whatever is asked for: a load behind a branch is waited for
+// at once.)
 __device__ __forceinline__ int32_t place(const ppk::PagedCache& c, int32_t seq, int32_t pos) {
     const bool in = seq >= 0 && seq < c.k && pos >= 0 && (pos >> c.shift) < c.max_pages;
     const int32_t page = c.table[in ? int64_t(seq) * c.max_pages + (pos >> c.shift) : 0];
@@ -142,6 +143,7 @@ __global__ __launch_bounds__(kBlock) void paged_append_kernel(ppk::PagedCache c,
         store8(q + HALF, hi);
         return;
     }
+    if (c.max_pages == 0) return;
     const int32_t row = place(c, i, pos);
     if (row < 0) return;
     const bool val = head >= c.H + c.Hkv;
@@ -165,7 +167,7 @@ __global__ __launch_bounds__(kBlock) void paged_append_kernel(ppk::PagedCache c,
 template <bool WRITE>
 void rows(int dtype, const ppk::PagedCache& c, const int32_t* seq, const int32_t* pos, int n, void* k, int64_t ldk,
           void* v, int64_t ldv, hipStream_t s) {
-    if (n == 0 || c.k == 0 || c.max_pages == 0 || c.n_pages == 0) return;   // (no row has a place)
+    if (c.max_pages == 0) return;   // no row has a place
     // columns of a workgroup: whole heads
     const int lanes = c.D / 8, cols = 2 * c.Hkv * lanes, wide = min(cols, kBlock), col_blocks = (cols + wide - 1) / wide;
     const int64_t per_block = int64_t(kBlock / wide) * kAhead;

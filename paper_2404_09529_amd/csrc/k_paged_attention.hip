@@ -647,8 +647,10 @@ __global__ __launch_bounds__(kBlock, 2) void paged_attention_kernel(ppk::PagedCa
                 const bool ends = at.st + 1 == at.steps;
                 if (!more || ends) {
                     flush(at.seq, begins && ends);
-                    if (ends)
-                        for (int i = at.seq + 1; i < split.k && lens.length(i) == 0; ++i) zero(i);
+                    if (ends) {   // (`next` stays in this sequence if it is the last one with keys)
+                        const int end = next.seq > at.seq ? next.seq : split.k;
+                        for (int i = at.seq + 1; i < end; ++i) zero(i);
+                    }
                     clear();
                     begins = true, piece = 1;
                 }

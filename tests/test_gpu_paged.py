@@ -532,3 +532,89 @@ def test_shared_pages():
     q = rand(torch.Generator().manual_seed(1), 2, H * D)
     got = run_attention(config(H, Hkv, D, "f32"), pool, lens, q.cuda())
     check_attention(got, q.double().view(2, H, D), pool, lens, H, "f32")
+
+
+def _many(name):
+    """Lengths of more sequences than a wavefront's registers hold at once (256), with empty ones around that border."""
+    g = torch.Generator().manual_seed(11)
+    n = torch.tensor([0, 1, 33, 70])[torch.randint(0, 4, (700,), generator=g)].tolist()
+    if name == "border":
+        n[250:259] = [0] * 9
+        n[511:515] = [40, 0, 0, 0]
+        n[249] = n[259] = 5
+    elif name == "one before":
+        n[254:258] = [33, 0, 20, 0]
+    elif name == "gap of a block":
+        n[200:600] = [0] * 400
+    elif name == "late":
+        n[:680] = [0] * 680
+    elif name == "last alone":
+        n = [0] * 699 + [50]
+    elif name == "long":
+        n[255], n[256], n[600] = 3000, 0, 4000
+    return n
+
+
+@pytest.mark.parametrize("dtype,kv", KINDS)
+@pytest.mark.parametrize("name", ["random", "border", "one before", "gap of a block", "late", "last alone", "long"])
+def test_attention_many_sequences(dtype, kv, name):
+    lens = _many(name)
+    H, Hkv, D = (2, 1, 128) if dtype == "bf16" else (1, 1, 64)
+    pool = Pool(kv, len(lens), Hkv, D, 32, -(-max(lens) // 32), seed=3).fill(4)
+    q = (2.0 * rand(torch.Generator().manual_seed(7), len(lens), H * D)).to(TYPES[dtype][1])
+    got = run_attention(config(H, Hkv, D, dtype), pool, lens, q.cuda())
+    check_attention(got, q.double().view(-1, H, D), pool, lens, H, dtype)
+
+
+@pytest.mark.parametrize("kv", ["f32", "i8"])
+def test_attention_tables_past_31_bits_of_steps(kv):
+    """Tables that reach 2^31 - 1 positions each: 33 sequences' steps pass 2^31.  One sequence is that long, with one page."""
+    H, Hkv, D, page, k = 2, 1, 64, 1 << 16, 33
+    max_pages = (1 << 31) // page
+    pool = Pool(kv, 1, Hkv, D, page, 1, spare=0, seed=3).fill(4)
+    lens = [(i * 37) % 300 for i in range(k)]
+    lens[3] = 2 ** 31 - 1
+    table = torch.full((k, max_pages), -1, dtype=torch.int32)
+    table[:, 0] = 0
+    table[3, 0], table[3, max_pages - 1] = -1, 0        # the last page, but for the last position
+    table[5, 0] = -1
+    pool.table = table
+    pool.to_device()
+    q = (2.0 * rand(torch.Generator().manual_seed(7), k, H * D))
+    got = run_attention(config(H, Hkv, D, "f32"), pool, lens, q.cuda())
+    # the same keys for a table of one page
+    pool.table, short = torch.zeros((k, 1), dtype=torch.int32), list(lens)
+    pool.table[5, 0] = -1
+    short[3] = page - 1
+    pool.to_device()
+    check_attention(got, q.double().view(-1, H, D), pool, short, H, "f32")
+
+
+@pytest.mark.parametrize("dtype,kv", KINDS)
+def test_tables_without_entries(dtype, kv):
+    """max_pages 0: nothing has a place, the query is rotated all the same."""
+    H, Hkv, D = (2, 1, 128) if dtype == "bf16" else (2, 1, 64)
+    t, w, cfg = TYPES[dtype][1], (H + 2 * Hkv) * D, config(H, Hkv, D, dtype)
+    pool = Pool(kv, 3, Hkv, D, 8, 1, seed=1).fill(2)
+    before = pool.host()
+    full = pool.cache
+    dev = pool.dev
+    cache = pp.PagedCache(PAGES[kv][0], torch.empty((3, 0), dtype=torch.int32, device="cuda"), dev["k"], dev["v"], dev["ks"], dev["vs"])
+    qkv = rand(torch.Generator().manual_seed(3), 3, w).to(t).cuda()
+    lens = torch.tensor([5, 0, 1], dtype=torch.int32, device="cuda")
+    q, q2 = (torch.full((3, H * D), 9.0, device="cuda").to(t) for _ in range(2))
+    pp.pp_paged_append(cfg, cache, lens, qkv, w, q, H * D)
+    rows = torch.zeros(3, dtype=torch.int32, device="cuda")
+    dense = torch.full((3, Hkv * D), 4.0, device="cuda").to(t)
+    pp.pp_paged_write(cfg, cache, rows, rows, 3, dense, Hkv * D, dense, Hkv * D)
+    pp.pp_paged_read(cfg, cache, rows, rows, 3, dense, Hkv * D, dense, Hkv * D)
+    out = torch.full((3, H * D), 9.0, device="cuda").to(t)
+    ws = torch.empty(pp.pp_paged_attention_workspace_size(cfg, cache), dtype=torch.uint8, device="cuda")
+    pp.pp_paged_attention(cfg, cache, lens, q, H * D, out, ws)
+    torch.cuda.synchronize()
+    for x, y in zip(before, pool.host()):
+        assert x is None or torch.equal(x, y)
+    assert bool((dense == 4).all()) and bool((out == 0).all()) and bool((q[1] == 9).all())
+    pp.pp_paged_append(cfg, full, lens, qkv, w, q2, H * D)
+    torch.cuda.synchronize()
+    assert torch.equal(q, q2)
