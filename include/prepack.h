@@ -594,7 +594,7 @@ pp_status pp_sample_workspace_size(int32_t k, int32_t vocab, size_t* bytes);
  *   T <= 0 (or NaN): the token that pp_first_token chooses, prob 1 (-1 and 0 where every logit is NaN).
  *   top_k <= 0, top_p >= 1 and min_p <= 0 (or NaN) are no limit; u below 0 or NaN counts as 0, u >= 1 gives the last kept id.
  *   NaN logits are never chosen, nor is -inf with T > 0 (no other logit: token -1, prob 0); ids of +inf share the sum evenly.
- *   tokens device int32 [k]; prob device float32 [k]; vocab up to 2^20.
+ *   tokens device int32 [k]; prob device float32 [k]; vocab below 2^20.
  * w is computed in float64 and summed exactly, as a multiple of 2^-44 (ids below 2^-45 of the likeliest are never chosen).
  * workspace: >= pp_sample_workspace_size bytes, 256-byte aligned, not used by two calls at a time.  Deterministic.
  * Errors: PP_ERR_INVALID_ARG (NULL logits, u or tokens, k < 0, vocab <= 0, ldl < vocab, misaligned workspace),

@@ -12,7 +12,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxHeadRows = 1 << 22;   // sequences times query heads: a launch holds fewer than 2^32 threads
-constexpr int32_t kMaxVocab = 1 << 20;      // sums of weights of up to 2^44 fit 64 bits
+constexpr int32_t kMaxVocab = (1 << 20) - 1;   // sums of weights of up to 2^44 fit 64 bits
 
 bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
 

@@ -265,3 +265,27 @@ def test_two_streams_at_once():
             pp.pp_sample(xs[a], v, k, v, None, None, None, None, us[a], out[a], ws[a], stream=streams[a])
     torch.cuda.synchronize()
     assert [o.cpu().tolist() for o in out] == want
+
+
+def test_more_rows_than_at_once():
+    """1500 rows, settings of their own, in several sets of launches."""
+    k, v = 1500, 40
+    g = torch.Generator().manual_seed(5)
+    r = lambda n: torch.rand(n, generator=g).tolist()
+    check(logits(k, v, 6, 1.5), t=[0.0 if x < 0.1 else 0.3 + 2 * x for x in r(k)], top_k=[int(50 * x) for x in r(k)],
+          top_p=[0.3 + x for x in r(k)], min_p=[0.2 * x - 0.05 for x in r(k)], u=r(k))
+
+
+@pytest.mark.parametrize("v", [1 << 19, (1 << 20) - 1])
+def test_largest_vocabularies_of_equal_logits(v):
+    """Weights of 2^44 each: sums close to 2^64.  With u and v below 2^24, u v is exact in float64."""
+    u = [0.0, 0.25, 0.5, 0.71875, 1 - 2.0 ** -20, 1 - 2.0 ** -24, 1.0, 0.125]
+    x = torch.zeros(len(u), v)
+    x[2] = 12.0
+    x[3] = -float(2 ** 20)
+    x[4] = float("inf")
+    tokens, prob = run(x, u=u)
+    assert tokens == [min(int(a * v), v - 1) for a in u]
+    assert all(abs(p * v - 1) <= 2.0 ** -23 for p in prob)
+    tokens, prob = run(x, u=u, top_k=[1000] * 8, top_p=[0.5] * 8)
+    assert tokens == [min(int(a * 500), 499) for a in u]

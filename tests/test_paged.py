@@ -124,14 +124,14 @@ def _sample(**kw):
 
 @pytest.mark.parametrize("want,kw", [
     (INV, dict(k=-1)), (INV, dict(vocab=0)), (INV, dict(vocab=-5)), (INV, dict(ldl=999)), (INV, dict(logits=None)),
-    (INV, dict(u=None)), (INV, dict(tokens=None)), (UNS, dict(vocab=(1 << 20) + 1, ldl=1 << 21)), (UNS, dict(k=1 << 21)),
+    (INV, dict(u=None)), (INV, dict(tokens=None)), (UNS, dict(vocab=1 << 20, ldl=1 << 21)), (UNS, dict(k=1 << 21)),
     (OK, dict(k=0, logits=None, u=None, tokens=None, ws=None, bytes=0))])
 def test_sample_arguments(want, kw):
     assert _sample(**kw) == want
 
 
 def test_sample_workspace():
-    for k, vocab in [(1, 10), (1, 32000), (64, 128256), (300, 128256), (2, 1 << 20)]:
+    for k, vocab in [(1, 10), (1, 32000), (64, 128256), (300, 128256), (2, (1 << 20) - 1)]:
         need = pp.pp_sample_workspace_size(k, vocab)
         assert 0 <= need <= 1 << 26
         if need:
@@ -139,7 +139,7 @@ def test_sample_workspace():
             assert _sample(ws=None, **kw) == INV
             assert _sample(ws=0x10010, **kw) == INV
             assert _sample(bytes=need - 1, **kw) == SMALL
-    for bad in [(-1, 10), (1, 0), (1, (1 << 20) + 1)]:
+    for bad in [(-1, 10), (1, 0), (1, 1 << 20)]:
         with pytest.raises(pp.PrepackError):
             pp.pp_sample_workspace_size(*bad)
     assert pp.lib().pp_sample_workspace_size(1, 10, None) == INV
