@@ -1,8 +1,11 @@
 // A paged cache's rows: written from dense rows (a prefill's caches), read back, and appended to by a
 // decode step with the rotation of its query and key (RESTART-PE: a sequence's positions are its own).
 //
-// A head's row of D values is D / 8 lanes' (16 for D = 128), 8 values each, so that its scale is a maximum over
-// lanes that sit side by side.  Memory bounds the rows' kernels; the append is a few microseconds of latency.
+// A head's row of D values is D / 16 lanes' (8 for D = 128), side by side, so that its scale is a maximum over few
+// lanes; a lane has 8 values of each half of the row, the pairs that are rotated together, and every load is of whole lines.
+// Memory bounds the rows' kernels.  24,352 rows of 32 heads of 128: into 8-bit pages (604 MB) 144 us, 4.2 TB/s, where the
+// codes' arithmetic is most of that time as well; back 102 us, 5.9 TB/s; 20,140 rows of 8 heads back 28 us, 4.5 TB/s.  The append is
+// latency: 2.9 us for one sequence, 4.5 for 64 (32 heads, 8-bit pages).
 #include "device.h"
 #include "kernels.h"
 #include "paged.h"
@@ -30,6 +33,21 @@ __device__ __forceinline__ RowCode head_code(const float (&v)[N]) {
     return row_code(top);
 }
 
+// A lane's 16 values of a head's row, 8 from dst on and 8 half a row behind; `lane` of the head's.
+template <int LANES, typename P>
+__device__ __forceinline__ void store_head(P* dst, float* scale, const float (&v)[16], int lane) {
+    constexpr int HALF = 8 * LANES;
+    if constexpr (sizeof(P) == 1) {
+        const RowCode rc = head_code<LANES>(v);
+        *reinterpret_cast<uint2*>(dst) = make_uint2(codes4(v, rc), codes4(v + 4, rc));
+        *reinterpret_cast<uint2*>(dst + HALF) = make_uint2(codes4(v + 8, rc), codes4(v + 12, rc));
+        if (lane == 0) *scale = rc.scale;
+    } else {
+        store8(dst, v);
+        store8(dst + HALF, v + 8);
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ void load_row8(const T* pages, const float*, int64_t src, int64_t, float* v) {
     load8(pages + src, v);
@@ -52,25 +70,27 @@ __device__ __forceinline__ int32_t place(const ppk::PagedCache& c, int32_t seq, 
     return in ? ppk::paged_row(page, c.n_pages, pos, c.shift) : -1;
 }
 
-// A thread has 8 values of a row (one of 2 Hkv D / 8 columns, those of the keys first) and kAhead rows on the way at
-// once; a workgroup has `wide` columns of kBlock / wide rows, kAhead times.
-constexpr int kAhead = 4;
+// A thread has dims j .. j + 7 and D / 2 + j .. + 7 of a head's row (one of 2 Hkv D / 16 columns, those of the keys first)
+// and kAhead rows on the way at once; a workgroup has `wide` columns of kBlock / wide rows, kAhead times.  In us, the first
+// figures above: 8 values a thread and one row at a time 149 and 120 (and 43 of 8 heads), two 156 and 151, four 156 and 117,
+// eight 154 and 108; 16 values and four rows 148 and 101, but few rows are slower (115 into bf16 pages: 4.1 and 3.8).
+constexpr int kAhead = 2;
 template <int D, typename T, typename P, bool WRITE>
 __global__ __launch_bounds__(kBlock) void paged_rows_kernel(ppk::PagedCache c, const int32_t* __restrict__ seq,
                                                             const int32_t* __restrict__ pos, int rows, T* k, int64_t ldk,
                                                             T* v, int64_t ldv, int wide, int col_blocks) {
-    constexpr int LANES = D / 8;
+    constexpr int LANES = D / 16, HALF = D / 2;
     const int half = c.Hkv * LANES, tall = kBlock / wide, local = threadIdx.x / wide;
     const int col = blockIdx.x % col_blocks * wide + threadIdx.x - local * wide;
     const int64_t first = int64_t(blockIdx.x / col_blocks) * tall * kAhead + local;
     if (local >= tall || col >= 2 * half || first >= rows) return;   // (heads as a whole)
     const bool val = col >= half;
-    const int in_row = val ? col - half : col;
-    T* dense = val ? v : k;
+    const int lane = col % LANES, head = (val ? col - half : col) / LANES, in_row = head * D + lane * 8;
+    T* dense = (val ? v : k) + in_row;
     const int64_t ld = val ? ldv : ldk;
-    P* pages = static_cast<P*>(val ? c.vp : c.kp) + in_row * 8;
-    float* scales = (val ? c.vs : c.ks) + in_row / LANES;
-    float y[kAhead][8];
+    P* pages = static_cast<P*>(val ? c.vp : c.kp) + in_row;
+    float* scales = (val ? c.vs : c.ks) + head;
+    float y[kAhead][16];
     int32_t s[kAhead], p[kAhead], row[kAhead];
     int64_t r[kAhead];
 #pragma unroll
@@ -81,7 +101,10 @@ __global__ __launch_bounds__(kBlock) void paged_rows_kernel(ppk::PagedCache c, c
     }
     if constexpr (WRITE) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) load8(dense + r[u] * ld + in_row * 8, y[u]);
+        for (int u = 0; u < kAhead; ++u) {
+            load8(dense + r[u] * ld, y[u]);
+            load8(dense + r[u] * ld + HALF, y[u] + 8);
+        }
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) row[u] = place(c, s[u], p[u]);
@@ -90,6 +113,7 @@ __global__ __launch_bounds__(kBlock) void paged_rows_kernel(ppk::PagedCache c, c
         for (int u = 0; u < kAhead; ++u) {
             const int64_t at = int64_t(max(row[u], 0)) * c.Hkv;
             load_row8(pages, scales, at * D, at, y[u]);
+            load_row8(pages, scales, at * D + HALF, at, y[u] + 8);
         }
     }
 #pragma unroll
@@ -97,13 +121,10 @@ __global__ __launch_bounds__(kBlock) void paged_rows_kernel(ppk::PagedCache c, c
         if (row[u] < 0 || first + int64_t(u) * tall >= rows) continue;
         const int64_t at = int64_t(row[u]) * c.Hkv;
         if constexpr (!WRITE) {
-            store8(dense + r[u] * ld + in_row * 8, y[u]);
-        } else if constexpr (sizeof(P) == 1) {
-            const RowCode rc = head_code<LANES>(y[u]);
-            *reinterpret_cast<uint2*>(pages + at * D) = make_uint2(codes4(y[u], rc), codes4(y[u] + 4, rc));
-            if (in_row % LANES == 0) scales[at] = rc.scale;
+            store8(dense + r[u] * ld, y[u]);
+            store8(dense + r[u] * ld + HALF, y[u] + 8);
         } else {
-            store8(pages + at * D, y[u]);
+            store_head<LANES>(pages + at * D, scales + at, y[u], lane);
         }
     }
 }
@@ -120,11 +141,11 @@ __global__ __launch_bounds__(kBlock) void paged_append_kernel(ppk::PagedCache c,
     if (pos < 0) return;
     const int head = blockIdx.y * HEADS + threadIdx.x / LANES, j = threadIdx.x % LANES * 8;
     const bool live = head < c.H + 2 * c.Hkv;
-    float lo[8], hi[8];
+    float x[16];
     if (live) {
-        const T* x = qkv + i * ldqkv + int64_t(head) * D + j;
-        load8(x, lo);
-        load8(x + HALF, hi);
+        const T* src = qkv + i * ldqkv + int64_t(head) * D + j;
+        load8(src, x);
+        load8(src + HALF, x + 8);
     }
     if (threadIdx.x < HALF) angle[threadIdx.x] = rope_entry(pos, threadIdx.x, D, theta);
     __syncthreads();
@@ -132,36 +153,23 @@ __global__ __launch_bounds__(kBlock) void paged_append_kernel(ppk::PagedCache c,
     if (head < c.H + c.Hkv) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const double x = lo[e], y = hi[e], cs = angle[j + e].x, sn = angle[j + e].y;
-            lo[e] = static_cast<float>(x * cs - y * sn);
-            hi[e] = static_cast<float>(y * cs + x * sn);
+            const double lo = x[e], hi = x[e + 8], cs = angle[j + e].x, sn = angle[j + e].y;
+            x[e] = static_cast<float>(lo * cs - hi * sn);
+            x[e + 8] = static_cast<float>(hi * cs + lo * sn);
         }
     }
     if (head < c.H) {
         T* q = q_out + i * ldq + int64_t(head) * D + j;
-        store8(q, lo);
-        store8(q + HALF, hi);
+        store8(q, x);
+        store8(q + HALF, x + 8);
         return;
     }
     if (c.max_pages == 0) return;
     const int32_t row = place(c, i, pos);
     if (row < 0) return;
     const bool val = head >= c.H + c.Hkv;
-    const int h = head - c.H - (val ? c.Hkv : 0);
-    const int64_t head_row = int64_t(row) * c.Hkv + h;
-    P* dst = static_cast<P*>(val ? c.vp : c.kp) + head_row * D + j;
-    if constexpr (sizeof(P) == 1) {
-        float both[16];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) both[e] = lo[e], both[e + 8] = hi[e];
-        const RowCode rc = head_code<LANES>(both);
-        *reinterpret_cast<uint2*>(dst) = make_uint2(codes4(lo, rc), codes4(lo + 4, rc));
-        *reinterpret_cast<uint2*>(dst + HALF) = make_uint2(codes4(hi, rc), codes4(hi + 4, rc));
-        if (j == 0) (val ? c.vs : c.ks)[head_row] = rc.scale;
-    } else {
-        store8(dst, lo);
-        store8(dst + HALF, hi);
-    }
+    const int64_t head_row = int64_t(row) * c.Hkv + head - c.H - (val ? c.Hkv : 0);
+    store_head<LANES>(static_cast<P*>(val ? c.vp : c.kp) + head_row * D + j, (val ? c.vs : c.ks) + head_row, x, j / 8);
 }
 
 template <bool WRITE>
@@ -169,7 +177,7 @@ void rows(int dtype, const ppk::PagedCache& c, const int32_t* seq, const int32_t
           void* v, int64_t ldv, hipStream_t s) {
     if (c.max_pages == 0) return;   // no row has a place
     // columns of a workgroup: whole heads
-    const int lanes = c.D / 8, cols = 2 * c.Hkv * lanes, wide = min(cols, kBlock), col_blocks = (cols + wide - 1) / wide;
+    const int cols = 2 * c.Hkv * (c.D / 16), wide = min(cols, kBlock), col_blocks = (cols + wide - 1) / wide;
     const int64_t per_block = int64_t(kBlock / wide) * kAhead;
     const unsigned blocks = static_cast<unsigned>((n + per_block - 1) / per_block * col_blocks);
     auto go = [&](auto d, auto t, auto p) {
