@@ -587,15 +587,30 @@ __device__ Place descend(const float* x, int vocab, const Settings& set, const A
 // An id in a list: ~key, id; in the order of these the likeliest comes first.
 __device__ __forceinline__ float logit_of(u64 entry) { return of_key(~static_cast<uint32_t>(entry >> 32)); }
 __device__ __forceinline__ u64 better_of(u64 x, u64 y, bool least) { return (x < y) == least ? x : y; }
+// Lane i ^ S's x, without LDS, which such exchanges of eight wavefronts would keep busy.
+template <int S>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t x) {
+    const int i = static_cast<int>(x);
+    if constexpr (S == 1) {
+        return __builtin_amdgcn_update_dpp(0, i, 0xb1, 0xf, 0xf, true);
+    } else if constexpr (S == 2) {
+        return __builtin_amdgcn_update_dpp(0, i, 0x4e, 0xf, 0xf, true);
+    } else if constexpr (S == 4) {   // from four lanes up, then in every other group of four from four lanes down
+        const int up = __builtin_amdgcn_update_dpp(0, i, 0x104, 0xf, 0x5, false);
+        return __builtin_amdgcn_update_dpp(up, i, 0x114, 0xf, 0xa, false);
+    } else if constexpr (S == 8) {
+        return __builtin_amdgcn_update_dpp(0, i, 0x128, 0xf, 0xf, true);
+    } else if constexpr (S == 16) {
+        const auto both = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? both[0] : both[1];
+    } else {
+        const auto both = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return threadIdx.x & 32 ? both[0] : both[1];
+    }
+}
 template <int S>
 __device__ __forceinline__ u64 lane_xor(u64 x) {
-    if constexpr (S == 32) {
-        return __shfl_xor(x, 32, kWave);
-    } else {
-        const uint32_t lo = __builtin_amdgcn_ds_swizzle(static_cast<int>(x), S << 10 | 0x1f);
-        const uint32_t hi = __builtin_amdgcn_ds_swizzle(static_cast<int>(x >> 32), S << 10 | 0x1f);
-        return u64(hi) << 32 | lo;
-    }
+    return u64(lane_xor<S>(static_cast<uint32_t>(x >> 32))) << 32 | lane_xor<S>(static_cast<uint32_t>(x));
 }
 // The last steps of a bitonic merge, partners S, S / 2 .. 1 lanes apart.
 template <int S>
@@ -615,7 +630,7 @@ __device__ __forceinline__ u64 sort_lanes(u64 x, int i) {
 __global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int parts) {
     __shared__ u64 list[kList];   // what of the order stands in the id's stead: ~key, id
     __shared__ u64 run[kList];    // running sums
-    __shared__ uint16_t bins[kList];
+    __shared__ uint16_t bins[kList], start[kBins];
     __shared__ union {
         Descent descent;
         u64 waves[kPick / kWave];
@@ -716,56 +731,58 @@ __global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int
                 if (j < held) v[j] = merge_lanes<kWave / 2>(v[j], ((tid + j * kPick) & size) == 0);
         }
     }
-    // Sums of the entries up to each, in order.
-    u64 carry = 0;
-    int bin[kHeld];
     __syncthreads();
 #pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+        if (tid + j * kPick < m) list[tid + j * kPick] = v[j];
+    __syncthreads();
+    // Sums of the entries up to each, in order; from here on a thread's are neighbours, entry base + j.
+    const int base = tid * held;
+    int bin[kHeld];
+    u64 total[kHeld], before[kHeld], mine = 0;
+#pragma unroll
     for (int j = 0; j < kHeld; ++j) {
-        if (j >= held) break;
-        const int i = tid + j * kPick;
+        bin[j] = kBins;
+        if (j >= held) continue;
+        const int i = base + j;
+        const bool is = i < n;
+        v[j] = is ? list[i] : ~0ull;
         const Depth d = sc.depth(logit_of(v[j]));
-        const u64 w = i < n ? weight(d, powers) : 0;
-        bin[j] = i < n ? min(bin_of(d), kBins - 1) : kBins;
-        const u64 sum = carry + block_scan<kPick / kWave>(w, lds.waves);
-        if (i < m) list[i] = v[j], run[i] = sum, bins[i] = static_cast<uint16_t>(bin[j]);
-        if (held > 1) {   // (the scan's next barriers are between this and its next use)
-            __syncthreads();
-            carry = run[min((j + 1) * kPick, m) - 1];
-        }
+        bin[j] = is ? min(bin_of(d), kBins - 1) : kBins;
+        before[j] = is ? plan->before[bin[j]] : 0;
+        if (is) mine += weight(d, powers), bins[i] = static_cast<uint16_t>(bin[j]);
+        total[j] = mine;
     }
+    const u64 up = block_scan<kPick / kWave>(mine, lds.waves) - mine;
     if (tid < 3) first[tid] = n - 1;
     if (tid == 0) likely = plan->before[plan->m0];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)   // (the scan's barriers are behind `bins`)
+        if (bin[j] < kBins) {
+            run[base + j] = total[j] += up;
+            if (base + j == 0 || bins[base + j - 1] != bin[j]) start[bin[j]] = static_cast<uint16_t>(base + j);
+        }
     __syncthreads();
     // Of all ids up to each: the bins before its own, and the list's entries of its bin.  `rank`: among these.
-    u64 total[kHeld];
     int rank[kHeld];
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
-        const int i = tid + j * kPick;
-        total[j] = 0, rank[j] = -1;
-        if (j >= held || i >= n) continue;
-        int lo = 0, hi = i;   // the first entry of the bin
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (bins[mid] < bin[j]) lo = mid + 1;
-            else hi = mid;
-        }
-        rank[j] = i - lo;
-        total[j] = plan->before[bin[j]] + run[i] - (lo ? run[lo - 1] : 0);
+        if (j >= held) continue;
+        const int lo = bin[j] < kBins ? start[bin[j]] : 0;
+        rank[j] = base + j - lo;
+        total[j] += before[j] - (lo ? run[lo - 1] : 0);
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
-        if (tid + j * kPick < n && j < held) run[tid + j * kPick] = total[j];
+        if (bin[j] < kBins) run[base + j] = total[j];
     // The first entry that passes; the last one if a sum of parts and one of ids differ in their last bits just here.
     auto place = [&](int slot, auto passes) {
 #pragma unroll
         for (int j = 0; j < kHeld; ++j) {
             if (j >= held) break;
-            const int i = tid + j * kPick;
-            const u64 here = __ballot(i < n && passes(total[j], bin[j], rank[j]));
-            if (here && tid % kWave == 0) atomicMin(&first[slot], i + __builtin_ctzll(here));
+            const u64 here = __ballot(bin[j] < kBins && passes(total[j], bin[j], rank[j]));
+            if (here && tid % kWave == 0) atomicMin(&first[slot], base + j + __builtin_ctzll(here) * held);
         }
         __syncthreads();
         return first[slot];
@@ -782,7 +799,7 @@ __global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int
     if (set.min_p > 0.0) {
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
-            if (j < held && tid + j * kPick < n && bin[j] >= plan->m0 && bin[j] <= plan->m1 &&
+            if (bin[j] < kBins && bin[j] >= plan->m0 && bin[j] <= plan->m1 &&
                 share_of(logit_of(v[j]), top, set) >= set.min_p)
                 atomicMax(&likely, total[j]);
         __syncthreads();
