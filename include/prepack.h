@@ -302,8 +302,8 @@ pp_status pp_final_norm_unpack(const float* x, const float* gain, int32_t d, flo
  * channel).  A value is its code times the scale of its row, codes are -127 .. 127, and a layer's
  * projections are pp_rmsnorm_quant or pp_quantize_rows followed by pp_gemm_quant; weights take
  * pp_quantize_rows once, when they are loaded.  Same conventions as the single steps.  A prefill layer
- * is complete with pp_rope, pp_kv_scatter and pp_attention; for a decode step there is no single step that
- * appends to the caches or attends from one token, and pp_prefill, pp_decode_step and pp_generate take no 8-bit
+ * is complete with pp_rope, pp_kv_scatter and pp_attention, a decode step's with pp_paged_append and
+ * pp_paged_attention (over a paged cache, below); pp_prefill, pp_decode_step and pp_generate take no 8-bit
  * weights.
  *
  * The code of a row y of d values: scale = max|y| * (1/127) (the float32 product with the float32 1/127),
@@ -561,7 +561,7 @@ pp_status pp_paged_read(const pp_config* cfg, const pp_paged_cache* cache, const
 pp_status pp_paged_append(const pp_config* cfg, const pp_paged_cache* cache, const int32_t* lens, const void* qkv,
                           int64_t ldqkv, void* q_out, int64_t ldq, void* stream);
 
-/* Bytes of device workspace pp_paged_attention needs (they depend on the heads and cache->k alone).
+/* Bytes of device workspace pp_paged_attention needs (they depend on the heads, and on whether cache->k is 0).
  * Errors: as pp_paged_attention's checks of cfg and of the cache's sizes. */
 pp_status pp_paged_attention_workspace_size(const pp_config* cfg, const pp_paged_cache* cache, size_t* bytes);
 

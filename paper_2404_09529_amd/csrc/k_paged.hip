@@ -3,7 +3,7 @@
 //
 // A head's row of D values is D / 16 lanes' (8 for D = 128), side by side, so that its scale is a maximum over few
 // lanes; a lane has 8 values of each half of the row, the pairs that are rotated together, and every load is of whole lines.
-// Memory bounds the rows' kernels.  24,352 rows of 32 heads of 128: into 8-bit pages (604 MB) 144 us, 4.2 TB/s, where the
+// Memory bounds the rows' kernels.  24,349 rows of 32 heads of 128: into 8-bit pages (604 MB) 144 us, 4.2 TB/s, where the
 // codes' arithmetic is most of that time as well; back 102 us, 5.9 TB/s; 20,140 rows of 8 heads back 28 us, 4.5 TB/s.  The append is
 // latency: 2.9 us for one sequence, 4.5 for 64 (32 heads, 8-bit pages).
 #include "device.h"
