@@ -212,22 +212,21 @@ __device__ __forceinline__ void over(const float* x, int v0, int v1, F f) {
 
 __device__ __forceinline__ bool above(float t, int i, float u, int j) { return t > u || (t == u && i < j); }
 
-// A part of up to U kThreads ids is read once.
+struct Bins {
+    u64 sum[kBins];
+    uint32_t count[kBins];
+    float tops[kWaves];
+    int ids[kWaves];
+};
+// Ids v0 .. v1 - 1 into bins, by kThreads threads.  A part of up to U kThreads ids is read once and stays in `held`.  Barriers
+// around the powers and the bins are in here, the last one if there are bins: if E is near.
 template <int U>
-__global__ __launch_bounds__(kThreads, 4) void hist_kernel(ppk::Sample a, Space s, int parts, int size) {
-    __shared__ u64 sum[kBins];
-    __shared__ uint32_t count[kBins];
-    __shared__ Powers powers;
-    __shared__ float tops[kWaves];
-    __shared__ int ids[kWaves];
-    const int row = blockIdx.x / parts, tid = threadIdx.x, v0 = blockIdx.x % parts * size, v1 = min(v0 + size, a.vocab);
-    const float* x = a.logits + row * a.ldl;
-    const Settings set = settings_of(a, row);
-    for (int b = tid; b < kBins; b += kThreads) sum[b] = 0, count[b] = 0;
+__device__ __forceinline__ Part part_of(const float* x, int v0, int v1, const Settings& set, Bins& lds, Powers& powers, float (&held)[U]) {
+    const int tid = threadIdx.x;
+    for (int b = tid; b < kBins; b += kThreads) lds.sum[b] = 0, lds.count[b] = 0;
     powers.fill();
     float top = -INFINITY;
     int id = INT32_MAX;
-    float held[U];
     const bool once = v1 - v0 <= U * kThreads;
     auto each = [&](auto f) {
         if (once) {
@@ -247,30 +246,42 @@ __global__ __launch_bounds__(kThreads, 4) void hist_kernel(ppk::Sample a, Space 
         const int i = __shfl_xor(id, o, kWave);
         if (above(t, i, top, id)) top = t, id = i;
     }
-    if (tid % kWave == 0) tops[tid / kWave] = top, ids[tid / kWave] = id;
+    if (tid % kWave == 0) lds.tops[tid / kWave] = top, lds.ids[tid / kWave] = id;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w)
-        if (above(tops[w], ids[w], top, id)) top = tops[w], id = ids[w];
+        if (above(lds.tops[w], lds.ids[w], top, id)) top = lds.tops[w], id = lds.ids[w];
     const double c = scale_of(set.t);
     const bool none = set.greedy || top == -INFINITY;
     const double E = none ? -INFINITY : exponent_of(top, c);
-    if (tid == 0) s.part[blockIdx.x] = {E, top, id};
-    if (!near(E)) return;
+    if (!near(E)) return {E, top, id};
     const Scale sc(c, E);
     const bool counted = set.top_k > 0;
     each([&](float y, int) {
         const Depth d = sc.depth(y);
         if (!live(d)) return;
         const u64 w = weight(d, powers);
-        atomicAdd(&sum[bin_of(d)], w);
-        if (counted) atomicAdd(&count[bin_of(d)], 1u);
+        atomicAdd(&lds.sum[bin_of(d)], w);
+        if (counted) atomicAdd(&lds.count[bin_of(d)], 1u);
     });
     __syncthreads();
+    return {E, top, id};
+}
+
+template <int U>
+__global__ __launch_bounds__(kThreads, 4) void hist_kernel(ppk::Sample a, Space s, int parts, int size) {
+    __shared__ Bins lds;
+    __shared__ Powers powers;
+    const int row = blockIdx.x / parts, tid = threadIdx.x, v0 = blockIdx.x % parts * size, v1 = min(v0 + size, a.vocab);
+    const Settings set = settings_of(a, row);
+    float held[U];
+    const Part part = part_of(a.logits + row * a.ldl, v0, v1, set, lds, powers, held);
+    if (tid == 0) s.part[blockIdx.x] = part;
+    if (!near(part.E)) return;
     const int64_t out = int64_t(blockIdx.x) * kBins;
     for (int b = tid; b < kBins; b += kThreads) {
-        s.sum[out + b] = sum[b];
-        if (counted) s.count[out + b] = count[b];
+        s.sum[out + b] = lds.sum[b];
+        if (set.top_k > 0) s.count[out + b] = lds.count[b];
     }
 }
 
@@ -313,12 +324,87 @@ __device__ __forceinline__ Whole whole_of(const Part* p, int parts) {   // by ev
 // Octaves from one exponent down to another, both whole numbers.
 __device__ __forceinline__ int octaves(double E, double part) { return E == part ? 0 : static_cast<int>(fmin(E - part, 64.0)); }
 
+// A row's bins, for their running sums.
+struct Sums {
+    u64 sum[kScan + 1];        // of a bin, then of the bins before each
+    uint32_t count[kScan + 1];
+    u64 wave_sums[kWide / kWave];
+    uint32_t wave_counts[kWide / kWave];
+    int at[5];
+};
+// The plan of a row from its bins in `lds`, by N threads; barriers at the beginning and, behind the plan, the caller's.
+template <int N>
+__device__ __forceinline__ void plan_of(const Settings& set, double E, float top, Sums& lds, Plan* plan) {
+    constexpr int PER = kScan / N;   // neighbours that a thread adds up
+    const int tid = threadIdx.x;
+    if (tid < 5) lds.at[tid] = kBins - 1;
+    __syncthreads();
+    u64 sum[PER];
+    uint32_t count[PER];
+    u64 se = 0;
+    uint32_t ce = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        sum[i] = se += lds.sum[PER * tid + i];
+        count[i] = ce += lds.count[PER * tid + i];
+    }
+    se = block_scan<N / kWave>(se, lds.wave_sums) - se;
+    ce = set.top_k ? block_scan<N / kWave>(ce, lds.wave_counts) - ce : 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) lds.sum[PER * tid + i + 1] = se + sum[i], lds.count[PER * tid + i + 1] = ce + count[i];
+    if (tid == 0) lds.sum[0] = 0, lds.count[0] = 0;
+    __syncthreads();
+    const u64* sums = lds.sum;
+    const uint32_t* counts = lds.count;
+    const u64 all = sums[kScan];
+    // at[slot]: the bin in which the sum (or count) passes the bound; a barrier follows
+    auto passing = [&](int slot, auto before, auto bound) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int b = PER * tid + i;
+            if (!bound(before[b]) && bound(before[b + 1])) lds.at[slot] = b;   // one thread
+        }
+    };
+    u64 lo = all, hi = all;   // of what is kept
+    int bk = -1;
+    if (set.top_k > 0 && static_cast<uint32_t>(set.top_k) < counts[kScan]) {
+        passing(0, counts, [&](uint32_t n) { return n >= static_cast<uint32_t>(set.top_k); });
+        __syncthreads();
+        bk = lds.at[0];
+        lo = sums[bk], hi = sums[bk + 1];
+    }
+    int p0 = 0, p1 = -1, m0 = 0, m1 = -1;
+    if (set.top_p < 1.0) {
+        const double t0 = fmax(set.top_p * static_cast<double>(lo), 1.0), t1 = fmax(set.top_p * static_cast<double>(hi), 1.0);
+        passing(1, sums, [&](u64 n) { return static_cast<double>(n) >= t0; });
+        passing(2, sums, [&](u64 n) { return static_cast<double>(n) >= t1; });
+        __syncthreads();
+        p0 = lds.at[1], p1 = lds.at[2];
+        lo = min(lo, sums[p0]), hi = min(hi, sums[p1 + 1]);
+    }
+    if (set.min_p > 0.0) {
+        // 2^-depth = min_p 2^-depth(top), one bin more on both sides
+        const double d = Scale(scale_of(set.t), E).at(top) / 64.0 - log2(set.min_p);
+        const int b = static_cast<int>(fmin(d, 46.0) * kPerOctave);
+        m0 = min(max(b - 1, 0), kBins - 1), m1 = min(b + 1, kBins - 1);
+        lo = min(lo, sums[m0]), hi = min(hi, sums[m1 + 1]);
+    }
+    const double u0 = choice_bound(set.u, fmax(static_cast<double>(lo), 1.0)), u1 = choice_bound(set.u, static_cast<double>(hi));
+    passing(3, sums, [&](u64 n) { return static_cast<double>(n) > u0; });
+    passing(4, sums, [&](u64 n) { return static_cast<double>(n) > u1; });
+    __syncthreads();
+    for (int b = tid; b < kBins; b += N) plan->before[b] = sums[b];
+    if (tid == 0) {
+        plan->k_bin = bk, plan->k_before = bk >= 0 ? static_cast<int>(counts[bk]) : 0;
+        plan->p0 = p0, plan->p1 = p1, plan->m0 = m0, plan->m1 = m1, plan->s0 = lds.at[3], plan->s1 = lds.at[4];
+        plan->all = all;
+    }
+}
+
 __global__ __launch_bounds__(kWide) void sum_kernel(ppk::Sample a, Space s, int parts) {
-    __shared__ u64 sums[kScan + 1];        // of the bins before each
-    __shared__ uint32_t counts[kScan + 1];
-    __shared__ u64 wave_sums[kWide / kWave];
-    __shared__ uint32_t wave_counts[kWide / kWave];
-    __shared__ int at[5], shifts[kMaxParts];
+    __shared__ Sums lds;
+    __shared__ int shifts[kMaxParts];
     const int row = blockIdx.x, tid = threadIdx.x;
     const Settings set = settings_of(a, row);
     const Part* ps = s.part + int64_t(row) * parts;
@@ -327,7 +413,6 @@ __global__ __launch_bounds__(kWide) void sum_kernel(ppk::Sample a, Space s, int 
     if (tid == 0) plan->E = w.E, plan->top = w.top;
     if (set.greedy || !near(w.E)) return;
     if (tid < kMaxParts) shifts[tid] = tid < parts && near(ps[tid].E) ? octaves(w.E, ps[tid].E) : 64;
-    if (tid < 5) at[tid] = kBins - 1;
     __syncthreads();
     // the bins of all parts, eight parts in one wait for memory (without branches: a part too many is the last one again)
     u64 t[2] = {0, 0};
@@ -359,60 +444,45 @@ __global__ __launch_bounds__(kWide) void sum_kernel(ppk::Sample a, Space s, int 
             }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) sums[tid + i * kWide] = t[i], counts[tid + i * kWide] = n[i];
-    __syncthreads();
-    // two neighbours a thread
-    const u64 sum0 = sums[2 * tid], sum1 = sums[2 * tid + 1];
-    const uint32_t count0 = counts[2 * tid], count1 = counts[2 * tid + 1];
-    const u64 se = block_scan<kWide / kWave>(sum0 + sum1, wave_sums);
-    const uint32_t ce = set.top_k ? block_scan<kWide / kWave>(count0 + count1, wave_counts) : 0;
-    sums[2 * tid + 2] = se, sums[2 * tid + 1] = se - sum1;
-    counts[2 * tid + 2] = ce, counts[2 * tid + 1] = ce - count1;
-    if (tid == 0) sums[0] = 0, counts[0] = 0;
-    __syncthreads();
-    const u64 all = sums[kScan];
-    // at[slot]: the bin in which the sum (or count) passes the bound; a barrier follows
-    auto passing = [&](int slot, auto before, auto bound) {
+    for (int i = 0; i < 2; ++i) lds.sum[tid + i * kWide] = t[i], lds.count[tid + i * kWide] = n[i];
+    plan_of<kWide>(set, w.E, w.top, lds, plan);
+}
+
+// The bins whose ids matter.
+struct Wanted {
+    int bk, p0, p1, m0, m1, s0, s1;
+    __device__ __forceinline__ explicit Wanted(const Plan* p)
+        : bk(p->k_bin), p0(p->p0), p1(p->p1), m0(p->m0), m1(p->m1), s0(p->s0), s1(p->s1) {}
+    __device__ __forceinline__ bool has(int b) const {
+        return b == bk || (b >= p0 && b <= p1) || (b >= m0 && b <= m1) || (b >= s0 && b <= s1);
+    }
+};
+// A thread's hits of U ids as bits, the wavefront's in one reservation of the list's room.
+template <int U>
+__device__ __forceinline__ void gather(const float (&y)[U], int first, const Scale& sc, int shift, const Wanted& bins,
+                                       u64* list, int room, int& listed) {
+    const int lane = threadIdx.x % kWave;
+    uint32_t hits = 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int b = 2 * tid + i;
-            if (!bound(before[b]) && bound(before[b + 1])) at[slot] = b;   // one thread
+    for (int i = 0; i < U; ++i) {
+        const int whole = sc.whole(y[i]);
+        hits |= uint32_t(whole < kLive && bins.has((whole >> 1) + shift)) << i;
+    }
+    int n = __popc(hits), end = n;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int up = __shfl_up(end, o, kWave);
+        if (lane >= o) end += up;
+    }
+    int base = 0;
+    if (lane == kWave - 1 && end) base = atomicAdd(&listed, end);
+    int to = __shfl(base, kWave - 1, kWave) + end - n;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+        if (hits >> i & 1) {
+            if (to < room) list[to] = u64(~key_of(y[i])) << 32 | static_cast<uint32_t>(first + i * kThreads);
+            ++to;
         }
-    };
-    u64 lo = all, hi = all;   // of what is kept
-    int bk = -1;
-    if (set.top_k > 0 && static_cast<uint32_t>(set.top_k) < counts[kScan]) {
-        passing(0, counts, [&](uint32_t n) { return n >= static_cast<uint32_t>(set.top_k); });
-        __syncthreads();
-        bk = at[0];
-        lo = sums[bk], hi = sums[bk + 1];
-    }
-    int p0 = 0, p1 = -1, m0 = 0, m1 = -1;
-    if (set.top_p < 1.0) {
-        const double t0 = fmax(set.top_p * static_cast<double>(lo), 1.0), t1 = fmax(set.top_p * static_cast<double>(hi), 1.0);
-        passing(1, sums, [&](u64 n) { return static_cast<double>(n) >= t0; });
-        passing(2, sums, [&](u64 n) { return static_cast<double>(n) >= t1; });
-        __syncthreads();
-        p0 = at[1], p1 = at[2];
-        lo = min(lo, sums[p0]), hi = min(hi, sums[p1 + 1]);
-    }
-    if (set.min_p > 0.0) {
-        // 2^-depth = min_p 2^-depth(top), one bin more on both sides
-        const double d = Scale(scale_of(set.t), w.E).at(w.top) / 64.0 - log2(set.min_p);
-        const int b = static_cast<int>(fmin(d, 46.0) * kPerOctave);
-        m0 = min(max(b - 1, 0), kBins - 1), m1 = min(b + 1, kBins - 1);
-        lo = min(lo, sums[m0]), hi = min(hi, sums[m1 + 1]);
-    }
-    const double u0 = choice_bound(set.u, fmax(static_cast<double>(lo), 1.0)), u1 = choice_bound(set.u, static_cast<double>(hi));
-    passing(3, sums, [&](u64 n) { return static_cast<double>(n) > u0; });
-    passing(4, sums, [&](u64 n) { return static_cast<double>(n) > u1; });
-    __syncthreads();
-    for (int b = tid; b < kBins; b += kWide) plan->before[b] = sums[b];
-    if (tid == 0) {
-        plan->k_bin = bk, plan->k_before = bk >= 0 ? static_cast<int>(counts[bk]) : 0;
-        plan->p0 = p0, plan->p1 = p1, plan->m0 = m0, plan->m1 = m1, plan->s0 = at[3], plan->s1 = at[4];
-        plan->all = all;
-    }
 }
 
 template <int U>
@@ -425,7 +495,7 @@ __global__ __launch_bounds__(kThreads, 4) void gather_kernel(ppk::Sample a, Spac
     const float t = a.temperature ? a.temperature[row] : 1.f;
     const Plan* plan = s.plan + row;
     const double E = plan->E, part_E = s.part[blockIdx.x].E;
-    const int bk = plan->k_bin, p0 = plan->p0, p1 = plan->p1, m0 = plan->m0, m1 = plan->m1, s0 = plan->s0, s1 = plan->s1;
+    const Wanted bins(plan);
     if (!(t > 0.f)) return;   // (greedy: of the plan nothing is there but E)
     if (!near(E)) {
         if (tid == 0) s.listed[blockIdx.x] = kList + 1;
@@ -437,34 +507,9 @@ __global__ __launch_bounds__(kThreads, 4) void gather_kernel(ppk::Sample a, Spac
     u64* list = s.list + int64_t(blockIdx.x) * room;
     if (near(part_E)) {
         const Scale sc(scale_of(t), part_E);
-        const int shift = octaves(E, part_E) * kPerOctave, lane = tid % kWave;
-        // A thread's hits of U ids as bits, the wavefront's in one reservation.
-        auto chunk = [&](const float (&y)[U], int first) {
-            uint32_t hits = 0;
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int whole = sc.whole(y[i]), b = (whole >> 1) + shift;
-                const bool hit = b == bk || (b >= p0 && b <= p1) || (b >= m0 && b <= m1) || (b >= s0 && b <= s1);
-                hits |= uint32_t(whole < kLive && hit) << i;
-            }
-            int n = __popc(hits), end = n;
-#pragma unroll
-            for (int o = 1; o < kWave; o <<= 1) {
-                const int up = __shfl_up(end, o, kWave);
-                if (lane >= o) end += up;
-            }
-            int base = 0;
-            if (lane == kWave - 1 && end) base = atomicAdd(&listed, end);
-            int to = __shfl(base, kWave - 1, kWave) + end - n;
-#pragma unroll
-            for (int i = 0; i < U; ++i)
-                if (hits >> i & 1) {
-                    if (to < room) list[to] = u64(~key_of(y[i])) << 32 | static_cast<uint32_t>(first + i * kThreads);
-                    ++to;
-                }
-        };
+        const int shift = octaves(E, part_E) * kPerOctave;
         for (int v = v0;;) {
-            chunk(held, v + tid);
+            gather(held, v + tid, sc, shift, bins, list, room, listed);
             if ((v += U * kThreads) >= v1) break;
             read(x, v, v1, held);
         }
@@ -632,62 +677,22 @@ __device__ __forceinline__ u64 sort_lanes(u64 x, int i) {
     return x;
 }
 
-__global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int parts) {
-    __shared__ u64 list[kList];   // what of the order stands in the id's stead: ~key, id
-    __shared__ u64 run[kList];    // running sums
-    __shared__ uint16_t bins[kList], start[kBins];
-    __shared__ union {
-        Descent descent;
-        u64 waves[kPick / kWave];
-    } lds;
-    __shared__ Powers powers;
-    __shared__ int first[3], starts[kMaxParts + 1];
-    __shared__ u64 likely;
-    const int row = blockIdx.x, tid = threadIdx.x;
-    const Settings set = settings_of(a, row);
-    const Part* ps = s.part + int64_t(row) * parts;
-    if (set.greedy || whole_of(ps, parts).E == -INFINITY) {
-        const Whole w = whole_of(ps, parts);
-        const bool none = w.id == INT32_MAX || !set.greedy;
-        if (tid == 0) {
-            a.tokens[row] = none ? -1 : w.id;
-            if (a.prob) a.prob[row] = none ? 0.f : 1.f;
-        }
-        return;
-    }
-    powers.fill();
-    const Plan* plan = s.plan + row;
-    const AnyScale sc = {scale_of(set.t), plan->E};
-    const float top = plan->top;
-    // the parts' lists, one behind the other
-    if (tid < kWave) {
-        const int c = tid < parts ? s.listed[int64_t(row) * parts + tid] : 0;
-        int end = c > room_of(parts) ? kList + 1 : c;   // (sixteen of these stay small)
-#pragma unroll
-        for (int o = 1; o < kMaxParts; o <<= 1) {
-            const int up = __shfl_up(end, o, kWave);
-            if (tid >= o) end += up;
-        }
-        if (tid < kMaxParts) starts[tid + 1] = end;
-        if (tid == 0) starts[0] = 0;
-    }
-    __syncthreads();
-    const int n = starts[parts];
-    auto write = [&](int id, float x, u64 kept) {   // by one thread
-        a.tokens[row] = id;
-        if (a.prob)
-            a.prob[row] = static_cast<float>(power(sc.depth(x), powers) * (static_cast<double>(1ull << kUnitBits) / static_cast<double>(kept)));
-    };
-    if (n > kList || n == 0) {
-        __syncthreads();
-        const Place p = descend(a.logits + row * a.ldl, a.vocab, set, sc, top, powers, lds.descent);
-        if (tid == 0) write(p.id, p.x, p.sum);
-        return;
-    }
-    for (int p = tid / kWave; p < parts; p += kPick / kWave)   // a wavefront copies a part's
-        for (int i = starts[p] + tid % kWave; i < starts[p + 1]; i += kWave)
-            list[i] = s.list[(int64_t(row) * parts + p) * room_of(parts) + i - starts[p]];
-    __syncthreads();
+struct List {
+    u64 entry[kList];    // what of the order stands in the id's stead: ~key, id
+    u64 run[kList];      // running sums
+    uint16_t bins[kList], start[kBins];
+    u64 waves[kPick / kWave];
+    int first[3];
+    u64 likely;
+};
+// The place among the n > 0 entries of a list, in any order, by kPick threads; a barrier is behind the entries.
+template <typename F>
+__device__ __forceinline__ void choose(int n, const Settings& set, const AnyScale& sc, float top, const Powers& powers, const Plan* plan, List& lds, F write) {
+    const int tid = threadIdx.x;
+    u64 *list = lds.entry, *run = lds.run, *waves = lds.waves;
+    uint16_t *bins = lds.bins, *start = lds.start;
+    int* first = lds.first;
+    u64& likely = lds.likely;
     // Bitonic sort of the next power of two in registers, entry tid + kPick j in register j: partners less than 64 apart are
     // lanes, others less than kPick apart come through LDS.
     constexpr int kHeld = kList / kPick;
@@ -758,7 +763,7 @@ __global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int
         if (is) mine += weight(d, powers), bins[i] = static_cast<uint16_t>(bin[j]);
         total[j] = mine;
     }
-    const u64 up = block_scan<kPick / kWave>(mine, lds.waves) - mine;
+    const u64 up = block_scan<kPick / kWave>(mine, waves) - mine;
     if (tid < 3) first[tid] = n - 1;
     if (tid == 0) likely = plan->before[plan->m0];
 #pragma unroll
@@ -815,6 +820,115 @@ __global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int
     if (tid == 0) write(static_cast<int>(static_cast<uint32_t>(list[i])), logit_of(list[i]), kept);
 }
 
+// What a row's choice writes.
+struct Out {
+    const ppk::Sample& a;
+    int row;
+    __device__ __forceinline__ void none() const {
+        if (threadIdx.x) return;
+        a.tokens[row] = -1;
+        if (a.prob) a.prob[row] = 0.f;
+    }
+    __device__ __forceinline__ void greedy(int id) const {
+        if (threadIdx.x) return;
+        a.tokens[row] = id;
+        if (a.prob) a.prob[row] = 1.f;
+    }
+    __device__ __forceinline__ void operator()(int id, double weight, u64 kept) const {   // by one thread
+        a.tokens[row] = id;
+        if (a.prob) a.prob[row] = static_cast<float>(weight * (static_cast<double>(1ull << kUnitBits) / static_cast<double>(kept)));
+    }
+};
+
+__global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int parts) {
+    __shared__ union {
+        Descent descent;
+        List list;
+    } lds;
+    __shared__ Powers powers;
+    __shared__ int starts[kMaxParts + 1];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const Settings set = settings_of(a, row);
+    const Out out = {a, row};
+    const Whole w = whole_of(s.part + int64_t(row) * parts, parts);
+    if (set.greedy && w.id != INT32_MAX) return out.greedy(w.id);
+    if (w.E == -INFINITY) return out.none();
+    powers.fill();
+    const Plan* plan = s.plan + row;
+    const AnyScale sc = {scale_of(set.t), plan->E};
+    const float top = plan->top;
+    // the parts' lists, one behind the other
+    if (tid < kWave) {
+        const int c = tid < parts ? s.listed[int64_t(row) * parts + tid] : 0;
+        int end = c > room_of(parts) ? kList + 1 : c;   // (sixteen of these stay small)
+#pragma unroll
+        for (int o = 1; o < kMaxParts; o <<= 1) {
+            const int up = __shfl_up(end, o, kWave);
+            if (tid >= o) end += up;
+        }
+        if (tid < kMaxParts) starts[tid + 1] = end;
+        if (tid == 0) starts[0] = 0;
+    }
+    __syncthreads();
+    const int n = starts[parts];
+    auto write = [&](int id, float x, u64 kept) { out(id, power(sc.depth(x), powers), kept); };
+    if (n > kList || n == 0) {
+        __syncthreads();
+        const Place p = descend(a.logits + row * a.ldl, a.vocab, set, sc, top, powers, lds.descent);
+        if (tid == 0) write(p.id, p.x, p.sum);
+        return;
+    }
+    for (int p = tid / kWave; p < parts; p += kPick / kWave)   // a wavefront copies a part's
+        for (int i = starts[p] + tid % kWave; i < starts[p + 1]; i += kWave)
+            lds.list.entry[i] = s.list[(int64_t(row) * parts + p) * room_of(parts) + i - starts[p]];
+    __syncthreads();
+    choose(n, set, sc, top, powers, plan, lds.list, write);
+}
+
+// A row that one workgroup reads at once, from the logits to the token.
+template <int U>
+__global__ __launch_bounds__(kThreads) void row_kernel(ppk::Sample a) {
+    static_assert(kThreads == kPick && U * kThreads <= kList, "the same threads to the end, room for every id");
+    __shared__ union {
+        struct {
+            Bins bins;
+            Sums sums;
+        } first;
+        Descent descent;
+        List list;
+    } lds;
+    __shared__ Powers powers;
+    __shared__ Plan plan;
+    __shared__ int listed;
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const float* x = a.logits + row * a.ldl;
+    const Settings set = settings_of(a, row);
+    const Out out = {a, row};
+    float held[U];
+    if (tid == 0) listed = 0;
+    const Part part = part_of(x, 0, a.vocab, set, lds.first.bins, powers, held);
+    if (set.greedy && part.id != INT32_MAX) return out.greedy(part.id);
+    if (part.E == -INFINITY) return out.none();
+    const AnyScale sc = {scale_of(set.t), part.E};
+    auto write = [&](int id, float y, u64 kept) { out(id, power(sc.depth(y), powers), kept); };
+    if (!near(part.E)) {
+        __syncthreads();
+        const Place p = descend(x, a.vocab, set, sc, part.top, powers, lds.descent);
+        if (tid == 0) write(p.id, p.x, p.sum);
+        return;
+    }
+    for (int b = tid; b < kScan; b += kThreads) {
+        lds.first.sums.sum[b] = b < kBins ? lds.first.bins.sum[b] : 0;
+        lds.first.sums.count[b] = b < kBins ? lds.first.bins.count[b] : 0;
+    }
+    plan_of<kThreads>(set, part.E, part.top, lds.first.sums, &plan);
+    __syncthreads();
+    gather(held, tid, Scale(scale_of(set.t), part.E), 0, Wanted(&plan), lds.list.entry, kList, listed);
+    __syncthreads();
+    choose(listed, set, sc, part.top, powers, &plan, lds.list, write);
+}
+
+constexpr int kWhole = 4096;        // ids of a row that are one workgroup's in one launch
 constexpr int kRowsAtOnce = 1024;   // rows of a set of launches: the workspace's bound
 
 // Parts of a row: about 512 workgroups, of 4096 ids at least.
@@ -826,10 +940,14 @@ namespace ppk {
 
 size_t sample_workspace(int k, int vocab) {
     const int rows = min(k, kRowsAtOnce);
-    return rows ? space_bytes(rows, parts_of(rows, vocab)) : 0;
+    return rows && vocab > kWhole ? space_bytes(rows, parts_of(rows, vocab)) : 0;
 }
 
 void sample(const Sample& all, hipStream_t s) {
+    if (all.vocab <= kWhole) {
+        row_kernel<kWhole / kThreads><<<all.k, kThreads, 0, s>>>(all);
+        return;
+    }
     const int most = min(all.k, kRowsAtOnce), parts = parts_of(most, all.vocab), size = (all.vocab + parts - 1) / parts;
     const Space space = space_at(all.ws, most, parts);
     for (int r = 0; r < all.k; r += most) {
