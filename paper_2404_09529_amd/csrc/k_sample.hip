@@ -13,7 +13,8 @@
 //   gather_kernel  a part's ids in these bins.
 //   pick_kernel    the list in order, running sums behind what the bins before hold, and the places themselves.  A list that is
 //                  too long (thousands of nearly equal logits) is resolved by descent through the logit's bits instead.
-// Rows are split into up to 16 parts, so that a few rows fill the chip: the logits are read twice, the second time from
+// A row that fits one workgroup's registers goes all this way in one launch (row_kernel).  Other rows are split into up to 16
+// parts, so that a few rows fill the chip: the logits are read twice, the second time from
 // the caches.  64 rows of 128,256 logits (33 MB, 6.5 us at a large copy's rate) with settings of their own take 17.5, 9.5, 13.5
 // and 16.7 us: about 35 instructions, a third of them float64, and an atomic for each logit, which all workgroups come to together
 // behind their loads; the latency of a workgroup; loads, then prefix sums; the order of the longest list (1,325 ids: 2048
@@ -175,8 +176,8 @@ struct Space {
 // Room for a part's ids: a quarter of what pick_kernel takes, or all of it for a row that is one part.
 __host__ __device__ constexpr int room_of(int parts) { return parts == 1 ? kList : kList / 4; }
 
-size_t space_bytes(int k, int parts) {
-    return size_t(k) * parts * (kBins * 12 + sizeof(Part) + room_of(parts) * 8 + 4) + size_t(k) * sizeof(Plan);
+size_t space_bytes(int rows, int parts, size_t room) {   // of `parts` parts in all
+    return size_t(rows) * sizeof(Plan) + size_t(parts) * (kBins * 12 + sizeof(Part) + 4) + room * 8;
 }
 Space space_at(void* ws, int k, int parts) {
     Space s;
@@ -462,13 +463,13 @@ template <int U>
 __device__ __forceinline__ void gather(const float (&y)[U], int first, const Scale& sc, int shift, const Wanted& bins,
                                        u64* list, int room, int& listed) {
     const int lane = threadIdx.x % kWave;
-    uint32_t hits = 0;
+    std::conditional_t<(U > 32), u64, uint32_t> hits = 0;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int whole = sc.whole(y[i]);
-        hits |= uint32_t(whole < kLive && bins.has((whole >> 1) + shift)) << i;
+        hits |= decltype(hits)(whole < kLive && bins.has((whole >> 1) + shift)) << i;
     }
-    int n = __popc(hits), end = n;
+    int n = U > 32 ? __popcll(hits) : __popc(hits), end = n;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
         const int up = __shfl_up(end, o, kWave);
@@ -885,10 +886,11 @@ __global__ __launch_bounds__(kPick) void pick_kernel(ppk::Sample a, Space s, int
     choose(n, set, sc, top, powers, plan, lds.list, write);
 }
 
-// A row that one workgroup reads at once, from the logits to the token.
+// A row that one workgroup reads at once, from the logits to the token.  512 threads, two wavefronts a SIMD: with 64 logits held
+// a thread has 253 registers.
 template <int U>
 __global__ __launch_bounds__(kThreads) void row_kernel(ppk::Sample a) {
-    static_assert(kThreads == kPick && U * kThreads <= kList, "the same threads to the end, room for every id");
+    static_assert(kThreads == kPick, "the same threads to the end");
     __shared__ union {
         struct {
             Bins bins;
@@ -911,12 +913,12 @@ __global__ __launch_bounds__(kThreads) void row_kernel(ppk::Sample a) {
     if (part.E == -INFINITY) return out.none();
     const AnyScale sc = {scale_of(set.t), part.E};
     auto write = [&](int id, float y, u64 kept) { out(id, power(sc.depth(y), powers), kept); };
-    if (!near(part.E)) {
+    auto by_descent = [&] {
         __syncthreads();
         const Place p = descend(x, a.vocab, set, sc, part.top, powers, lds.descent);
         if (tid == 0) write(p.id, p.x, p.sum);
-        return;
-    }
+    };
+    if (!near(part.E)) return by_descent();
     for (int b = tid; b < kScan; b += kThreads) {
         lds.first.sums.sum[b] = b < kBins ? lds.first.bins.sum[b] : 0;
         lds.first.sums.count[b] = b < kBins ? lds.first.bins.count[b] : 0;
@@ -925,28 +927,39 @@ __global__ __launch_bounds__(kThreads) void row_kernel(ppk::Sample a) {
     __syncthreads();
     gather(held, tid, Scale(scale_of(set.t), part.E), 0, Wanted(&plan), lds.list.entry, kList, listed);
     __syncthreads();
+    if (U * kThreads > kList && listed > kList) return by_descent();
     choose(listed, set, sc, part.top, powers, &plan, lds.list, write);
 }
 
-constexpr int kWhole = 4096;        // ids of a row that are one workgroup's in one launch
 constexpr int kRowsAtOnce = 1024;   // rows of a set of launches: the workspace's bound
 
 // Parts of a row: about 512 workgroups, of 4096 ids at least.
 int parts_of(int rows, int vocab) { return std::max(1, std::min({512 / rows, (vocab + 4095) / 4096, kMaxParts})); }
 
+// Logits that each thread of a row's one workgroup holds, or 0: rows in parts.  In us, four launches and one: one row of 1000
+// logits 22 and 12, of 4096 23 and 13, of 8192 24 and 17, of 16,384 24.6 and 23.2, of 32,000 25 and 36; 64 rows 26 and 14, 26 and
+// 15, 28 and 18, 28 and 25, 31 and 39; 128 rows of 20,000 and 32,000 43 and 35, 45 and 41; 256 46 and 34, 51 and 42.
+int whole_row(int k, int vocab) {
+    return vocab <= 8 * kThreads ? 8 : vocab <= 16 * kThreads ? 16 : vocab <= 32 * kThreads ? 32 : vocab <= 64 * kThreads && k >= 128 ? 64 : 0;
+}
+
 }  // namespace
 
 namespace ppk {
 
+// (Not less for more rows, so that the largest batch's serves all.)
 size_t sample_workspace(int k, int vocab) {
-    const int rows = min(k, kRowsAtOnce);
-    return rows && vocab > kWhole ? space_bytes(rows, parts_of(rows, vocab)) : 0;
+    if (whole_row(1, vocab) || !k) return 0;
+    const int rows = min(k, kRowsAtOnce), most = max(min(rows * parts_of(1, vocab), 512), rows);
+    return space_bytes(rows, most, rows > 256 ? size_t(rows) * room_of(1) : size_t(most) * room_of(2));
 }
 
 void sample(const Sample& all, hipStream_t s) {
-    if (all.vocab <= kWhole) {
-        row_kernel<kWhole / kThreads><<<all.k, kThreads, 0, s>>>(all);
-        return;
+    switch (whole_row(all.k, all.vocab)) {
+        case 8: row_kernel<8><<<all.k, kThreads, 0, s>>>(all); return;
+        case 16: row_kernel<16><<<all.k, kThreads, 0, s>>>(all); return;
+        case 32: row_kernel<32><<<all.k, kThreads, 0, s>>>(all); return;
+        case 64: row_kernel<64><<<all.k, kThreads, 0, s>>>(all); return;
     }
     const int most = min(all.k, kRowsAtOnce), parts = parts_of(most, all.vocab), size = (all.vocab + parts - 1) / parts;
     const Space space = space_at(all.ws, most, parts);

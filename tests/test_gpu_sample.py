@@ -158,28 +158,31 @@ def test_ties():
     assert run(y, u=[0.999, 0.5], top_p=[0.5, 1.0])[0] == [70, 200]
 
 
-def test_close_logits():
+@pytest.mark.parametrize("v", [5000, 15000, 36000])
+def test_close_logits(v):
     """Thousands of ids within one float32 step of each other's neighbours: every bit of the logit decides."""
     base = np.float32(12.0).view(np.int32)
     bits = base + np.random.default_rng(1).permutation(5000).astype(np.int32)
-    x = torch.from_numpy(bits.view(np.float32).copy())[None].repeat(4, 1)
+    x = torch.full((4, v), -100.0)
+    x[:, :5000] = torch.from_numpy(bits.view(np.float32).copy())
     check(x, u=[0.1, 0.5, 0.9, 0.3], top_k=[0, 1, 4000, 77], top_p=[1.0, 1.0, 0.5, 1.0])
 
 
-def test_masked_and_special_logits():
+@pytest.mark.parametrize("v", [2000, 10000, 20000])
+def test_masked_and_special_logits(v):
     """-inf and NaN are never chosen, +inf takes everything; rows with nothing left."""
     inf, nan, low = float("inf"), float("nan"), torch.finfo(torch.float32).min
-    x = logits(9, 2000, 3)
+    x = logits(9, v, 3)
     x[0, 5:] = -inf
     x[1, ::2] = nan
     x[2, [7, 9]] = inf
     x[3] = -inf
     x[4] = nan
-    x[5, :1999] = low
+    x[5, :v - 1] = low
     x[6] = low
     x[7, 1:] = nan
     x[7, 0] = -inf
-    x[8] = torch.where(torch.arange(2000) % 2 == 0, 3e38, -3e38)
+    x[8] = torch.where(torch.arange(v) % 2 == 0, 3e38, -3e38)
     for u in (0.0, 0.4, 0.99999):
         tokens = check(x, u=[u] * 9)
         assert tokens[3] == tokens[4] == tokens[7] == -1 and tokens[2] in (7, 9) and tokens[0] < 5
@@ -188,8 +191,9 @@ def test_masked_and_special_logits():
     assert greedy[3] == 0 and greedy[4] == -1 and greedy[7] == 0
 
 
-def test_temperatures_at_their_ends():
-    x = logits(7, 5000, 4)
+@pytest.mark.parametrize("v", [3000, 5000, 12000, 40000])
+def test_temperatures_at_their_ends(v):
+    x = logits(7, v, 4)
     check(x, u=[0.6] * 7, t=[1e-38, 1e-45, 3e38, float("inf"), -1.0, float("nan"), 1e-3])
 
 
@@ -267,9 +271,9 @@ def test_two_streams_at_once():
     assert [o.cpu().tolist() for o in out] == want
 
 
-def test_more_rows_than_at_once():
-    """1500 rows, settings of their own, in several sets of launches."""
-    k, v = 1500, 40
+@pytest.mark.parametrize("k,v", [(1500, 40), (1100, 33000)])
+def test_more_rows_than_at_once(k, v):
+    """Settings of their own; the larger rows in two sets of launches."""
     g = torch.Generator().manual_seed(5)
     r = lambda n: torch.rand(n, generator=g).tolist()
     check(logits(k, v, 6, 1.5), t=[0.0 if x < 0.1 else 0.3 + 2 * x for x in r(k)], top_k=[int(50 * x) for x in r(k)],
@@ -289,3 +293,32 @@ def test_largest_vocabularies_of_equal_logits(v):
     assert all(abs(p * v - 1) <= 2.0 ** -23 for p in prob)
     tokens, prob = run(x, u=u, top_k=[1000] * 8, top_p=[0.5] * 8)
     assert tokens == [min(int(a * 500), 499) for a in u]
+
+
+# sizes around those where the way changes
+WAYS = [(1, 4096), (2, 4097), (3, 8192), (2, 8193), (2, 16384), (2, 16385), (127, 20001), (130, 20001), (128, 32768), (128, 32769)]
+
+
+@pytest.mark.parametrize("name", ["plain", "hot", "nucleus", "wide", "all", "min-p", "greedy"])
+@pytest.mark.parametrize("k,v", WAYS)
+def test_ways(name, k, v):
+    x = logits(k, v, v + k)
+    x[0, 7::5] = float("-inf")
+    x[k - 1, 3::9] = float("nan")
+    u = torch.rand(k, generator=torch.Generator().manual_seed(k)).tolist()
+    check(x, u=u, **{n: [y] * k for n, y in SETTINGS[name].items()})
+
+
+@pytest.mark.parametrize("k,v", [(2, 4096), (3, 8000), (3, 16384), (128, 32768), (3, 32768)])
+def test_ways_with_equal_logits(k, v):
+    """More equal logits, and nearly equal ones, than a list holds."""
+    x = torch.zeros(k, v)
+    x[1] = 1e-6 * torch.randn(v, generator=torch.Generator().manual_seed(2))
+    x[k - 1, 5] = float("nan")
+    u = [(i + 0.5) / k for i in range(k)]
+    check(x, u=u)
+    check(x, u=u, top_k=[v // 3] * k, top_p=[0.75] * k)
+    tokens, prob = run(x, u=u, t=[1e-30] * k)            # exponents of 2^30 and more
+    for i in range(k):
+        token, share, near = definition(x[i].numpy(), 1e-30, u=u[i])
+        assert near or (tokens[i] == token and abs(prob[i] - share) <= 2.0 ** -23 * share)

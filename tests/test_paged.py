@@ -139,6 +139,9 @@ def test_sample_workspace():
             assert _sample(ws=None, **kw) == INV
             assert _sample(ws=0x10010, **kw) == INV
             assert _sample(bytes=need - 1, **kw) == SMALL
+    for vocab in (1000, 16384, 16385, 32000, 40000, 128256):    # the largest batch's workspace serves all
+        sizes = [pp.pp_sample_workspace_size(k, vocab) for k in range(1, 1400)]
+        assert sizes == sorted(sizes)
     for bad in [(-1, 10), (1, 0), (1, 1 << 20)]:
         with pytest.raises(pp.PrepackError):
             pp.pp_sample_workspace_size(*bad)
