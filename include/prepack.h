@@ -596,7 +596,8 @@ pp_status pp_sample_workspace_size(int32_t k, int32_t vocab, size_t* bytes);
  *   NaN logits are never chosen, nor is -inf with T > 0 (no other logit: token -1, prob 0); ids of +inf share the sum evenly.
  *   tokens device int32 [k]; prob device float32 [k]; vocab below 2^20.
  * w is computed in float64 and summed exactly, as a multiple of 2^-44 (ids below 2^-45 of the likeliest are never chosen).
- * workspace: >= pp_sample_workspace_size bytes, 256-byte aligned, not used by two calls at a time.  Deterministic.
+ * workspace: >= pp_sample_workspace_size bytes (never less for a larger k), 256-byte aligned, not used by two calls at a
+ * time.  Deterministic; a bound within that step of a place may take the id beside it with another k.
  * Errors: PP_ERR_INVALID_ARG (NULL logits, u or tokens, k < 0, vocab <= 0, ldl < vocab, misaligned workspace),
  *         PP_ERR_UNSUPPORTED (vocab), PP_ERR_BUFFER_TOO_SMALL (workspace), PP_ERR_HIP. */
 pp_status pp_sample(const float* logits, int64_t ldl, int32_t k, int32_t vocab, const float* temperature,
