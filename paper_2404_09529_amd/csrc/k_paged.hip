@@ -3,9 +3,9 @@
 //
 // A head's row of D values is D / 16 lanes' (8 for D = 128), side by side, so that its scale is a maximum over few
 // lanes; a lane has 8 values of each half of the row, the pairs that are rotated together, and every load is of whole lines.
-// Memory bounds the rows' kernels.  24,349 rows of 32 heads of 128: into 8-bit pages (604 MB) 144 us, 4.2 TB/s, where the
-// codes' arithmetic is most of that time as well; back 102 us, 5.9 TB/s; 20,140 rows of 8 heads back 28 us, 4.5 TB/s.  The append is
-// latency: 2.9 us for one sequence, 4.5 for 64 (32 heads, 8-bit pages).
+// Memory bounds the rows' kernels.  24,349 rows of 32 heads of 128: into 8-bit pages (604 MB) 125 us by itself, 4.8 TB/s, and 143
+// behind a kernel whose 403 MB are still on their way to memory; back 102 us, 5.9 TB/s; 20,140 rows of 8 heads back 27-28 us, 4.5
+// TB/s.  The append is latency: 2.9 us for one sequence, 4.4 for 64 (32 heads, 8-bit pages).
 #include "device.h"
 #include "kernels.h"
 #include "paged.h"
@@ -73,7 +73,9 @@ __device__ __forceinline__ int32_t place(const ppk::PagedCache& c, int32_t seq, 
 // A thread has dims j .. j + 7 and D / 2 + j .. + 7 of a head's row (one of 2 Hkv D / 16 columns, those of the keys first)
 // and kAhead rows on the way at once; a workgroup has `wide` columns of kBlock / wide rows, kAhead times.  In us, the first
 // figures above: 8 values a thread and one row at a time 149 and 120 (and 43 of 8 heads), two 156 and 151, four 156 and 117,
-// eight 154 and 108; 16 values and four rows 148 and 101, but few rows are slower (115 into bf16 pages: 4.1 and 3.8).
+// eight 154 and 108; 16 values
+// and two rows 144 and 102, four 148 and 101 and few rows slower (459 rows of 16 heads into bf16 pages: 3.8 and 4.1).  16
+// neighbouring values, whole 16-byte pieces of codes: 143 and 120.
 constexpr int kAhead = 2;
 template <int D, typename T, typename P, bool WRITE>
 __global__ __launch_bounds__(kBlock) void paged_rows_kernel(ppk::PagedCache c, const int32_t* __restrict__ seq,
