@@ -71,11 +71,10 @@ __device__ __forceinline__ int32_t place(const ppk::PagedCache& c, int32_t seq, 
 }
 
 // A thread has dims j .. j + 7 and D / 2 + j .. + 7 of a head's row (one of 2 Hkv D / 16 columns, those of the keys first)
-// and kAhead rows on the way at once; a workgroup has `wide` columns of kBlock / wide rows, kAhead times.  In us, the first
-// figures above: 8 values a thread and one row at a time 149 and 120 (and 43 of 8 heads), two 156 and 151, four 156 and 117,
-// eight 154 and 108; 16 values
-// and two rows 144 and 102, four 148 and 101 and few rows slower (459 rows of 16 heads into bf16 pages: 3.8 and 4.1).  16
-// neighbouring values, whole 16-byte pieces of codes: 143 and 120.
+// and kAhead rows on the way at once; a workgroup has `wide` columns of kBlock / wide rows, kAhead times.  In us, the rows of 32
+// heads written and read back in turn: 8 values a thread and one row at a time 149 and 120, two 156 and 151, four 156 and 117,
+// eight 154 and 108; 16 values and two rows 144 and 102, four 148 and 101, and few rows are slower then (459 rows of 16 heads into bf16
+// pages: 3.8 and 4.1); 16 neighbouring values, codes in whole pieces of 16 bytes, 143 and 120.
 constexpr int kAhead = 2;
 template <int D, typename T, typename P, bool WRITE>
 __global__ __launch_bounds__(kBlock) void paged_rows_kernel(ppk::PagedCache c, const int32_t* __restrict__ seq,
