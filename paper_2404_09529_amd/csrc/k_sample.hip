@@ -31,12 +31,13 @@ namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
 constexpr int kUnitBits = 44, kPerOctave = 32;
-constexpr int kBins = 46 * kPerOctave;          // weights below 2^-45 are none
+constexpr int kLive = 45 * 64;                  // 64ths of an octave: weights below 2^-45 are none
+constexpr int kBins = kLive / 2;                // of a part, and of the row: what falls behind is none, whatever part it is in
 constexpr int kWide = 1024;                     // threads that sum a row's parts
 constexpr int kScan = 2 * kWide;                // bins as they hold them, two each
 constexpr int kPick = 512;                      // threads that choose
 constexpr int kList = 4096, kMaxParts = 16;
-static_assert(kScan >= kBins, "two bins a thread");
+static_assert(kScan >= kBins && 2 * kPerOctave == 64, "two bins a thread, two 64ths a bin");
 typedef unsigned long long u64;
 
 // Integers ordered as the logits are (NaN excepted); both zeros are one.
@@ -99,7 +100,6 @@ struct AnyScale {
     }
 };
 __device__ __forceinline__ double scale_of(float t) { return 1.4426950408889634 / static_cast<double>(t); }
-constexpr int kLive = 45 * 64;
 __device__ __forceinline__ bool live(const Depth& d) { return d.whole < kLive; }
 __device__ __forceinline__ int bin_of(const Depth& d) { return d.whole >> 1; }   // of a live id
 
@@ -117,8 +117,9 @@ __device__ __forceinline__ double series(const Depth& d, const Powers& p) {
 // whole = 64 q - i with 0 <= i < 64: 2^-(whole / 64) = 2^(i / 64) 2^-q
 __device__ __forceinline__ int octave_of(const Depth& d) { return (d.whole + 63) >> 6; }
 __device__ __forceinline__ double power(const Depth& d, const Powers& p) { return ldexp(series(d, p), -octave_of(d)); }
-// 2^(44 - depth) rounded: adding 2^52 leaves the whole number in the low bits.
+// 2^(44 - depth) rounded, 0 where there is none: adding 2^52 leaves the whole number in the low bits.
 __device__ __forceinline__ u64 weight(const Depth& d, const Powers& p) {
+    if (!live(d)) return 0;   // (the exponent below would wrap)
     const double unit = __hiloint2double((1023 + kUnitBits - octave_of(d)) << 20, 0);   // 2^(44 - octave)
     return static_cast<u64>(__double_as_longlong(fma(series(d, p), unit, 0x1p52))) & ((1ull << 52) - 1);
 }
@@ -438,8 +439,8 @@ __global__ __launch_bounds__(kWide) void sum_kernel(ppk::Sample a, Space s, int 
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int p = 0; p < 8; ++p) {
-                // (a part without anything, 64 octaves down, has written no bins)
-                const bool has = from(i, p) >= 0 && from(i, p) < kBins;
+                // (a part without anything, 64 octaves down, has written no bins; a part's last bins may lie behind the row's)
+                const bool has = from(i, p) >= 0 && from(i, p) < kBins && tid + i * kWide < kBins;
                 t[i] += has ? x[i][p] >> (shifts[p0 + p] & 63) : 0;
                 n[i] += has ? c[i][p] : 0;
             }
