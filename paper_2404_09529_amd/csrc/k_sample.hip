@@ -547,7 +547,7 @@ struct Descent {
 // The first place, in order, where the running count or sum passes the bound; there is one.
 __device__ Place find(const float* x, int vocab, const AnyScale& sc, const Powers& powers, Bound what, double bound, Descent& lds) {
     const int tid = threadIdx.x, lane = tid % kWave;
-    uint32_t prefix = 0, mask = 0, above_n = 0;
+    uint32_t prefix = 0, mask = 0, above_n = 0, equal = 0;   // the last digit's ids: equal logits
     u64 above_s = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
         __syncthreads();
@@ -569,13 +569,13 @@ __device__ Place find(const float* x, int vocab, const AnyScale& sc, const Power
         if (tid < 256 && !passes(what, es - s, en - n, bound) && passes(what, es, en, bound))
             lds.digit = 255 - tid, lds.above_sum = es - s, lds.above_count = en - n;
         __syncthreads();
-        above_s = lds.above_sum, above_n = lds.above_count;
+        above_s = lds.above_sum, above_n = lds.above_count, equal = lds.count[lds.digit];
         prefix |= static_cast<uint32_t>(lds.digit) << shift;
         mask |= 255u << shift;
     }
     const float v = of_key(prefix);
     const u64 w = weight(sc.depth(v), powers);
-    uint32_t lo = 1, hi = vocab;   // the number of equal logits that passes
+    uint32_t lo = 1, hi = equal;   // the number of them that passes (the sum of more than there are may pass 64 bits)
     while (lo < hi) {
         const uint32_t mid = (lo + hi) / 2;
         if (passes(what, above_s + w * mid, above_n + mid, bound)) hi = mid;

@@ -103,3 +103,21 @@ def test_confident_rows(v, rows_of_a_call, limits):
     u = [[0.0, 0.5, 0.9, 1 - 2.0 ** -24, float(torch.rand(1, generator=g))][i // 2 % 5] for i in range(rows)]
     check(x, rows_of_a_call, t=[t for _, t in pairs], u=u, **({} if limits == "min-p" else dict(top_k=k)),
           **{n: [y] * rows for n, y in LIMITS[limits].items()})
+
+
+@pytest.mark.parametrize("v", [800_000, 2 ** 20 - 1])
+def test_groups_of_equal_logits_in_the_largest_rows(v):
+    """Sums close to 2^64, and an id that lies among equal ones behind others."""
+    g = torch.Generator().manual_seed(v)
+    mixed = torch.randperm(v, generator=g)
+    x = torch.zeros(8, v)
+    x[0:3, mixed[:v // 4]] = -1e-7
+    x[3, mixed[:v // 2]] = -0.25
+    x[4, mixed[:v // 100]] = -1e-7
+    x[5, mixed[:v - v // 100]] = -3e-7
+    x[6:] = -10 - torch.randn(2, v, generator=g)
+    x[7] = torch.round(4 * x[7]) / 4                         # some dozens of values
+    t = [1.0] * 6 + [1e6] * 2
+    u = [0.9, 0.76, 1 - 2.0 ** -24, 0.8, 0.995, 0.5, 0.97, 0.9]
+    check(x, 8, t=t, u=u)
+    check(x, 8, t=t, u=u, top_k=[v - 5] * 8, top_p=[0.95] * 8)
