@@ -595,9 +595,10 @@ pp_status pp_sample_workspace_size(int32_t k, int32_t vocab, size_t* bytes);
  *   top_k <= 0, top_p >= 1 and min_p <= 0 (or NaN) are no limit; u below 0 or NaN counts as 0, u >= 1 gives the last kept id.
  *   NaN logits are never chosen, nor is -inf with T > 0 (no other logit: token -1, prob 0); ids of +inf share the sum evenly.
  *   tokens device int32 [k]; prob device float32 [k]; vocab below 2^20.
- * w is computed in float64 and summed exactly, as a multiple of 2^-44 (ids below 2^-45 of the likeliest are never chosen).
+ * w is computed in float64 and summed in whole steps of 2^-44 to 2^-43, the likeliest id being 1 (ids below 2^-45 of it are
+ * never chosen, ids below 2^-43 need not be).
  * workspace: >= pp_sample_workspace_size bytes (never less for a larger k), 256-byte aligned, not used by two calls at a
- * time.  Deterministic; a bound within that step of a place may take the id beside it with another k.
+ * time.  Deterministic; a bound within half a step per id of a place may take the id beside it with another k.
  * Errors: PP_ERR_INVALID_ARG (NULL logits, u or tokens, k < 0, vocab <= 0, ldl < vocab, misaligned workspace),
  *         PP_ERR_UNSUPPORTED (vocab), PP_ERR_BUFFER_TOO_SMALL (workspace), PP_ERR_HIP. */
 pp_status pp_sample(const float* logits, int64_t ldl, int32_t k, int32_t vocab, const float* temperature,

@@ -129,7 +129,7 @@ struct Settings {
     float t;
     int top_k;
     double top_p, min_p, u;   // 1 and more: no limit; 0: no limit; in [0, 1]
-    bool greedy;
+    bool greedy, last;        // last: u is 1 or more, the last kept id whatever the sums' last bits
 };
 __device__ __forceinline__ Settings settings_of(const ppk::Sample& a, int row) {
     Settings s;
@@ -140,17 +140,15 @@ __device__ __forceinline__ Settings settings_of(const ppk::Sample& a, int row) {
     s.top_p = p < 1.f ? static_cast<double>(p) : 1.0;
     s.min_p = m > 0.f ? fmin(static_cast<double>(m), 1.0) : 0.0;
     s.u = u >= 0.f ? static_cast<double>(u) : 0.0;
+    s.last = u >= 1.f;
     return s;
 }
 // exp((x - top) / T), as min-p asks for it.
 __device__ __forceinline__ double share_of(float x, float top, const Settings& s) {
     return x == top ? 1.0 : exp((static_cast<double>(x) - static_cast<double>(top)) / static_cast<double>(s.t));
 }
-// The bound that the chosen id's running sum exceeds; it is below the sum.
-__device__ __forceinline__ double choice_bound(double u, double sum) {
-    const double below = nextafter(sum, 0.0);
-    return u < 1.0 ? fmin(u * sum, below) : below;
-}
+// The bound that the chosen id's running sum exceeds, u below 1; it is below the sum.
+__device__ __forceinline__ double choice_bound(double u, double sum) { return fmin(u * sum, nextafter(sum, 0.0)); }
 
 struct Part {   // of a row, by hist_kernel
     double E;   // -inf: no id that may be chosen
@@ -393,8 +391,9 @@ __device__ __forceinline__ void plan_of(const Settings& set, double E, float top
         lo = min(lo, sums[m0]), hi = min(hi, sums[m1 + 1]);
     }
     const double u0 = choice_bound(set.u, fmax(static_cast<double>(lo), 1.0)), u1 = choice_bound(set.u, static_cast<double>(hi));
-    passing(3, sums, [&](u64 n) { return static_cast<double>(n) > u0; });
-    passing(4, sums, [&](u64 n) { return static_cast<double>(n) > u1; });
+    lo = max(lo, u64(1));
+    passing(3, sums, [&](u64 n) { return set.last ? n >= lo : static_cast<double>(n) > u0; });
+    passing(4, sums, [&](u64 n) { return set.last ? n >= hi : static_cast<double>(n) > u1; });
     __syncthreads();
     for (int b = tid; b < kBins; b += N) plan->before[b] = sums[b];
     if (tid == 0) {
@@ -441,7 +440,8 @@ __global__ __launch_bounds__(kWide) void sum_kernel(ppk::Sample a, Space s, int 
             for (int p = 0; p < 8; ++p) {
                 // (a part without anything, 64 octaves down, has written no bins; a part's last bins may lie behind the row's)
                 const bool has = from(i, p) >= 0 && from(i, p) < kBins && tid + i * kWide < kBins;
-                t[i] += has ? x[i][p] >> (shifts[p0 + p] & 63) : 0;
+                const int down = shifts[p0 + p] & 63;   // to the nearest: a bin with an id in it is not 0
+                t[i] += has ? (x[i][p] + ((1ull << down) >> 1)) >> down : 0;
                 n[i] += has ? c[i][p] : 0;
             }
     }
@@ -531,7 +531,8 @@ __device__ __forceinline__ bool passes(Bound b, u64 sum, uint32_t count, double 
 
 struct Place {
     int id;
-    u64 sum;   // of the ids up to this one
+    u64 sum;      // of the ids up to this one
+    uint32_t n;   // and how many they are
     float x;
 };
 struct Descent {
@@ -600,19 +601,19 @@ __device__ Place find(const float* x, int vocab, const AnyScale& sc, const Power
     __syncthreads();
     const int id = lds.found;
     __syncthreads();
-    return {id, above_s + w * lo, v};
+    return {id, above_s + w * lo, above_n + lo, v};
 }
 
 __device__ Place descend(const float* x, int vocab, const Settings& set, const AnyScale& sc, float top, const Powers& powers,
                          Descent& lds) {
     u64 all = 0, likely = 0;
-    uint32_t count = 0;
+    uint32_t count = 0, likely_n = 0;
     over<4, kPick>(x, 0, vocab, [&](float y, int) {
         const Depth d = sc.depth(y);
         if (!live(d)) return;
         const u64 w = weight(d, powers);
         all += w, ++count;
-        if (share_of(y, top, set) >= set.min_p) likely += w;
+        if (share_of(y, top, set) >= set.min_p) likely += w, ++likely_n;
     });
     auto total = [&](auto v, auto* waves) {
         v = block_scan<kPick / kWave>(v, waves);
@@ -626,11 +627,13 @@ __device__ Place descend(const float* x, int vocab, const Settings& set, const A
     u64 kept = total(all, lds.wave_sum);
     likely = total(likely, lds.wave_sum);
     count = total(count, lds.wave_count);
-    if (set.top_k && static_cast<uint32_t>(set.top_k) < count) kept = find(x, vocab, sc, powers, kCount, set.top_k, lds).sum;
-    if (set.top_p < 1.0)
-        kept = find(x, vocab, sc, powers, kReaches, fmax(set.top_p * static_cast<double>(kept), 1.0), lds).sum;
-    kept = min(kept, likely);
-    Place p = find(x, vocab, sc, powers, kExceeds, choice_bound(set.u, static_cast<double>(kept)), lds);
+    likely_n = total(likely_n, lds.wave_count);
+    auto keep = [&](const Place& p) { kept = p.sum, count = p.n; };
+    if (set.top_k && static_cast<uint32_t>(set.top_k) < count) keep(find(x, vocab, sc, powers, kCount, set.top_k, lds));
+    if (set.top_p < 1.0) keep(find(x, vocab, sc, powers, kReaches, fmax(set.top_p * static_cast<double>(kept), 1.0), lds));
+    kept = min(kept, likely), count = min(count, likely_n);
+    Place p = set.last ? find(x, vocab, sc, powers, kCount, count, lds)
+                       : find(x, vocab, sc, powers, kExceeds, choice_bound(set.u, static_cast<double>(kept)), lds);
     p.sum = kept;
     return p;
 }
@@ -684,7 +687,7 @@ struct List {
     u64 run[kList];      // running sums
     uint16_t bins[kList], start[kBins];
     u64 waves[kPick / kWave];
-    int first[3];
+    int first[4];
     u64 likely;
 };
 // The place among the n > 0 entries of a list, in any order, by kPick threads; a barrier is behind the entries.
@@ -766,7 +769,7 @@ __device__ __forceinline__ void choose(int n, const Settings& set, const AnyScal
         total[j] = mine;
     }
     const u64 up = block_scan<kPick / kWave>(mine, waves) - mine;
-    if (tid < 3) first[tid] = n - 1;
+    if (tid < 4) first[tid] = tid < 3 ? n - 1 : n;
     if (tid == 0) likely = plan->before[plan->m0];
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)   // (the scan's barriers are behind `bins`)
@@ -800,25 +803,27 @@ __device__ __forceinline__ void choose(int n, const Settings& set, const AnyScal
         return first[slot];
     };
     u64 kept = plan->all;
+    int end = n - 1;   // the last kept entry
     if (plan->k_bin >= 0) {
         const int last = set.top_k - plan->k_before - 1, of = plan->k_bin;
-        kept = run[place(0, [&](u64, int b, int r) { return b == of && r == last; })];
+        kept = run[end = place(0, [&](u64, int b, int r) { return b == of && r == last; })];
     }
     if (set.top_p < 1.0) {
         const double bound = fmax(set.top_p * static_cast<double>(kept), 1.0);
-        kept = run[place(1, [&](u64 sum, int, int) { return static_cast<double>(sum) >= bound; })];
+        kept = run[end = place(1, [&](u64 sum, int, int) { return static_cast<double>(sum) >= bound; })];
     }
     if (set.min_p > 0.0) {
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
-            if (bin[j] < kBins && bin[j] >= plan->m0 && bin[j] <= plan->m1 &&
-                share_of(logit_of(v[j]), top, set) >= set.min_p)
-                atomicMax(&likely, total[j]);
+            if (bin[j] < kBins && bin[j] >= plan->m0) {
+                if (bin[j] <= plan->m1 && share_of(logit_of(v[j]), top, set) >= set.min_p) atomicMax(&likely, total[j]);
+                else atomicMin(&first[3], base + j);
+            }
         __syncthreads();
-        kept = min(kept, likely);
+        kept = min(kept, likely), end = min(end, max(first[3] - 1, 0));
     }
     const double bound = choice_bound(set.u, static_cast<double>(kept));
-    const int i = place(2, [&](u64 sum, int, int) { return static_cast<double>(sum) > bound; });
+    const int i = set.last ? end : place(2, [&](u64 sum, int, int) { return static_cast<double>(sum) > bound; });
     if (tid == 0) write(static_cast<int>(static_cast<uint32_t>(list[i])), logit_of(list[i]), kept);
 }
 

@@ -121,3 +121,28 @@ def test_groups_of_equal_logits_in_the_largest_rows(v):
     u = [0.9, 0.76, 1 - 2.0 ** -24, 0.8, 0.995, 0.5, 0.97, 0.9]
     check(x, 8, t=t, u=u)
     check(x, 8, t=t, u=u, top_k=[v - 5] * 8, top_p=[0.95] * 8)
+
+
+@pytest.mark.parametrize("limits", ["none", *LIMITS])
+@pytest.mark.parametrize("v,rows_of_a_call", [(2000, 36), (16384, 36), (32000, 1), (32000, 36), (128256, 36), (128256, 1)])
+def test_last_kept_id(v, rows_of_a_call, limits):
+    """u of 1 and more."""
+    rows = 6 if rows_of_a_call == 1 else 36
+    pairs = list(itertools.product(WINNERS, TEMPERATURES))[1::72 // rows]
+    x = confident(rows, v, v + rows + 1, [w for w, _ in pairs])
+    k = [[50, 2, 200, 1, 1000][i % 5] for i in range(rows)]
+    check(x, rows_of_a_call, t=[t for _, t in pairs], u=[[1.0, 2.0, float("inf")][i % 3] for i in range(rows)],
+          **({} if limits in ("none", "min-p") else dict(top_k=k)), **{n: [y] * rows for n, y in LIMITS.get(limits, {}).items()})
+
+
+@pytest.mark.parametrize("v", [4000, 16000, 40000])
+def test_last_kept_id_of_many_likely_ones(v):
+    """Sums past 2^53, whose last ids are a unit or two each; in lists, and by descent (more than 4096 equal ids)."""
+    x = torch.full((6, v), -float("inf"))
+    for i, n in enumerate([1000, 1500, 2000, 3000, v // 2, 3 * v // 4]):
+        x[i, :n] = 0.0
+        x[i, n:n + 600] = -30.0 - 0.25 * (torch.arange(600) % 3)        # 1.6, 1.3 and 1.0 units
+    u = [1.0] * 6
+    check(x, 6, t=[1.0] * 6, u=u)
+    check(x, 6, t=[1.0] * 6, u=u, top_k=[1100, 1601, 2555, 100, v // 2 + 599, 3 * v // 4 + 250])
+    check(x, 6, t=[1.0] * 6, u=u, min_p=[9e-14, 7.5e-14, 0.5, 9e-14, 9e-14, 7.5e-14])
