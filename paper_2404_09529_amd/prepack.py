@@ -660,12 +660,14 @@ class PagedCache:
     """One layer's pages (tensors of the caller's) plus the pp_paged_cache struct that points at them.
 
     page_table int32 [k, max_pages]; k_pages, v_pages [n_pages, page_size, Hkv * D] in the model's type, or int8 with
-    k_scale, v_scale float32 [n_pages, page_size, Hkv] (kv_type PP_KV_I8).  The layers of a model share one table."""
+    k_scale, v_scale float32 [n_pages, page_size, Hkv] (kv_type PP_KV_I8).  The layers of a model share one table.  The
+    calls below refuse a config of other heads than the pages and scales have: the library sees addresses only."""
 
     def __init__(self, kv_type: int, page_table, k_pages, v_pages, k_scale=None, v_scale=None):
         torch = _torch()
         want = {PP_KV_F32: torch.float32, PP_KV_BF16: torch.bfloat16, PP_KV_I8: torch.int8}[kv_type]
         n_pages, page_size, kvw = k_pages.shape
+        self.kvw, self.scale_heads = kvw, None
         if k_pages.dtype != want or v_pages.dtype != want or v_pages.shape != k_pages.shape:
             raise ValueError(f"k_pages and v_pages must be {want} of one shape")
         if page_table.dtype != torch.int32 or page_table.dim() != 2:
@@ -673,8 +675,11 @@ class PagedCache:
         tensors = [page_table, k_pages, v_pages]
         if kv_type == PP_KV_I8:
             for t in (k_scale, v_scale):
-                if t is None or t.dtype != torch.float32 or t.shape[:2] != k_pages.shape[:2] or kvw % t.shape[2]:
+                if t is None or t.dtype != torch.float32 or t.dim() != 3 or t.shape[:2] != k_pages.shape[:2]:
                     raise ValueError("k_scale and v_scale must be float32 [n_pages, page_size, Hkv]")
+            self.scale_heads = k_scale.shape[2]
+            if v_scale.shape != k_scale.shape or self.scale_heads == 0 or kvw % self.scale_heads:
+                raise ValueError("k_scale and v_scale must be float32 [n_pages, page_size, Hkv]")
             tensors += [k_scale, v_scale]
         if not all(t.is_contiguous() for t in tensors):
             raise ValueError("page_table, pages and scales must be contiguous")
@@ -682,38 +687,47 @@ class PagedCache:
         self.struct = PPPagedCache(kv_type=kv_type, k=page_table.shape[0], page_size=page_size,
                                    max_pages=page_table.shape[1], n_pages=n_pages, page_table=_p(page_table),
                                    k_pages=_p(k_pages), v_pages=_p(v_pages), k_scale=_p(k_scale), v_scale=_p(v_scale))
+        self.ref = ctypes.byref(self.struct)
+
+    def of(self, cfg: PPConfig):
+        """The struct for a call with this config, whose key/value heads have to be the pages' own."""
+        heads = cfg.n_kv_heads
+        if self.kvw == heads * cfg.head_dim and (self.scale_heads is None or self.scale_heads == heads):
+            return self.ref
+        raise ValueError(f"pages of {self.kvw} values a token" + (f", scales of {self.scale_heads} heads" if self.scale_heads else "") +
+                         f": the config has {heads} key/value heads of {cfg.head_dim}")
 
 
 def pp_paged_write(cfg: PPConfig, cache: PagedCache, seq, pos, rows: int, keys, ldk: int, values, ldv: int,
                    stream=None) -> None:
     """Rows of keys and values into the pages: row r is token pos[r] of sequence seq[r] (int32 device tensors)."""
-    _check(lib().pp_paged_write(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(seq), _p(pos), rows, _p(keys), ldk,
+    _check(lib().pp_paged_write(ctypes.byref(cfg), cache.of(cfg), _p(seq), _p(pos), rows, _p(keys), ldk,
                                 _p(values), ldv, _stream(stream)), "pp_paged_write")
 
 
 def pp_paged_read(cfg: PPConfig, cache: PagedCache, seq, pos, rows: int, keys, ldk: int, values, ldv: int,
                   stream=None) -> None:
     """The keys and values of the tokens (seq[r], pos[r]) into dense rows."""
-    _check(lib().pp_paged_read(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(seq), _p(pos), rows, _p(keys), ldk,
+    _check(lib().pp_paged_read(ctypes.byref(cfg), cache.of(cfg), _p(seq), _p(pos), rows, _p(keys), ldk,
                                _p(values), ldv, _stream(stream)), "pp_paged_read")
 
 
 def pp_paged_append(cfg: PPConfig, cache: PagedCache, lens, qkv, ldqkv: int, q_out, ldq: int, stream=None) -> None:
     """The newest token of every sequence (position lens[i] - 1): query and key rotated, key and value stored."""
-    _check(lib().pp_paged_append(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(lens), _p(qkv), ldqkv, _p(q_out),
+    _check(lib().pp_paged_append(ctypes.byref(cfg), cache.of(cfg), _p(lens), _p(qkv), ldqkv, _p(q_out),
                                  ldq, _stream(stream)), "pp_paged_append")
 
 
 def pp_paged_attention_workspace_size(cfg: PPConfig, cache: PagedCache) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib().pp_paged_attention_workspace_size(ctypes.byref(cfg), ctypes.byref(cache.struct), ctypes.byref(n)),
+    _check(lib().pp_paged_attention_workspace_size(ctypes.byref(cfg), cache.of(cfg), ctypes.byref(n)),
            "pp_paged_attention_workspace_size")
     return n.value
 
 
 def pp_paged_attention(cfg: PPConfig, cache: PagedCache, lens, q, ldq: int, out, workspace, stream=None) -> None:
     """out [k, H D]: attention of one query row per sequence over its first lens[i] keys."""
-    _check(lib().pp_paged_attention(ctypes.byref(cfg), ctypes.byref(cache.struct), _p(lens), _p(q), ldq, _p(out),
+    _check(lib().pp_paged_attention(ctypes.byref(cfg), cache.of(cfg), _p(lens), _p(q), ldq, _p(out),
                                     _p(workspace), _nbytes(workspace), _stream(stream)), "pp_paged_attention")
 
 
