@@ -147,8 +147,14 @@ __device__ __forceinline__ Settings settings_of(const ppk::Sample& a, int row) {
 __device__ __forceinline__ double share_of(float x, float top, const Settings& s) {
     return x == top ? 1.0 : exp((static_cast<double>(x) - static_cast<double>(top)) / static_cast<double>(s.t));
 }
-// The bound that the chosen id's running sum exceeds, u below 1; it is below the sum.
-__device__ __forceinline__ double choice_bound(double u, double sum) { return fmin(u * sum, nextafter(sum, 0.0)); }
+// Bounds in whole steps, which a running sum exceeds at its place: that of the shortest beginning that reaches top_p of `sum`, and
+// of the chosen id (the last kept one: where all of the sum is there).  Both factors are at most 1 - 2^-24.
+__device__ __forceinline__ u64 share_bound(double top_p, u64 sum) {
+    return static_cast<u64>(ceil(fmax(top_p * static_cast<double>(sum), 1.0))) - 1;
+}
+__device__ __forceinline__ u64 choice_bound(const Settings& s, u64 sum) {
+    return s.last ? sum - 1 : static_cast<u64>(s.u * static_cast<double>(sum));
+}
 
 struct Part {   // of a row, by hist_kernel
     double E;   // -inf: no id that may be chosen
@@ -376,9 +382,9 @@ __device__ __forceinline__ void plan_of(const Settings& set, double E, float top
     }
     int p0 = 0, p1 = -1, m0 = 0, m1 = -1;
     if (set.top_p < 1.0) {
-        const double t0 = fmax(set.top_p * static_cast<double>(lo), 1.0), t1 = fmax(set.top_p * static_cast<double>(hi), 1.0);
-        passing(1, sums, [&](u64 n) { return static_cast<double>(n) >= t0; });
-        passing(2, sums, [&](u64 n) { return static_cast<double>(n) >= t1; });
+        const u64 t0 = share_bound(set.top_p, lo), t1 = share_bound(set.top_p, hi);
+        passing(1, sums, [&](u64 n) { return n > t0; });
+        passing(2, sums, [&](u64 n) { return n > t1; });
         __syncthreads();
         p0 = lds.at[1], p1 = lds.at[2];
         lo = min(lo, sums[p0]), hi = min(hi, sums[p1 + 1]);
@@ -390,10 +396,9 @@ __device__ __forceinline__ void plan_of(const Settings& set, double E, float top
         m0 = min(max(b - 1, 0), kBins - 1), m1 = min(b + 1, kBins - 1);
         lo = min(lo, sums[m0]), hi = min(hi, sums[m1 + 1]);
     }
-    const double u0 = choice_bound(set.u, fmax(static_cast<double>(lo), 1.0)), u1 = choice_bound(set.u, static_cast<double>(hi));
-    lo = max(lo, u64(1));
-    passing(3, sums, [&](u64 n) { return set.last ? n >= lo : static_cast<double>(n) > u0; });
-    passing(4, sums, [&](u64 n) { return set.last ? n >= hi : static_cast<double>(n) > u1; });
+    const u64 u0 = choice_bound(set, max(lo, u64(1))), u1 = choice_bound(set, hi);
+    passing(3, sums, [&](u64 n) { return n > u0; });
+    passing(4, sums, [&](u64 n) { return n > u1; });
     __syncthreads();
     for (int b = tid; b < kBins; b += N) plan->before[b] = sums[b];
     if (tid == 0) {
@@ -524,10 +529,8 @@ __global__ __launch_bounds__(kThreads, 4) void gather_kernel(ppk::Sample a, Spac
 // Where the list is too long: eight bits of the logit at a time, a histogram of counts and sums, the bin in which the
 // bound is passed, then the next eight bits of that bin's ids; equal logits have equal weights, and the id among them is
 // counted off.
-enum Bound { kCount, kReaches, kExceeds };   // count >= bound; sum >= bound; sum > bound
-__device__ __forceinline__ bool passes(Bound b, u64 sum, uint32_t count, double bound) {
-    return b == kCount ? count >= bound : b == kReaches ? static_cast<double>(sum) >= bound : static_cast<double>(sum) > bound;
-}
+enum Bound { kCount, kSum };   // what is to exceed the bound
+__device__ __forceinline__ bool passes(Bound b, u64 sum, uint32_t count, u64 bound) { return (b == kCount ? count : sum) > bound; }
 
 struct Place {
     int id;
@@ -546,7 +549,7 @@ struct Descent {
 };
 
 // The first place, in order, where the running count or sum passes the bound; there is one.
-__device__ Place find(const float* x, int vocab, const AnyScale& sc, const Powers& powers, Bound what, double bound, Descent& lds) {
+__device__ Place find(const float* x, int vocab, const AnyScale& sc, const Powers& powers, Bound what, u64 bound, Descent& lds) {
     const int tid = threadIdx.x, lane = tid % kWave;
     uint32_t prefix = 0, mask = 0, above_n = 0, equal = 0;   // the last digit's ids: equal logits
     u64 above_s = 0;
@@ -629,11 +632,10 @@ __device__ Place descend(const float* x, int vocab, const Settings& set, const A
     count = total(count, lds.wave_count);
     likely_n = total(likely_n, lds.wave_count);
     auto keep = [&](const Place& p) { kept = p.sum, count = p.n; };
-    if (set.top_k && static_cast<uint32_t>(set.top_k) < count) keep(find(x, vocab, sc, powers, kCount, set.top_k, lds));
-    if (set.top_p < 1.0) keep(find(x, vocab, sc, powers, kReaches, fmax(set.top_p * static_cast<double>(kept), 1.0), lds));
+    if (set.top_k && static_cast<uint32_t>(set.top_k) < count) keep(find(x, vocab, sc, powers, kCount, set.top_k - 1, lds));
+    if (set.top_p < 1.0) keep(find(x, vocab, sc, powers, kSum, share_bound(set.top_p, kept), lds));
     kept = min(kept, likely), count = min(count, likely_n);
-    Place p = set.last ? find(x, vocab, sc, powers, kCount, count, lds)
-                       : find(x, vocab, sc, powers, kExceeds, choice_bound(set.u, static_cast<double>(kept)), lds);
+    Place p = set.last ? find(x, vocab, sc, powers, kCount, count - 1, lds) : find(x, vocab, sc, powers, kSum, choice_bound(set, kept), lds);
     p.sum = kept;
     return p;
 }
@@ -809,8 +811,8 @@ __device__ __forceinline__ void choose(int n, const Settings& set, const AnyScal
         kept = run[end = place(0, [&](u64, int b, int r) { return b == of && r == last; })];
     }
     if (set.top_p < 1.0) {
-        const double bound = fmax(set.top_p * static_cast<double>(kept), 1.0);
-        kept = run[end = place(1, [&](u64 sum, int, int) { return static_cast<double>(sum) >= bound; })];
+        const u64 bound = share_bound(set.top_p, kept);
+        kept = run[end = place(1, [&](u64 sum, int, int) { return sum > bound; })];
     }
     if (set.min_p > 0.0) {
 #pragma unroll
@@ -822,8 +824,8 @@ __device__ __forceinline__ void choose(int n, const Settings& set, const AnyScal
         __syncthreads();
         kept = min(kept, likely), end = min(end, max(first[3] - 1, 0));
     }
-    const double bound = choice_bound(set.u, static_cast<double>(kept));
-    const int i = set.last ? end : place(2, [&](u64 sum, int, int) { return static_cast<double>(sum) > bound; });
+    const u64 bound = choice_bound(set, kept);
+    const int i = set.last ? end : place(2, [&](u64 sum, int, int) { return sum > bound; });
     if (tid == 0) write(static_cast<int>(static_cast<uint32_t>(list[i])), logit_of(list[i]), kept);
 }
 
