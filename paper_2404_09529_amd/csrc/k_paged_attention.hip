@@ -18,9 +18,10 @@
 // The query heads are the instructions' columns; with fewer than 16 the rest are zeros (the matrix cores are idle
 // otherwise: a step of 16 KB takes them 384 cycles of the 1600 that a CU's share of the memory needs).
 //
-// bf16 operands hold what is exact in them: bf16 keys, values and queries, and 8-bit codes, whose scales multiply scores
-// and probabilities.  Probabilities (times a value's scale) are two bf16 terms, off by 2^-17, so that the result is as good
-// as its one rounding; with float32 queries over 8-bit pages queries and probabilities are three terms, all of float32's bits.
+// bf16 operands hold what is exact in them: bf16 keys, values and queries, and 8-bit codes, which are turned into bf16 in
+// registers, two for three instructions; their scales multiply scores and probabilities.  Probabilities (times a value's scale) are two
+// bf16 terms, off by 2^-17, so that the result is as good as its one rounding; with float32 queries over 8-bit pages queries and
+// probabilities are three terms, all of float32's bits.
 // float32 pages take the float32 matrix instructions.
 #include <float.h>
 
@@ -37,7 +38,6 @@ constexpr int kBlock = ppk::kPagedWaves * kWave;
 constexpr int kRows = 16;   // query heads of a wavefront
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 // f(0) .. f(N - 1) with constants for arguments.
 template <typename F, int... I>
@@ -248,19 +248,18 @@ struct Tile<D, bf16, bf16> {
     }
 };
 
-// 8-bit pages, without turning codes into numbers one by one.
-// Keys: the query as digits of 7 bits (three, for float32 four; value = sum of digit * 128^i * 2^-shift, exact
-// down to 2^-20, 2^-27 of the row's largest), products of int8 in int32.  K operand of instruction (t, c): dims 64 c + 16 g
-// .. + 15.
-// Values: a code is exact in bf16, the upper half of its float32 form.  Lane's part of a row: dims D / 16 ln ..
+// 8-bit pages.  A code is exact in bf16, the upper half of its float32 form.
+// Keys: the query, brought into -1 .. 1 by a power of two, as one bf16 term (bf16) or three.  K operand of instruction (t, c, h):
+// dims 64 c + 16 g + 8 h .. + 7.
+// Values: lane's part of a row: dims D / 16 ln ..
 template <int D, typename T>
 struct Tile<D, T, int8_t> {
-    static constexpr int NC = D / 64, NJ = D / 16, NV = D / 64, QD = sizeof(T) == 2 ? 3 : 4, PT = sizeof(T) == 2 ? 2 : 3;
+    static constexpr int NC = D / 64, NJ = D / 16, NV = D / 64, QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3;
     u32x4 k[2][NC];
     uint32_t v[8][NV];
     struct Query {
-        i32x4 f[QD][NC];
-        int shift;      // of the row
+        bf16x8 f[QT][NC][2];
+        int shift;      // of the row: the terms' sum is q * 2^shift
         float poison;   // 0; not a number where the row holds no numbers
     };
 
@@ -293,21 +292,16 @@ struct Tile<D, T, int8_t> {
         const bool finite = max16(top < 0x7f800000u ? 0.f : 1.f) == 0.f;
         const float m = max16(__uint_as_float(finite ? top : 0u));
         q.poison = finite ? 0.f : __uint_as_float(0x7fc00000u);
-        q.shift = 7 * QD - 1 - __builtin_amdgcn_frexp_expf(m);   // the largest becomes 2^(7 QD - 2) .. 2^(7 QD - 1)
+        q.shift = -__builtin_amdgcn_frexp_expf(m);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4)
+            for (int e = 0; e < 16; ++e) {
+                bf16 t[QT];
+                terms(finite ? ldexpf(y[c][e], q.shift) : 0.f, t);
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    int n = static_cast<int>(rintf(finite ? ldexpf(y[c][e + b], q.shift) : 0.f));
-#pragma unroll
-                    for (int i = 0; i < QD; ++i) {
-                        const int d = i + 1 < QD ? (n << 25) >> 25 : n;   // -64 .. 63, the last one up to +-65
-                        n = (n - d) >> 7;
-                        q.f[i][c][e / 4] = (b ? q.f[i][c][e / 4] : 0) | (d & 255) << (8 * b);
-                    }
-                }
+                for (int i = 0; i < QT; ++i) q.f[i][c][e / 8][e % 8] = t[i];
+            }
     }
     __device__ __forceinline__ void load_k(int t, const char* p) {
 #pragma unroll
@@ -323,22 +317,25 @@ struct Tile<D, T, int8_t> {
     }
     __device__ __forceinline__ void clear_v(int) {}   // codes are numbers whatever they are
     __device__ __forceinline__ f32x4 scores(int t, const Query& q) const {
-        i32x4 s[QD];
+        f32x4 s = {};
 #pragma unroll
-        for (int i = 0; i < QD; ++i) {
-            s[i] = i32x4{};
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-                s[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, k[t][c]), q.f[i][c], s[i], 0, 0, 0);
-        }
-        f32x4 f;
+            for (int h = 0; h < 2; ++h) {
+                u32x4 f;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {   // |s| < 2^21
-            const float lo = static_cast<float>(s[1][r] * 128 + s[0][r]);
-            const float hi = static_cast<float>(QD == 4 ? s[QD - 1][r] * 128 + s[2][r] : s[2][r]);
-            f[r] = ldexpf(fmaf(hi, 16384.f, lo), -q.shift) + q.poison;
-        }
-        return f;
+                for (int w = 0; w < 2; ++w) {
+                    const uint32_t x = k[t][c][2 * h + w];
+                    f[2 * w] = __builtin_amdgcn_perm(byte_value<1>(x), byte_value<0>(x), 0x07060302u);
+                    f[2 * w + 1] = __builtin_amdgcn_perm(byte_value<3>(x), byte_value<2>(x), 0x07060302u);
+                }
+#pragma unroll
+                for (int i = QT - 1; i >= 0; --i)
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), q.f[i][c][h], s, 0, 0, 0);
+            }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = ldexpf(s[r], -q.shift) + q.poison;
+        return s;
     }
     __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&o)[NJ]) const {
         bf16x8 w[PT];
