@@ -16,12 +16,13 @@
 // so that lane group g (16 lanes) holds the scores of keys 8 g .. 8 g + 7, which is what it has to hold as the operand of
 // O^T = V^T P^T; a lane reads the same 16 (or 8, or 4) columns' part of those 8 rows of V, whole rows per 16 lanes.
 // The query heads are the instructions' columns; with fewer than 16 the rest are zeros (the matrix cores are idle
-// otherwise: a step of 16 KB takes them 384 cycles of the 1600 that a CU's share of the memory needs).
+// otherwise: a step of 16 KB takes them 512 cycles of the 1600 that a CU's share of the memory needs).
 //
-// bf16 operands hold what is exact in them: bf16 keys, values and queries, and 8-bit codes, which are turned into bf16 in
-// registers, two for three instructions; their scales multiply scores and probabilities.  Probabilities (times a value's scale) are two
-// bf16 terms, off by 2^-17, so that the result is as good as its one rounding; with float32 queries over 8-bit pages queries and
-// probabilities are three terms, all of float32's bits.
+// bf16 operands hold all bits of what they stand for: bf16 keys, values and queries and 8-bit codes are exact in one, and
+// probabilities (times a value's scale) and float32 queries are three terms, off by 2^-25.  Codes are turned into bf16 in registers,
+// two for three instructions; their scales multiply scores and probabilities.  (Fewer bits bring no time: probabilities
+// of two terms, and 8-bit keys met by the query's 7-bit digits in the int8 instructions, took 80.1 and 96.3 us for the two calls above
+// where this takes 80.2 and 96.5, and a query with one loud element lost the others.)
 // float32 pages take the float32 matrix instructions.
 #include <float.h>
 
@@ -228,12 +229,12 @@ struct Tile<D, bf16, bf16> {
         return s;
     }
     __device__ __forceinline__ void add(const float (&p)[8], f32x4 (&o)[NJ]) const {
-        bf16x8 hi, lo;
+        bf16x8 w[3];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            bf16 t[2];
+            bf16 t[3];
             terms(p[e], t);
-            hi[e] = t[0], lo[e] = t[1];
+            w[0][e] = t[0], w[1][e] = t[1], w[2][e] = t[2];
         }
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
@@ -242,8 +243,8 @@ struct Tile<D, bf16, bf16> {
             for (int e = 0; e < 4; ++e)
                 f[e] = __builtin_amdgcn_perm(v[2 * e + 1][j / 2], v[2 * e][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
             const bf16x8 a = __builtin_bit_cast(bf16x8, f);
-            o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, hi, o[j], 0, 0, 0);
-            o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, lo, o[j], 0, 0, 0);
+#pragma unroll
+            for (int i = 2; i >= 0; --i) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[i], o[j], 0, 0, 0);
         }
     }
 };
@@ -254,7 +255,7 @@ struct Tile<D, bf16, bf16> {
 // Values: lane's part of a row: dims D / 16 ln ..
 template <int D, typename T>
 struct Tile<D, T, int8_t> {
-    static constexpr int NC = D / 64, NJ = D / 16, NV = D / 64, QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3;
+    static constexpr int NC = D / 64, NJ = D / 16, NV = D / 64, QT = sizeof(T) == 2 ? 1 : 3, PT = 3;
     u32x4 k[2][NC];
     uint32_t v[8][NV];
     struct Query {

@@ -1,12 +1,14 @@
-"""How exact pp_paged_attention's scores are: float32's bits, whatever the pages hold and however large one element of a
-query is."""
+"""How exact pp_paged_attention's scores and probabilities are: float32's bits, whatever the pages hold and however large one
+element of a query is."""
+import math
+
 import pytest
 import torch
 
 from paper_2404_09529_amd import prepack as pp
 
 from .gpu_util import require_gpu
-from .test_gpu_paged import KINDS, TYPES, Pool, check_attention, config, rand, run_attention
+from .test_gpu_paged import KINDS, TYPES, U, Pool, check_attention, config, rand, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +32,42 @@ def test_loud_elements_of_a_query(dtype, kv, lens, loud):
     q = q.to(TYPES[dtype][1])
     got = run_attention(config(H, Hkv, D, dtype), pool, lens, q.view(len(lens), -1).cuda())
     check_attention(got, q.double(), pool, lens, H, dtype)
+
+
+@pytest.mark.parametrize("table", ["narrow", "wide"])
+@pytest.mark.parametrize("kv", ["bf16", "i8"])
+def test_probabilities_that_nearly_cancel(kv, table):
+    """Three keys: the likeliest with the value 0, and two of nearly equal probability with the values 1 and -1.  Scores
+    are exact in float32.  x, a score's distance to the largest in powers of two, is off by 2^-23 of itself (its
+    constant and its product are rounded), 2^x by that (times ln 2), a step of 2^-23 and what the terms leave, 2^-24; sums and
+    products of three keys in three terms add 12 2^-24 of sum p |v|, and the result is rounded once."""
+    k, H, D = 64, 16, 128
+    pool = Pool(kv, k, 1, D, 16, 1 if table == "narrow" else 128, seed=1, spare=1)
+    q = torch.zeros(k, H, D)
+    g = torch.Generator().manual_seed(3)
+    q[:, :, 0] = (0.5 + torch.rand(k, H, generator=g)).bfloat16().float()
+    q[:, :, 1] = 2.0 ** -9
+    for x in (pool.k, pool.v):
+        x.zero_()
+    if kv == "i8":
+        pool.ks.fill_(1.0), pool.vs.fill_(1.0)
+    keys, values = pool.k.view(-1, D), pool.v.view(-1, D)
+    for i in range(k):
+        a, b, m = (pool.row(i, j) for j in range(3))
+        keys[m, 0] = 100
+        keys[a, 0] = keys[b, 0] = 99 - i % 16
+        keys[b, 1] = 1 + i // 16
+        values[a], values[b] = 1, -1
+    pool.to_device()
+    got = run_attention(config(H, 1, D, "bf16"), pool, [3] * k, q.to(torch.bfloat16).view(k, -1).cuda())[:k].double().cpu().view(k, H, D)
+    K, V = pool.values()
+    rows = torch.tensor([[pool.row(i, j) for j in range(3)] for i in range(k)])
+    s = (K[rows, 0][:, None] * q.double()[:, :, None]).sum(-1) / math.sqrt(D)      # [k, H, 3]
+    p = torch.softmax(s, -1)
+    want = (p[:, :, 0] - p[:, :, 1])[..., None].expand(k, H, D)
+    x = (s.amax(-1) - s[..., 0]) / math.log(2)
+    e = x * 2 * U + 2 * U + U
+    tol = ((e + 12 * U) * (p[..., 0] + p[..., 1]))[..., None] + 2.0 ** -8 * want.abs()
+    worst = float(((got - want).abs() / tol).max())
+    print(f"[paged attention] worst error / tolerance {worst:.3f}", flush=True)
+    assert worst <= 1.0
