@@ -571,7 +571,8 @@ pp_status pp_paged_attention_workspace_size(const pp_config* cfg, const pp_paged
  * q [k, H D] in dtype (row stride ldq, a multiple of 8; 16-byte aligned), post-RoPE (pp_paged_append's q_out); out [k, H D]
  * in dtype, 16-byte aligned, no overlap with q.  workspace: >= pp_paged_attention_workspace_size bytes, 256-byte aligned, not used by
  * two calls at a time; its contents do not matter.  Scores, softmax and sums are float32; bf16 results are rounded
- * once.  Deterministic; how the keys are split, and with it the last bits of float32 results, depends on all lengths.
+ * once.  Deterministic; how the keys are split, and with it the last bits of float32 results, depends on all lengths and on
+ * max_pages * page_size (few sequences whose tables reach at most 1024 positions, 512 in float32 pages, are one launch).
  * Errors: as pp_paged_write, PP_ERR_INVALID_ARG (misaligned workspace), PP_ERR_BUFFER_TOO_SMALL (workspace). */
 pp_status pp_paged_attention(const pp_config* cfg, const pp_paged_cache* cache, const int32_t* lens, const void* q,
                              int64_t ldq, void* out, void* workspace, size_t workspace_bytes, void* stream);

@@ -7,8 +7,8 @@
 // is written right away, the pieces of others leave (o, maximum, sum) for join_kernel.  256 workgroups of eight wavefronts,
 // which have neighbouring heads of the same keys, read as fast as anything measured (2 x 415 MB of bf16 rows of 8 heads, reads
 // alone: eight heads to a workgroup, 200 of these, 6.4 TB/s; one head to a workgroup of four, 1600 of these, 5.2).
-// 64 sequences of 8 to 4096 keys, 32 heads in bf16 (400 MB): 75 us, 5.4 TB/s, and 5.5 for the join; 12 of 6000 to 32,768 keys, 8
-// heads in 8 bits (471 MB): 90 us, 5.2 TB/s, and 5.7.  512 workgroups, steps of 64 keys, two sets of registers for what is on the
+// 64 sequences of 8 to 4096 keys, 32 heads in bf16 (400 MB): 76 us, 5.3 TB/s, and 5.5 for the join; 12 of 6000 to 32,768 keys, 8
+// heads in 8 bits (471 MB): 91 us, 5.2 TB/s, and 5.8; 8 of these in float32 (964 MB): 165 us, 5.8 TB/s, and 5.0.  512 workgroups, steps of 64 keys, two sets of registers for what is on the
 // way, non-temporal loads: the same or slower.
 //
 // Nothing passes through LDS on the way: keys go from memory into the registers that the 16 x 16 matrix
@@ -767,9 +767,9 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const float* __restrict__ p
 int heads_of(int H, int Hkv) { return Hkv * ((H / Hkv + kRows - 1) / kRows); }
 
 // Sequences that a short table bounds are a workgroup's each, in one launch, if the workgroups find room at once.  Ranges
-// and their join, and this, in us: one sequence of 500 keys, 8 heads in bf16 10.5 and 8.0, of 1000 12.3 and 12.2, of 2000
-// 12.6 and 22.0; 8 bits, 1000: 13.4 and 11.5; eight sequences of up to 485 keys, 2 heads of 64 in float32, 9.1 and 9.3, of up
-// to 895 10.1 and 13.5.
+// and their join, and this, in us: one sequence of 500 keys, 8 heads in bf16 10.5 and 8.1, of 1000 12.4 and 12.5, of 2000
+// 12.5 and 20.8; 8 bits, 1000: 12.5 and 11.7; eight sequences of up to 485 keys, 2 heads of 64 in float32, 9.5 and 9.4, of up
+// to 895 9.9 and 13.4.  (The lengths are the device's: a short sequence with a long table is split, 285 keys 10.6 rather than 6.6.)
 constexpr int kWhole = 1024, kWholeF32 = 512, kWholeBlocks = 256;
 
 }  // namespace

@@ -4,10 +4,11 @@
 // With the row's ids in order (largest logit first, ties lowest id first) every setting, and the choice itself, asks for
 // the first place where a running count or sum passes a bound.  No row is sorted for that.  In powers of two, y =
 // x log2(e) / T, the weight 2^y is cut into bins of 1/32 octave below an integer exponent E; sums of weights are integers,
-// multiples of 2^(E - 44), the same in whatever order they are formed.
+// multiples of 2^(E - 44), the same in whatever order they are formed.  Ids 45 octaves below E are none.
 //   hist_kernel    a part of a row: its largest logit, E = ceil of its y, and the sum (and for top-k the count) of
 //                  every bin.  E is the part's own: parts differ by whole octaves, that is by shifts, so no pass over the
-//                  row has to come before to find its largest logit.
+//                  row has to come before to find its largest logit.  (What a shift takes behind the row's last bin is none; sums are
+//                  rounded, half a step a bin.)
 //   sum_kernel     the parts' bins together; the bins in which the bounds are passed, or several where one bound depends
 //                  on another's exact place.
 //   gather_kernel  a part's ids in these bins.
@@ -15,10 +16,10 @@
 //                  too long (thousands of nearly equal logits) is resolved by descent through the logit's bits instead.
 // A row that fits one workgroup's registers goes all this way in one launch (row_kernel).  Other rows are split into up to 16
 // parts, so that a few rows fill the chip: the logits are read twice, the second time from
-// the caches.  64 rows of 128,256 logits (33 MB, 6.5 us at a large copy's rate) with settings of their own take 17.5, 9.5, 13.5
+// the caches.  64 rows of 128,256 logits (33 MB, 6.5 us at a large copy's rate) with settings of their own take 19.1, 10.2, 12.8
 // and 16.7 us: about 35 instructions, a third of them float64, and an atomic for each logit, which all workgroups come to together
 // behind their loads; the latency of a workgroup; loads, then prefix sums; the order of the longest list (1,325 ids: 2048
-// entries through 66 comparisons on one CU; lists of a few ids take 6.4).  One row of 32,000: 5.5, 7.5, 4.5 and 6.4 us, each a
+// entries through 66 comparisons on one CU; lists of a few ids take 6.4).  One row of 32,000: 5.9, 8.2, 4.4 and 6.7 us, each a
 // launch and a chain of loads and barriers.
 // (Every row by descent through the bits of its logits, a pass for each of eight bits, as long lists are: 1101 us and 222.)
 #include <algorithm>
