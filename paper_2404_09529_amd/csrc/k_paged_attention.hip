@@ -8,8 +8,8 @@
 // which have neighbouring heads of the same keys, read as fast as anything measured (2 x 415 MB of bf16 rows of 8 heads, reads
 // alone: eight heads to a workgroup, 200 of these, 6.4 TB/s; one head to a workgroup of four, 1600 of these, 5.2).
 // 64 sequences of 8 to 4096 keys, 32 heads in bf16 (400 MB): 76 us, 5.3 TB/s, and 5.5 for the join; 12 of 6000 to 32,768 keys, 8
-// heads in 8 bits (471 MB): 91 us, 5.2 TB/s, and 5.8; 8 of these in float32 (964 MB): 165 us, 5.8 TB/s, and 5.0.  512 workgroups, steps of 64 keys, two sets of registers for what is on the
-// way, non-temporal loads: the same or slower.
+// heads in 8 bits (471 MB): 91 us, 5.2 TB/s, and 5.8; 8 of as many keys in float32 (964 MB): 165 us, 5.8 TB/s, and 5.0.  512
+// workgroups, steps of 64 keys, two sets of registers for what is on the way, non-temporal loads: the same or slower.
 //
 // Nothing passes through LDS on the way: keys go from memory into the registers that the 16 x 16 matrix
 // instructions take them from.  S^T = K Q^T puts key 8 g + 4 t + r of a step into row 4 g + r of score tile t,
